@@ -540,6 +540,138 @@ tw_status tw_weave_layer_auto(const tw_layer_args *layer, int64_t threshold, int
 tw_status tw_weave_tune(const tw_layer_args *layer, int64_t multiple, const int64_t *offsets, int n_offsets, int reps,
                         void *stream_compute, void *stream_comm, int64_t *best_row, float *us);
 
+/*
+ * Attention over a packed batch: what a layer does between two boundaries on the attention side. The
+ * query rows of a sequence are the last of its keys' rows, so one call takes whole prompts (as many
+ * query rows as keys), the later chunks or the second split of a prompt (the keys of the chunks before
+ * included), single decode tokens, and any mix of them.
+ *
+ * Sequence b has the query rows [q_offsets[b], q_offsets[b+1]) of q and out and the keys
+ * [k_offsets[b], k_offsets[b+1]) of k and v, Lq and Lk of them. Query head h uses key head
+ * h / (q_heads / kv_heads). For row i < Lq of head h, over the keys j < Lk that it sees, all of them or
+ * with `causal` those with j <= i + Lk - Lq:
+ *
+ *   s[j]   = scale * q[i,h] . k[j]
+ *   out    = bf16( sum_j exp(s[j] - m) v[j] / sum_j exp(s[j] - m) ),  m = max_j s[j]
+ *   lse    = m + log( sum_j exp(s[j] - m) )
+ *
+ * A row that sees no key (Lk < Lq, or Lk == 0) gets out = 0 and lse = -inf. Keys that a row does not see
+ * have no part in its result, whatever their values: Inf and NaN there stay there. Scores, maxima and
+ * sums are fp32; exp(s[j] - m) is rounded to bf16 where it multiplies v and not where it is summed.
+ *
+ *   q           device bf16, row t, head h, at q + t * q_stride + h * head_dim (strides count elements)
+ *   k, v        device bf16, row t, key head h, at k + t * k_stride + h * head_dim; may be columns of one
+ *               buffer with q (the result of one projection), and of each other
+ *   out         device bf16, like q; must not overlap any input (all byte ranges count from the first
+ *               row to the end of the last, gaps between the rows included)
+ *   lse         device fp32 [q_rows x q_heads], 4-byte aligned, or NULL
+ *   q_offsets   device int32 [n_seqs + 1], ascending: of no more than q_rows rows; read by the kernels.
+ *   k_offsets   the same for k and v. Offsets outside the tensors are taken as their nearest row, so
+ *               that wrong ones give wrong results and nothing else.
+ *               Rows of out and lse outside [q_offsets[0], q_offsets[n_seqs]) are left as they were.
+ *   n_seqs      0 ... TW_MAX_SEQS; with n_seqs == 0 or q_rows == 0 nothing is launched
+ *   q_rows, k_rows   rows of the tensors, sequences or not; q_rows * (q_heads / kv_heads) < 2^31 - 1024
+ *   q_heads     a multiple of kv_heads, at most TW_MAX_HEADS
+ *   head_dim    a multiple of 8 up to TW_MAX_HEAD_DIM; sizes other than 64 and 128 cost what the next of
+ *               the two does
+ *   strides     multiples of 8, at least heads * head_dim, at most TW_MAX_ROW_STRIDE
+ *   scale       finite, > 0
+ *   workspace   device memory of tw_attention_workspace_bytes() for these arguments (0 for many, in which
+ *               case it may be NULL), 16-byte aligned, overwritten; calls that may run at the same time
+ *               need one each
+ *
+ * Where rows and heads alone are too few for the device, each sequence's keys are cut into parts of at
+ * least 512 that work side by side, and a second kernel joins them. The result bits of a row depend
+ * on its own q, its sequence's k and v, and on the form of the launch, which follows from the sizes of
+ * the call (tw_attention_plan): calls of the same form, e.g. one batch and the same batch split in two
+ * large halves, give the same bits.
+ * Errors: TW_ERR_NULL, TW_ERR_SHAPE (sizes; workspace_bytes too few), TW_ERR_ALIGN, TW_ERR_ALIAS,
+ * TW_ERR_UNSUPPORTED (head_dim, strides, counts beyond the above).
+ */
+#define TW_MAX_HEAD_DIM 128
+#define TW_MAX_HEADS 1024
+#define TW_MAX_SEQS (1 << 20)
+#define TW_MAX_ROW_STRIDE (1 << 22)
+
+typedef struct tw_attention_args {
+    const void *q;
+    const void *k;
+    const void *v;
+    void *out;
+    float *lse;
+    const int32_t *q_offsets;
+    const int32_t *k_offsets;
+    int64_t n_seqs;
+    int64_t q_rows;
+    int64_t k_rows;
+    int64_t q_stride;
+    int64_t k_stride;
+    int64_t v_stride;
+    int64_t out_stride;
+    int q_heads;
+    int kv_heads;
+    int head_dim;
+    float scale;
+    int causal;
+} tw_attention_args;
+
+tw_status tw_attention(const tw_attention_args *args, void *workspace, int64_t workspace_bytes, void *stream);
+
+/* Bytes of workspace that tw_attention needs for these sizes (pointers are not looked at); -1 for sizes it refuses. Host only. */
+int64_t tw_attention_workspace_bytes(const tw_attention_args *args);
+
+/*
+ * Tokens to their experts and back: what a layer whose MLP is a set of experts does around their
+ * products. N tokens of top_k experts each make N * top_k pairs; pair p = n * top_k + i is token n's i-th.
+ *
+ * tw_expert_sort puts the pairs in the order of their experts, those of one expert in the order of p:
+ *   order[s]       the pair in place s; the pairs without an expert stand behind all others
+ *   position[p]    its place, the inverse of order, and -1 for a pair without an expert
+ *   offsets[e]     the first place of expert e, offsets[n_experts] the number of pairs that have one: expert
+ *                  e's rows are [offsets[e], offsets[e+1])
+ *   expert_ids     device, [N x top_k] of int32 (id_bytes 4) or int64 (8), aligned to it. An id outside
+ *                  [0, n_experts), e.g. -1, stands for no expert: padding rows, dropped pairs
+ *   order, position   device int32 [N * top_k]; offsets device int32 [n_experts + 1]
+ *   n_experts      1 ... TW_MAX_EXPERTS; top_k 1 ... TW_MAX_TOP_K; N * top_k < 2^31
+ *   workspace      device memory of tw_expert_sort_workspace_bytes(), 4-byte aligned, overwritten (0 bytes for
+ *                  small N); calls that may run at the same time need one each
+ * No atomics order the result: the same ids give the same order every time. With N == 0 only offsets
+ * (all 0) is written.
+ *
+ * tw_expert_dispatch: out[position[p]] = x[n]. Places that no pair has are left as they were.
+ * tw_expert_combine:  out[n] = bf16( sum_i weights[p] * y[position[p]] ), summed in fp32 in the order of i; pairs
+ *   without a place add nothing, and a token without any gets 0. weights NULL: all 1, which is the gradient
+ *   of tw_expert_dispatch (y the gradient of its out, out that of its x).
+ * tw_expert_combine_backward, the gradient of tw_expert_combine with weights, dout the gradient of its out:
+ *   dy[position[p]] = bf16( weights[p] * dout[n] ); dweights[p] = y[position[p]] . dout[n] in fp32, 0 for a pair without
+ *   a place. Rows of dy that no pair has are left as they were. dy may be y (same start address).
+ *   x, out of combine, dout   device bf16 [N x H]
+ *   out of dispatch, y, dy    device bf16 [rows x H]
+ *   position                  device int32 [N x top_k], from tw_expert_sort; a place outside [0, rows) counts as
+ *                             none. No two pairs may have the same place.
+ *   weights, dweights         device fp32 [N x top_k], 4-byte aligned
+ *   H                         a multiple of 8, 8 ... TW_MAX_H
+ * Outputs must not overlap inputs or each other but as stated.
+ */
+#define TW_MAX_EXPERTS 1024
+#define TW_MAX_TOP_K 32
+
+tw_status tw_expert_sort(const void *expert_ids, int id_bytes, int64_t N, int top_k, int n_experts, int32_t *order,
+                         int32_t *position, int32_t *offsets, void *workspace, int64_t workspace_bytes, void *stream);
+
+/* Bytes of workspace that tw_expert_sort needs; -1 for sizes it refuses. Host only. */
+int64_t tw_expert_sort_workspace_bytes(int64_t N, int top_k, int n_experts);
+
+tw_status tw_expert_dispatch(const void *x, const int32_t *position, int64_t N, int top_k, int64_t H, void *out,
+                             int64_t rows, void *stream);
+
+tw_status tw_expert_combine(const void *y, int64_t rows, const int32_t *position, const float *weights, int64_t N,
+                            int top_k, int64_t H, void *out, void *stream);
+
+tw_status tw_expert_combine_backward(const void *dout, const void *y, int64_t rows, const int32_t *position,
+                                     const float *weights, int64_t N, int top_k, int64_t H, void *dy, float *dweights,
+                                     void *stream);
+
 /* Compute units of the current device; -1 when no device can be queried. */
 int tw_device_cu_count(void);
 /* Static, NUL-terminated description of a status code (never NULL). */

@@ -243,6 +243,22 @@ tw_status tw_streams_overlap(void *stream_a, void *stream_b, int *overlap);
 tw_status tw_stream_create_cu_masked(int first_cu, int n_cus, void **stream);
 tw_status tw_stream_destroy(void *stream);
 
+/*
+ * The form of tw_attention's launch for these sizes (pointers are not looked at); all zero where nothing is launched. Calls
+ * of the same form give a row the same bits. Host only.
+ *   tile_rows   rows of a group's list (query rows times the heads that share a key head) to a workgroup
+ *   key_waves   waves that share a tile's keys
+ *   chunks      most parts that a sequence's keys are cut into, of at least min_chunk keys; 1: not cut, no workspace
+ */
+typedef struct tw_attention_launch {
+    int tile_rows;
+    int key_waves;
+    int chunks;
+    int min_chunk;
+} tw_attention_launch;
+
+tw_status tw_attention_plan(const tw_attention_args *args, tw_attention_launch *launch);
+
 #ifdef __cplusplus
 }
 #endif

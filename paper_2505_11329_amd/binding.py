@@ -53,6 +53,19 @@ class LayerArgs(ctypes.Structure):
                 ("Y", _vp), ("gemm_cu_budget", ctypes.c_int), ("schedule", ctypes.c_int)]
 
 
+class AttentionArgs(ctypes.Structure):
+    """struct tw_attention_args"""
+    _fields_ = [("q", _vp), ("k", _vp), ("v", _vp), ("out", _vp), ("lse", _vp), ("q_offsets", _vp), ("k_offsets", _vp),
+                ("n_seqs", _i64), ("q_rows", _i64), ("k_rows", _i64), ("q_stride", _i64), ("k_stride", _i64),
+                ("v_stride", _i64), ("out_stride", _i64), ("q_heads", ctypes.c_int), ("kv_heads", ctypes.c_int),
+                ("head_dim", ctypes.c_int), ("scale", ctypes.c_float), ("causal", ctypes.c_int)]
+
+
+class AttentionLaunch(ctypes.Structure):
+    """struct tw_attention_launch"""
+    _fields_ = [("tile_rows", ctypes.c_int), ("key_waves", ctypes.c_int), ("chunks", ctypes.c_int), ("min_chunk", ctypes.c_int)]
+
+
 class GemmLaunch(ctypes.Structure):
     """struct tw_gemm_launch"""
     _fields_ = [("tile_m", ctypes.c_int), ("tile_n", ctypes.c_int), ("tiles_per_workgroup", ctypes.c_int),
@@ -157,6 +170,22 @@ def lib():
         L.tw_gemm_plan.restype = ctypes.c_int
         L.tw_train_place.argtypes = [ctypes.POINTER(LayerArgs), ctypes.c_int]
         L.tw_train_place.restype = ctypes.c_int
+        L.tw_attention.argtypes = [ctypes.POINTER(AttentionArgs), _vp, _i64, _vp]
+        L.tw_attention.restype = ctypes.c_int
+        L.tw_attention_workspace_bytes.argtypes = [ctypes.POINTER(AttentionArgs)]
+        L.tw_attention_workspace_bytes.restype = _i64
+        L.tw_attention_plan.argtypes = [ctypes.POINTER(AttentionArgs), ctypes.POINTER(AttentionLaunch)]
+        L.tw_attention_plan.restype = ctypes.c_int
+        L.tw_expert_sort.argtypes = [_vp, ctypes.c_int, _i64, ctypes.c_int, ctypes.c_int, _vp, _vp, _vp, _vp, _i64, _vp]
+        L.tw_expert_sort.restype = ctypes.c_int
+        L.tw_expert_sort_workspace_bytes.argtypes = [_i64, ctypes.c_int, ctypes.c_int]
+        L.tw_expert_sort_workspace_bytes.restype = _i64
+        L.tw_expert_dispatch.argtypes = [_vp, _vp, _i64, ctypes.c_int, _i64, _vp, _i64, _vp]
+        L.tw_expert_dispatch.restype = ctypes.c_int
+        L.tw_expert_combine.argtypes = [_vp, _i64, _vp, _vp, _i64, ctypes.c_int, _i64, _vp, _vp]
+        L.tw_expert_combine.restype = ctypes.c_int
+        L.tw_expert_combine_backward.argtypes = [_vp, _vp, _i64, _vp, _vp, _i64, ctypes.c_int, _i64, _vp, _vp, _vp]
+        L.tw_expert_combine_backward.restype = ctypes.c_int
         L.tw_hbm_probe_mixed.argtypes = [_vp, _vp, _i64, ctypes.c_int, ctypes.c_int, ctypes.c_int, _vp]
         L.tw_hbm_probe_mixed.restype = ctypes.c_int
         L.tw_hbm_probe_shaped.argtypes = [_vp, _vp, _i64, ctypes.c_int, ctypes.c_int, ctypes.c_int, ctypes.c_int, _vp]
@@ -439,6 +468,58 @@ def weave_layer_auto(X1, W1, partials, residual, weight, eps, W2, stream_compute
     return (_native or native()).weave_layer_auto(X1, W1, partials, residual, weight, eps, W2, stream_compute, stream_comm,
                                                   fused_cu_budget, gemm_cu_budget, out, residual_out, Y, parent,
                                                   use_parent, join, schedule, threshold, multiple)
+
+
+def attention(q, k, v, q_offsets, k_offsets, causal=True, scale=None, out=None, lse=None, workspace=None, stream=None):
+    """tw_attention: q [rows, q_heads, head_dim], k and v [k_rows, kv_heads, head_dim], whose rows may be strided (columns of
+    one projection's output), offsets int32 [n_seqs + 1]. scale None: 1 / sqrt(head_dim). Returns (out, lse); rows of no
+    sequence are not written in either. workspace None: from torch's allocator, for this call's stream."""
+    return (_native or native()).attention(q, k, v, q_offsets, k_offsets, causal, scale, out, lse, workspace, stream)
+
+
+def expert_sort(expert_ids, n_experts, order=None, position=None, offsets=None, workspace=None, stream=None):
+    """tw_expert_sort: expert_ids int32 or int64 [N, top_k]. Returns (order, position, offsets). workspace: as for attention."""
+    return (_native or native()).expert_sort(expert_ids, n_experts, order, position, offsets, workspace, stream)
+
+
+def expert_dispatch(x, position, out=None, stream=None):
+    """tw_expert_dispatch: x [N, H], position [N, top_k]. Returns out [N * top_k, H] (or as many rows as the given one has);
+    rows without a pair are not written. Its gradient is expert_combine without weights."""
+    return (_native or native()).expert_dispatch(x, position, out, stream)
+
+
+def expert_combine(y, position, weights=None, out=None, stream=None):
+    """tw_expert_combine: y [rows, H], weights float32 [N, top_k] or None for 1. Returns out [N, H]."""
+    return (_native or native()).expert_combine(y, position, weights, out, stream)
+
+
+def expert_combine_backward(dout, y, position, weights, dy=None, dweights=None, stream=None):
+    """tw_expert_combine_backward. Returns (dy, dweights); rows of dy without a pair are not written."""
+    return (_native or native()).expert_combine_backward(dout, y, position, weights, dy, dweights, stream)
+
+
+def _attention_sizes(n_seqs, q_rows, k_rows, q_heads, kv_heads, head_dim):
+    w, kw = q_heads * head_dim, kv_heads * head_dim
+    return AttentionArgs(n_seqs=n_seqs, q_rows=q_rows, k_rows=k_rows, q_stride=w, k_stride=kw, v_stride=kw, out_stride=w,
+                         q_heads=q_heads, kv_heads=kv_heads, head_dim=head_dim, scale=1.0)
+
+
+def attention_workspace_bytes(n_seqs, q_rows, k_rows, q_heads, kv_heads, head_dim):
+    """tw_attention_workspace_bytes for tensors of these sizes; strides do not change it."""
+    a = _attention_sizes(n_seqs, q_rows, k_rows, q_heads, kv_heads, head_dim)
+    return int(lib().tw_attention_workspace_bytes(ctypes.byref(a)))
+
+
+def attention_plan(n_seqs, q_rows, k_rows, q_heads, kv_heads, head_dim):
+    """tw_attention_plan: the form of the launch for tensors of these sizes, an AttentionLaunch."""
+    a, launch = _attention_sizes(n_seqs, q_rows, k_rows, q_heads, kv_heads, head_dim), AttentionLaunch()
+    _check(lib().tw_attention_plan(ctypes.byref(a), ctypes.byref(launch)), "tw_attention_plan")
+    return launch
+
+
+def expert_sort_workspace_bytes(N, top_k, n_experts):
+    """tw_expert_sort_workspace_bytes."""
+    return int(lib().tw_expert_sort_workspace_bytes(int(N), int(top_k), int(n_experts)))
 
 
 GEMM_PHASES = 8

@@ -1,0 +1,707 @@
+// Attention of a packed batch: out = softmax(scale * q k^T) v for each sequence, grouped heads, one pass over the keys.
+//
+// The rows of a sequence's query heads that share a key head are one list: row r of it is query row r / G, head r % G of
+// the group (G = q_heads / kv_heads). So a tile of rows reads each key once for all heads of the group, and a single
+// decode token still has G rows for the matrix cores.
+//
+// A wave owns 32 rows, one to a lane and its partner 32 lanes on. It computes S^T = K Q^T, whose column (a lane's 16
+// values) belongs to one row: the running maximum and sum of the softmax are one register each, and O^T = V^T P^T is
+// rescaled by a factor per lane. P^T needs no exchange between lanes: the order of the keys within a product's depth is
+// free, and V's fragments are read in the order that S^T leaves them in (four keys of one column to a lane by the
+// transposing LDS read).
+//   p = 2^(s c - m), c = scale / ln 2, m the row's maximum of s c; l = sum p; out = (sum p v) / l; lse = (m + log2 l) ln 2
+// p is rounded to bf16 for the product with v, as an operand of the matrix cores has to be (relative 2^-9 each, the
+// sum over keys is in fp32); l sums the unrounded p in fp32.
+#include <algorithm>
+
+#include "tw_internal.h"
+#include "tw_mfma.h"
+
+namespace tw {
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) bf16x4 *lds_bf16x4_ptr_t;
+
+struct AttentionParams {
+    const char *q, *k, *v;
+    char *out;
+    float *lse;
+    const int32_t *q_offsets, *k_offsets;
+    float *part;      // partial sums, then their maxima and sums (one chunk of the keys each), where chunks > 1
+    float *part_ml;
+    int64_t q_rows, k_rows;
+    int64_t q_stride, k_stride, v_stride, out_stride;  // bytes
+    int n_seqs, q_heads, kv_heads, group, dim, causal;
+    int chunks, min_chunk;
+    float c;
+};
+
+static constexpr float kMinusInf = -__builtin_inff();
+static constexpr float kLn2 = 0.693147180559945309f;
+
+// The matrix instruction of M x M results, depth 512 / M: operands are 8 values of one row (or column) to a lane, lane l
+// holding row l % M and the l / M-th eight of the depth; of the result's column l % M it holds rows
+// U (i / 4) + 4 (l / M) + i % 4, U = 256 / M.
+template <int M>
+struct Mfma;
+template <>
+struct Mfma<32> {
+    using acc = f32x16;
+    static __device__ __forceinline__ acc run(bf16x8 a, bf16x8 b, acc c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
+};
+template <>
+struct Mfma<16> {
+    using acc = f32x4;
+    static __device__ __forceinline__ acc run(bf16x8 a, bf16x8 b, acc c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+};
+
+// Over the lanes of one row, 16 or 32 apart; all of them end with the same bits.
+__device__ __forceinline__ float swap_max16(float v)
+{
+    const unsigned u = __builtin_bit_cast(unsigned, v);
+    const auto r = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+    return fmaxf(__builtin_bit_cast(float, static_cast<unsigned>(r[0])), __builtin_bit_cast(float, static_cast<unsigned>(r[1])));
+}
+__device__ __forceinline__ float swap_max32(float v)
+{
+    const unsigned u = __builtin_bit_cast(unsigned, v);
+    const auto r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+    return fmaxf(__builtin_bit_cast(float, static_cast<unsigned>(r[0])), __builtin_bit_cast(float, static_cast<unsigned>(r[1])));
+}
+template <int M>
+__device__ __forceinline__ float row_max(float v)
+{
+    return swap_max32(M == 16 ? swap_max16(v) : v);
+}
+template <int M>
+__device__ __forceinline__ float row_sum(float v)
+{
+    return swap_add32(M == 16 ? swap_add16(v) : v);
+}
+
+// Sequence b's rows, clamped to the tensors whatever the offsets say.
+struct Sequence {
+    int64_t q0, k0;
+    int q_len, k_len;
+};
+__device__ __forceinline__ int clamp_row(int row, int from, int64_t rows)
+{
+    return min(max(row, from), static_cast<int>(rows));
+}
+__device__ __forceinline__ Sequence sequence(const AttentionParams &p, int b)
+{
+    // (b is the same in all lanes; what is loaded with it is made so for the compiler, too)
+    const int q0 = clamp_row(__builtin_amdgcn_readfirstlane(p.q_offsets[b]), 0, p.q_rows);
+    const int q1 = clamp_row(__builtin_amdgcn_readfirstlane(p.q_offsets[b + 1]), q0, p.q_rows);
+    const int k0 = clamp_row(__builtin_amdgcn_readfirstlane(p.k_offsets[b]), 0, p.k_rows);
+    const int k1 = clamp_row(__builtin_amdgcn_readfirstlane(p.k_offsets[b + 1]), k0, p.k_rows);
+    return {q0, k0, q1 - q0, k1 - k0};
+}
+
+// The sequence that the `tile`-th tile of TILE rows of the batch is of, and its place there; false past the last one.
+// Every wave finds it by itself: 64 sequences at a time, a lane each.
+template <int TILE>
+__device__ __forceinline__ bool find_tile(const AttentionParams &p, int64_t tile, int *seq, int *at)
+{
+    const int lane = threadIdx.x & 63;
+    for (int b0 = 0; b0 < p.n_seqs; b0 += 64) {
+        const int b = b0 + lane;
+        int n = 0;
+        if (b < p.n_seqs) {
+            const int q0 = clamp_row(p.q_offsets[b], 0, p.q_rows), q1 = clamp_row(p.q_offsets[b + 1], q0, p.q_rows);
+            n = ((q1 - q0) * p.group + TILE - 1) / TILE;
+        }
+        int upto = n;
+        for (int d = 1; d < 64; d <<= 1) {
+            const int o = __shfl_up(upto, d);
+            if (lane >= d) upto += o;
+        }
+        const int total = __builtin_amdgcn_readlane(upto, 63);
+        if (tile < total) {
+            const int first = __builtin_ctzll(__ballot(upto > tile));
+            *seq = b0 + first;
+            const int of = __builtin_amdgcn_readlane(n, first);
+            // the last tiles first: under a causal mask they have the most keys
+            *at = of - 1 - static_cast<int>(tile - (__builtin_amdgcn_readlane(upto, first) - of));
+            return true;
+        }
+        tile -= total;
+    }
+    return false;
+}
+
+// The keys [begin, end) of chunk c of a sequence.
+struct Keys {
+    int begin, end;
+};
+__device__ __forceinline__ Keys chunk_keys(const AttentionParams &p, int k_len, int c)
+{
+    if (p.chunks == 1) return {0, k_len};
+    const int each = max(p.min_chunk, (((k_len + p.chunks - 1) / p.chunks) + 127) & ~127);
+    const int64_t b = static_cast<int64_t>(each) * c;
+    if (b >= k_len) return {0, 0};
+    return {static_cast<int>(b), static_cast<int>(min(b + each, static_cast<int64_t>(k_len)))};
+}
+
+// DP: head size padded to 64 or 128. M: rows of a wave (and the matrix instruction). WR waves of a workgroup have M rows
+// each, and each such group of rows has WK waves that share the keys: of a tile of WK * KEYS keys in LDS, KEYS for each.
+template <int DP, int M, int WR, int WK, int KEYS, int STAGES>
+struct AttentionShape {
+    static constexpr int kWaves = WR * WK;
+    static constexpr int kThreads = 64 * kWaves;
+    static constexpr int kRows = M * WR;
+    static constexpr int kKeys = WK * KEYS;
+    static constexpr int kRowBytes = DP * 2;
+    static constexpr int kTileBytes = kKeys * kRowBytes;  // K or V
+    static constexpr int kStageBytes = 2 * kTileBytes;
+    static constexpr int kPieces = DP / 8;  // 16-byte pieces of a row
+    static constexpr int kRowsPerPass = kThreads / kPieces;
+    static constexpr int kPasses = kKeys / kRowsPerPass;
+    static constexpr int kJoinBytes = WK == 1 ? 0 : kRows * WK * (DP + 2) * 4;
+    static constexpr int kLds = STAGES * kStageBytes > kJoinBytes ? STAGES * kStageBytes : kJoinBytes;
+    static_assert(kRowsPerPass % 16 == 0 && kPasses * kRowsPerPass == kKeys, "a thread's pieces have one swizzle");
+    static_assert(WK == 1 || 64 * WK / M == 16, "sixteen threads join a row");
+};
+
+// Where piece c of row r of a tile lies: at c XOR the row's swizzle. K's rows are read one piece of each of 16 rows at a
+// time, V's by 8-byte halves, 32 or 64 bytes of each of eight rows, four neighbouring ones among them. What is read together
+// lies in different LDS banks.
+template <int DP>
+__device__ __forceinline__ constexpr int k_swizzle(int r)
+{
+    return DP == 128 ? (r & 15) : ((r >> 1) & 7);
+}
+template <int DP>
+__device__ __forceinline__ constexpr int v_swizzle(int r)
+{
+    return DP == 128 ? (((r & 3) << 2) | (((r >> 2) & 1) << 1) | ((r >> 3) & 1)) : ((((r >> 1) & 1) << 2) | (((r >> 2) & 1) << 1));
+}
+
+// A bit in each half of a pair that holds Inf or NaN, and the pair with zeros in their place.
+__device__ __forceinline__ uint32_t infinite_bf16x2(uint32_t x) { return ((x & 0x7f807f80u) + 0x00800080u) & 0x80008000u; }
+__device__ __forceinline__ uint32_t finite_bf16x2(uint32_t x)
+{
+    const uint32_t bad = infinite_bf16x2(x);
+    return x & ~((bad - (bad >> 15)) | bad);
+}
+
+template <int DP, int M, int WR, int WK, int KEYS, int STAGES, bool SCAN>
+__global__ __launch_bounds__(64 * WR * WK, 2) void attention_kernel(AttentionParams p)
+{
+    using Shape = AttentionShape<DP, M, WR, WK, KEYS, STAGES>;
+    using Acc = typename Mfma<M>::acc;
+    constexpr int kDepth = 512 / M, kUnit = 256 / M;  // of a product; keys (or columns of O) to four values of a lane
+    constexpr int kSteps = DP / kDepth;                // products in a block of Q K^T
+    constexpr int kKeyBlocks = KEYS / M;               // blocks of S
+    constexpr int kBlocks = DP / M;                    // blocks of columns of O
+    constexpr int kAcc = M * M / 64, kQuads = kAcc / 4;
+    constexpr int kSlices = KEYS / kDepth;             // products in a block of O
+    extern __shared__ __align__(16) char lds[];
+    __shared__ int flags[STAGES * Shape::kWaves];  // a wave's part of the V tile holds Inf or NaN; where rows see a part of the tile
+    const int lane = threadIdx.x & 63, part8 = lane / M, row_lane = lane % M;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wr = wave / WK, wk = wave % WK;
+
+    const int kv_head = blockIdx.x % p.kv_heads;
+    const int rest = blockIdx.x / p.kv_heads;
+    const int chunk = rest % p.chunks;
+    int seq = rest / p.chunks, tile = 0;
+    if constexpr (SCAN) {
+        if (!find_tile<Shape::kRows>(p, rest / p.chunks, &seq, &tile)) return;
+        seq = __builtin_amdgcn_readfirstlane(seq);
+        tile = __builtin_amdgcn_readfirstlane(tile);
+    }
+    const Sequence s = sequence(p, seq);
+    const int list = s.q_len * p.group;  // rows of the group's list
+    const Keys keys = chunk_keys(p, s.k_len, chunk);
+    const int past = s.k_len - s.q_len;
+
+    // where this thread's 16-byte pieces of a K and a V tile come from, and go to
+    const int piece = threadIdx.x % Shape::kPieces, piece_row = threadIdx.x / Shape::kPieces;
+    const uint32_t k_from = piece * 8 < p.dim ? static_cast<uint32_t>(piece_row * p.k_stride + piece * 16) : kPastTensor;
+    const uint32_t v_from = piece * 8 < p.dim ? static_cast<uint32_t>(piece_row * p.v_stride + piece * 16) : kPastTensor;
+    const int k_to = piece_row * Shape::kRowBytes + ((piece ^ k_swizzle<DP>(piece_row)) << 4);
+    const int v_to = Shape::kTileBytes + piece_row * Shape::kRowBytes + ((piece ^ v_swizzle<DP>(piece_row)) << 4);
+    const char *const k_head = p.k + s.k0 * p.k_stride + static_cast<int64_t>(kv_head) * p.dim * 2;
+    const char *const v_head = p.v + s.k0 * p.v_stride + static_cast<int64_t>(kv_head) * p.dim * 2;
+
+    // fragments' places in a tile
+    const int k_frag = (wk * KEYS + row_lane) * Shape::kRowBytes;
+    const int k_piece = (part8 ^ k_swizzle<DP>(row_lane)) << 4;  // a step on is a step's pieces on: XOR
+    const int i16 = lane & 15, v_row = wk * KEYS + 4 * part8 + (i16 >> 2);
+    const int v_frag = Shape::kTileBytes + v_row * Shape::kRowBytes + (i16 & 1) * 8;
+    const int v_piece = (((lane / 16) % (M / 16) * 2 + ((i16 & 3) >> 1)) ^ v_swizzle<DP>(v_row)) << 4;
+
+    // In the form without a scan a workgroup has all tiles of its sequence (one, as a rule).
+    for (;; ++tile) {
+        if (tile * Shape::kRows >= list) return;
+        const int r = tile * Shape::kRows + wr * M + row_lane;
+        const int pos = r / p.group, head = kv_head * p.group + r % p.group;
+        const bool real = r < list;
+        // keys [0, last] are visible to this lane's row
+        const int last = real ? min(p.causal ? pos + past : s.k_len - 1, keys.end - 1) : -1;
+        const int last_pos = (min((tile + 1) * Shape::kRows, list) - 1) / p.group;
+        const int end = min(keys.end, p.causal ? last_pos + past + 1 : s.k_len);
+        // the first row of the wave, and of the tile, sees the fewest keys
+        const int first_last = __builtin_amdgcn_readfirstlane(last);
+        const int tile_first_last = min(keys.end - 1, p.causal ? tile * Shape::kRows / p.group + past : s.k_len - 1);
+
+        bf16x8 qf[kSteps];
+#pragma unroll
+        for (int t = 0; t < kSteps; ++t) {
+            u32x4 x = {0, 0, 0, 0};
+            const int col = t * kDepth + part8 * 8;
+            if (real && col < p.dim)
+                x = *reinterpret_cast<const u32x4 *>(p.q + (s.q0 + pos) * p.q_stride + (static_cast<int64_t>(head) * p.dim + col) * 2);
+            qf[t] = __builtin_bit_cast(bf16x8, x);
+        }
+        Acc o[kBlocks];
+#pragma unroll
+        for (int b = 0; b < kBlocks; ++b) o[b] = Acc{};
+        float m = kMinusInf, l = 0.0f;
+
+        u32x4 kr[Shape::kPasses], vr[Shape::kPasses];
+        auto load = [&](int key0) {
+            const int rows = min(Shape::kKeys, end - key0);  // rows past the last visible key read as zeros
+            const auto rk = make_rsrc(k_head + static_cast<int64_t>(key0) * p.k_stride,
+                                      rows > 0 ? static_cast<uint32_t>((rows - 1) * p.k_stride + p.dim * 2) : 0);
+            const auto rv = make_rsrc(v_head + static_cast<int64_t>(key0) * p.v_stride,
+                                      rows > 0 ? static_cast<uint32_t>((rows - 1) * p.v_stride + p.dim * 2) : 0);
+#pragma unroll
+            for (int i = 0; i < Shape::kPasses; ++i) {
+                kr[i] = __builtin_amdgcn_raw_buffer_load_b128(rk, k_from, static_cast<int>(i * Shape::kRowsPerPass * p.k_stride), 0);
+                vr[i] = __builtin_amdgcn_raw_buffer_load_b128(rv, v_from, static_cast<int>(i * Shape::kRowsPerPass * p.v_stride), 0);
+            }
+        };
+        auto store = [&](int stage, int key0) {
+            if (key0 + Shape::kKeys - 1 > tile_first_last) {  // a tile that some row sees a part of
+                uint32_t bad = 0;
+#pragma unroll
+                for (int i = 0; i < Shape::kPasses; ++i)
+#pragma unroll
+                    for (int w = 0; w < 4; ++w) bad |= infinite_bf16x2(vr[i][w]);
+                const bool any = __any(bad != 0);
+                if (lane == 0) flags[stage * Shape::kWaves + wave] = any;
+            }
+#pragma unroll
+            for (int i = 0; i < Shape::kPasses; ++i) {
+                const int at = stage * Shape::kStageBytes + i * Shape::kRowsPerPass * Shape::kRowBytes;
+                *reinterpret_cast<u32x4 *>(lds + at + k_to) = kr[i];
+                *reinterpret_cast<u32x4 *>(lds + at + v_to) = vr[i];
+            }
+        };
+        auto compute = [&](int key0, int stage, auto masked) {
+            const char *const base = lds + stage * Shape::kStageBytes;
+            Acc sc[kKeyBlocks];
+#pragma unroll
+            for (int n = 0; n < kKeyBlocks; ++n) {
+                sc[n] = Acc{};
+#pragma unroll
+                for (int t = 0; t < kSteps; ++t) {
+                    const bf16x8 kf = *reinterpret_cast<const bf16x8 *>(base + k_frag + n * M * Shape::kRowBytes + (k_piece ^ (t * kDepth * 2)));
+                    sc[n] = Mfma<M>::run(kf, qf[t], sc[n]);
+                }
+            }
+            const int wave_key0 = key0 + wk * KEYS;
+            if constexpr (decltype(masked)::value) {
+                const int seen = last - wave_key0 - 4 * part8;
+#pragma unroll
+                for (int n = 0; n < kKeyBlocks; ++n)
+#pragma unroll
+                    for (int i = 0; i < kAcc; ++i)
+                        if (n * M + kUnit * (i / 4) + i % 4 > seen) sc[n][i] = kMinusInf;
+            }
+            float top = sc[0][0];
+#pragma unroll
+            for (int n = 0; n < kKeyBlocks; ++n)
+#pragma unroll
+                for (int i = 0; i < kAcc; ++i) top = fmaxf(top, sc[n][i]);
+            top = row_max<M>(top) * p.c;
+            const float m_new = fmaxf(m, top);
+            const float m_use = m_new == kMinusInf ? 0.0f : m_new;
+            const float alpha = __builtin_amdgcn_exp2f(m - m_use);
+            m = m_new;
+            l *= alpha;
+#pragma unroll
+            for (int n = 0; n < kKeyBlocks; ++n)
+#pragma unroll
+                for (int i = 0; i < kAcc; ++i) {
+                    sc[n][i] = __builtin_amdgcn_exp2f(fmaf(sc[n][i], p.c, -m_use));
+                    l += sc[n][i];
+                }
+#pragma unroll
+            for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+                for (int i = 0; i < kAcc; ++i) o[b][i] *= alpha;
+            auto add_values = [&](auto clean) {
+#pragma unroll
+                for (int t = 0; t < kSlices; ++t) {
+                    u32x4 pf;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int at = t * 8 + 2 * i;  // among all the lane's values of S
+                        pf[i] = pack_bf16x2(sc[at / kAcc][at % kAcc], sc[(at + 1) / kAcc][(at + 1) % kAcc]);
+                    }
+#pragma unroll
+                    for (int b = 0; b < kBlocks; ++b) {
+                        u32x4 vf;
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) {
+                            // a unit of eight rows on, the swizzle of 128 columns differs by a piece
+                            const int at = (t * kDepth + e * kUnit) * Shape::kRowBytes + (v_piece ^ (b * M * 2) ^ (DP == 128 && M == 32 ? e << 4 : 0));
+                            const u32x2 x = __builtin_bit_cast(
+                                u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4_ptr_t)(base + v_frag + at)));
+                            vf[2 * e] = decltype(clean)::value ? finite_bf16x2(x[0]) : x[0];
+                            vf[2 * e + 1] = decltype(clean)::value ? finite_bf16x2(x[1]) : x[1];
+                        }
+                        o[b] = Mfma<M>::run(__builtin_bit_cast(bf16x8, vf), __builtin_bit_cast(bf16x8, pf), o[b]);
+                    }
+                }
+            };
+            if constexpr (decltype(masked)::value) {
+                bool infinite = false;
+#pragma unroll
+                for (int w = 0; w < Shape::kWaves; ++w) infinite |= flags[stage * Shape::kWaves + w] != 0;
+                if (__builtin_expect(__builtin_amdgcn_readfirstlane(infinite), 0)) {
+                    // Inf and NaN of hidden keys must not meet a p of zero: left out of the product, and added to the
+                    // rows that see them (p > 0 times one of them is the same)
+                    add_values(std::true_type{});
+#pragma unroll 1
+                    for (int j = 0; j < KEYS; ++j) {
+                        const int row = wk * KEYS + j;
+                        const bool sees = wave_key0 + j <= last;
+#pragma unroll
+                        for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+                            for (int g = 0; g < kQuads; ++g) {
+                                const int col = b * M + g * kUnit + part8 * 4;
+                                const u32x2 x = *reinterpret_cast<const u32x2 *>(
+                                    base + Shape::kTileBytes + row * Shape::kRowBytes + (((col >> 3) ^ v_swizzle<DP>(row)) << 4) + (col & 4) * 2);
+#pragma unroll
+                                for (int i = 0; i < 4; ++i) {
+                                    const uint32_t bits = i & 1 ? x[i >> 1] & 0xffff0000u : x[i >> 1] << 16;
+                                    o[b][g * 4 + i] += sees && (bits & 0x7f800000u) == 0x7f800000u ? __uint_as_float(bits) : 0.0f;
+                                }
+                            }
+                    }
+                    return;
+                }
+            }
+            add_values(std::false_type{});
+        };
+
+        // this chunk's tiles; a tile of keys that no row sees is not read
+        const int key_begin = keys.begin;
+        int stage = 0;
+        if (key_begin < end) {
+            load(key_begin);
+            for (int key0 = key_begin; key0 < end; key0 += Shape::kKeys) {
+                store(stage, key0);
+                if (key0 + Shape::kKeys < end) load(key0 + Shape::kKeys);
+                __syncthreads();
+                const int wave_key0 = key0 + wk * KEYS;
+                if (first_last >= wave_key0 + KEYS - 1) compute(key0, stage, std::false_type{});
+                else if (__any(last >= wave_key0)) compute(key0, stage, std::true_type{});
+                if (STAGES == 1) __syncthreads();
+                else stage ^= 1;
+            }
+        }
+        l = row_sum<M>(l);
+
+        // a row's maximum and sum, and four of its columns
+        auto put_row = [&](int64_t at, float m_row, float l_row) {
+            if (p.chunks > 1) {
+                float *const to = p.part_ml + (chunk * p.q_rows * p.q_heads + at) * 2;
+                to[0] = m_row;
+                to[1] = l_row;
+            } else if (p.lse) {
+                p.lse[at] = l_row == 0.0f ? kMinusInf : (m_row + __builtin_amdgcn_logf(l_row)) * kLn2;
+            }
+        };
+        auto put4 = [&](int64_t row, int of_head, int col, f32x4 x, float inv) {
+            if (col >= p.dim) return;
+            if (p.chunks > 1) {
+                const int64_t slot = (chunk * p.q_rows + row) * p.q_heads + of_head;
+                *reinterpret_cast<f32x4 *>(p.part + slot * p.dim + col) = x;
+            } else {
+                const u32x2 y = {pack_bf16x2(x[0] * inv, x[1] * inv), pack_bf16x2(x[2] * inv, x[3] * inv)};
+                *reinterpret_cast<u32x2 *>(p.out + row * p.out_stride + (static_cast<int64_t>(of_head) * p.dim + col) * 2) = y;
+            }
+        };
+        // (a chunk of no keys has no columns to put: the sum of 0 says so)
+        const bool put_columns = p.chunks == 1 || keys.begin < keys.end;
+        if constexpr (WK == 1) {
+            if (real) {
+                if (part8 == 0) put_row((s.q0 + pos) * p.q_heads + head, m, l);
+                // a row that sees no key has l = 0
+                const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+                if (put_columns) {
+#pragma unroll
+                    for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+                        for (int g = 0; g < kQuads; ++g)
+                            put4(s.q0 + pos, head, b * M + g * kUnit + part8 * 4,
+                                 f32x4{o[b][g * 4], o[b][g * 4 + 1], o[b][g * 4 + 2], o[b][g * 4 + 3]}, inv);
+                }
+            }
+        } else {
+            // the waves' maxima, sums and sums of v pass through the LDS and are joined in the order of the waves, by
+            // sixteen threads to a row
+            __syncthreads();
+            float *const part = reinterpret_cast<float *>(lds);
+            float *const ml = part + WK * Shape::kRows * DP;
+            const int slot = wk * Shape::kRows + wr * M + row_lane;
+#pragma unroll
+            for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+                for (int g = 0; g < kQuads; ++g) {
+                    const int c = ((b * M + g * kUnit) / 4 + part8) ^ (row_lane & 7);
+                    *reinterpret_cast<f32x4 *>(part + slot * DP + c * 4) =
+                        f32x4{o[b][g * 4], o[b][g * 4 + 1], o[b][g * 4 + 2], o[b][g * 4 + 3]};
+                }
+            if (part8 == 0) {
+                ml[slot * 2] = m;
+                ml[slot * 2 + 1] = l;
+            }
+            __syncthreads();
+            constexpr int kFours = DP / 64;  // of a thread's columns
+            const int jr = threadIdx.x >> 4, j16 = threadIdx.x & 15, r_join = tile * Shape::kRows + jr;
+            if (r_join < list) {
+                float top = kMinusInf, sum = 0.0f;
+#pragma unroll
+                for (int w = 0; w < WK; ++w) top = fmaxf(top, ml[(w * Shape::kRows + jr) * 2]);
+                const float top_use = top == kMinusInf ? 0.0f : top;
+                f32x4 x[kFours] = {};
+#pragma unroll
+                for (int w = 0; w < WK; ++w) {
+                    const int from = w * Shape::kRows + jr;
+                    const float f = __builtin_amdgcn_exp2f(ml[from * 2] - top_use);
+                    sum += f * ml[from * 2 + 1];
+#pragma unroll
+                    for (int b = 0; b < kFours; ++b)
+                        x[b] += f * *reinterpret_cast<const f32x4 *>(part + from * DP + ((b * 16 + j16) ^ (jr & 7)) * 4);
+                }
+                const int64_t row = s.q0 + r_join / p.group;
+                const int of_head = kv_head * p.group + r_join % p.group;
+                if (j16 == 0) put_row(row * p.q_heads + of_head, top, sum);
+                const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+                if (put_columns) {
+#pragma unroll
+                    for (int b = 0; b < kFours; ++b) put4(row, of_head, (b * 16 + j16) * 4, x[b], inv);
+                }
+            }
+        }
+        if constexpr (SCAN) return;
+        __syncthreads();
+    }
+}
+
+// The chunks of one row and head joined: a wave each, lane c of it with chunk c's maximum and sum.
+__global__ __launch_bounds__(256) void attention_join_kernel(AttentionParams p)
+{
+    const int lane = threadIdx.x & 63;
+    const int64_t at = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6);
+    const int64_t row = at / p.q_heads;
+    // rows of no sequence stay as they are
+    if (row >= p.q_rows || row < p.q_offsets[0] || row >= p.q_offsets[p.n_seqs]) return;
+    const int64_t step = p.q_rows * p.q_heads;
+    float m = kMinusInf, l = 0.0f;
+    if (lane < p.chunks) {
+        m = p.part_ml[(lane * step + at) * 2];
+        l = p.part_ml[(lane * step + at) * 2 + 1];
+    }
+    const bool empty = m == kMinusInf;
+    float top = m;
+    for (int d = 32; d; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
+    const float f = empty ? 0.0f : __builtin_amdgcn_exp2f(m - top);
+    const float sum = group_sum(empty && l == 0.0f ? 0.0f : f * l, 6);
+    const int c0 = lane * 2;
+    float a = 0.0f, b = 0.0f;
+    uint64_t live = __ballot(!(empty && l == 0.0f));
+    while (live) {
+        const int c = __builtin_ctzll(live);
+        live &= live - 1;
+        const float w = __shfl(f, c);
+        if (c0 < p.dim) {
+            const float2 x = *reinterpret_cast<const float2 *>(p.part + (c * step + at) * p.dim + c0);
+            a = fmaf(w, x.x, a);
+            b = fmaf(w, x.y, b);
+        }
+    }
+    const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+    if (p.lse && lane == 0) p.lse[at] = sum == 0.0f ? kMinusInf : (top + __builtin_amdgcn_logf(sum)) * kLn2;
+    if (c0 < p.dim)
+        *reinterpret_cast<uint32_t *>(p.out + row * p.out_stride + ((at - row * p.q_heads) * p.dim + c0) * 2) =
+            pack_bf16x2(a * inv, b * inv);
+}
+
+// ---- host ----
+
+static uint64_t span(int64_t rows, int64_t stride, int64_t width)
+{
+    return rows == 0 ? 0 : (static_cast<uint64_t>(rows - 1) * stride + width) * 2u;
+}
+
+static tw_status attention_sizes(const tw_attention_args &a)
+{
+    if (a.n_seqs < 0 || a.q_rows < 0 || a.k_rows < 0 || a.q_heads < 1 || a.kv_heads < 1 || a.head_dim < 1) return TW_ERR_SHAPE;
+    if (a.q_heads % a.kv_heads != 0) return TW_ERR_SHAPE;
+    if (!(a.scale > 0.0f) || !(a.scale <= 3.402823466e+38f)) return TW_ERR_SHAPE;
+    if (a.head_dim % 8 != 0 || a.head_dim > TW_MAX_HEAD_DIM) return TW_ERR_UNSUPPORTED;
+    if (a.q_heads > TW_MAX_HEADS || a.n_seqs > TW_MAX_SEQS) return TW_ERR_UNSUPPORTED;
+    const int64_t wq = static_cast<int64_t>(a.q_heads) * a.head_dim, wk = static_cast<int64_t>(a.kv_heads) * a.head_dim;
+    if (a.q_stride < wq || a.out_stride < wq || a.k_stride < wk || a.v_stride < wk) return TW_ERR_SHAPE;
+    for (const int64_t s : {a.q_stride, a.k_stride, a.v_stride, a.out_stride})
+        if (s % 8 != 0 || s > TW_MAX_ROW_STRIDE) return TW_ERR_UNSUPPORTED;
+    // offsets are 32-bit, and so are the places in a group's list of rows
+    if (a.q_rows * (a.q_heads / a.kv_heads) > INT32_MAX - 1024 || a.q_rows > INT32_MAX - 1024 || a.k_rows > INT32_MAX - 1024)
+        return TW_ERR_UNSUPPORTED;
+    return TW_OK;
+}
+
+// How a call is launched.
+struct AttentionPlan {
+    bool few;       // tiles of 16 rows whose four waves share the keys; otherwise 256 rows, each wave 32 of its own
+    int chunks;     // parts of each sequence's keys, joined by a second kernel where there are more than one
+    int min_chunk;  // fewest keys of a part but the last
+};
+
+static AttentionPlan attention_plan(const tw_attention_args &a)
+{
+    AttentionPlan plan;
+    const int64_t group = a.q_heads / a.kv_heads, list = a.q_rows * group;
+    plan.few = list <= 16 * a.n_seqs;
+    const int64_t tiles = (plan.few ? a.n_seqs : list / 256 + 1) * a.kv_heads;
+    const int64_t keys = a.k_rows / a.n_seqs;
+    plan.min_chunk = 512;
+    int64_t chunks = 1;
+    if (tiles < 512) chunks = std::min<int64_t>((1024 + tiles - 1) / tiles, (keys + plan.min_chunk - 1) / plan.min_chunk);
+    plan.chunks = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(chunks, 32)));
+    return plan;
+}
+
+static int64_t attention_workspace(const tw_attention_args &a)
+{
+    if (a.n_seqs == 0 || a.q_rows == 0) return 0;
+    const AttentionPlan plan = attention_plan(a);
+    return plan.chunks == 1 ? 0 : static_cast<int64_t>(plan.chunks) * a.q_rows * a.q_heads * (a.head_dim + 2) * 4;
+}
+
+template <int DP, int M, int WR, int WK, int KEYS, int STAGES, bool SCAN>
+static tw_status launch_attention(const AttentionParams &p, int64_t tiles, hipStream_t stream)
+{
+    using Shape = AttentionShape<DP, M, WR, WK, KEYS, STAGES>;
+    static std::atomic<int> allowed[kMaxDevices];
+    auto kernel = attention_kernel<DP, M, WR, WK, KEYS, STAGES, SCAN>;
+    TW_TRY(allow_dynamic_lds(reinterpret_cast<const void *>(kernel), Shape::kLds, allowed));
+    const int64_t grid = tiles * p.chunks * p.kv_heads;
+    if (grid > INT32_MAX) return TW_ERR_UNSUPPORTED;
+    TW_HIP(launch_kernel(kernel, dim3(static_cast<uint32_t>(grid)), dim3(Shape::kThreads), Shape::kLds, stream, p));
+    return TW_OK;
+}
+
+template <int DP>
+static tw_status launch_attention_for(const AttentionParams &p, const AttentionPlan &plan, hipStream_t stream)
+{
+    if (plan.few) return launch_attention<DP, 16, 1, 4, 32, 1, false>(p, p.n_seqs, stream);
+    return launch_attention<DP, 32, 8, 1, 64, 2, true>(p, p.q_rows * p.group / 256 + p.n_seqs, stream);
+}
+
+}  // namespace tw
+
+using namespace tw;
+
+extern "C" {
+
+int64_t tw_attention_workspace_bytes(const tw_attention_args *args)
+{
+    if (!args || attention_sizes(*args) != TW_OK) return -1;
+    return attention_workspace(*args);
+}
+
+tw_status tw_attention_plan(const tw_attention_args *args, tw_attention_launch *launch)
+{
+    if (!args || !launch) return TW_ERR_NULL;
+    TW_TRY(attention_sizes(*args));
+    *launch = {};
+    if (args->n_seqs == 0 || args->q_rows == 0) return TW_OK;
+    const AttentionPlan plan = attention_plan(*args);
+    launch->tile_rows = plan.few ? 16 : 256;
+    launch->key_waves = plan.few ? 4 : 1;
+    launch->chunks = plan.chunks;
+    launch->min_chunk = plan.min_chunk;
+    return TW_OK;
+}
+
+tw_status tw_attention(const tw_attention_args *args, void *workspace, int64_t workspace_bytes, void *stream)
+{
+    if (!args) return TW_ERR_NULL;
+    const tw_attention_args &a = *args;
+    TW_TRY(attention_sizes(a));
+    if (a.n_seqs == 0 || a.q_rows == 0) return TW_OK;
+    if (!a.q || !a.out || !a.q_offsets || !a.k_offsets || (a.k_rows > 0 && (!a.k || !a.v))) return TW_ERR_NULL;
+    if (!aligned16(a.q) || !aligned16(a.out) || !aligned16(a.k) || !aligned16(a.v)) return TW_ERR_ALIGN;
+    for (const void *p : {static_cast<const void *>(a.q_offsets), static_cast<const void *>(a.k_offsets), static_cast<const void *>(a.lse)})
+        if (reinterpret_cast<uintptr_t>(p) & 3u) return TW_ERR_ALIGN;
+    const int64_t need = attention_workspace(a);
+    if (need > 0) {
+        if (!workspace) return TW_ERR_NULL;
+        if (!aligned16(workspace)) return TW_ERR_ALIGN;
+        if (workspace_bytes < need) return TW_ERR_SHAPE;
+    }
+    const int64_t wq = static_cast<int64_t>(a.q_heads) * a.head_dim, wk = static_cast<int64_t>(a.kv_heads) * a.head_dim;
+    struct Range {
+        const void *p;
+        uint64_t bytes;
+    };
+    const Range written[] = {{a.out, span(a.q_rows, a.out_stride, wq)},
+                             {a.lse, a.lse ? static_cast<uint64_t>(a.q_rows) * a.q_heads * 4u : 0},
+                             {workspace, static_cast<uint64_t>(need)}};
+    const Range read[] = {{a.q, span(a.q_rows, a.q_stride, wq)},       {a.k, span(a.k_rows, a.k_stride, wk)},
+                          {a.v, span(a.k_rows, a.v_stride, wk)},       {a.q_offsets, static_cast<uint64_t>(a.n_seqs + 1) * 4u},
+                          {a.k_offsets, static_cast<uint64_t>(a.n_seqs + 1) * 4u}};
+    for (int i = 0; i < 3; ++i) {
+        for (const Range &r : read)
+            if (ranges_overlap(written[i].p, written[i].bytes, r.p, r.bytes)) return TW_ERR_ALIAS;
+        for (int j = 0; j < i; ++j)
+            if (ranges_overlap(written[i].p, written[i].bytes, written[j].p, written[j].bytes)) return TW_ERR_ALIAS;
+    }
+
+    const AttentionPlan plan = attention_plan(a);
+    AttentionParams p;
+    p.q = static_cast<const char *>(a.q);
+    p.k = static_cast<const char *>(a.k);
+    p.v = static_cast<const char *>(a.v);
+    p.out = static_cast<char *>(a.out);
+    p.lse = a.lse;
+    p.q_offsets = a.q_offsets;
+    p.k_offsets = a.k_offsets;
+    p.part = static_cast<float *>(workspace);
+    p.part_ml = p.part + static_cast<int64_t>(plan.chunks) * a.q_rows * a.q_heads * a.head_dim;
+    p.q_rows = a.q_rows;
+    p.k_rows = a.k_rows;
+    p.q_stride = a.q_stride * 2;
+    p.k_stride = a.k_stride * 2;
+    p.v_stride = a.v_stride * 2;
+    p.out_stride = a.out_stride * 2;
+    p.n_seqs = static_cast<int>(a.n_seqs);
+    p.q_heads = a.q_heads;
+    p.kv_heads = a.kv_heads;
+    p.group = a.q_heads / a.kv_heads;
+    p.dim = a.head_dim;
+    p.causal = a.causal != 0;
+    p.chunks = plan.chunks;
+    p.min_chunk = plan.min_chunk;
+    p.c = static_cast<float>(a.scale * 1.4426950408889634);
+    const hipStream_t s = static_cast<hipStream_t>(stream);
+    TW_TRY(a.head_dim > 64 ? launch_attention_for<128>(p, plan, s) : launch_attention_for<64>(p, plan, s));
+    if (plan.chunks > 1) {
+        const int64_t grid = (a.q_rows * a.q_heads + 3) / 4;
+        if (grid > INT32_MAX) return TW_ERR_UNSUPPORTED;
+        TW_HIP(launch_kernel(attention_join_kernel, dim3(static_cast<uint32_t>(grid)), dim3(256), 0, s, p));
+    }
+    return TW_OK;
+}
+
+}  // extern "C"

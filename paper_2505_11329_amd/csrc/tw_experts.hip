@@ -1,0 +1,460 @@
+// Tokens to their experts and back: the pairs of tokens and experts sorted by expert, rows copied to the sorted places,
+// the weighted sum of a token's rows, and its gradient.
+#include <algorithm>
+
+#include "tw_device.h"
+#include "tw_internal.h"
+
+namespace tw {
+
+// ---- sort ----
+//
+// A stable counting sort. A workgroup has a run of consecutive pairs and each of its waves a part of the run; the place of a
+// pair is the number of pairs of lower experts, plus those of its expert in earlier runs, in earlier waves of its own, and
+// earlier in its wave. Only counts meet between waves, so nothing depends on the order they run in.
+
+static constexpr int kRun = 4096;       // fewest pairs of a workgroup, where there is more than one
+static constexpr int kMaxRuns = 256;
+
+struct SortParams {
+    const void *ids;
+    int32_t *order, *position, *offsets;
+    int32_t *counts;  // [runs x (experts + 1)]
+    int64_t pairs;
+    int64_t run;      // pairs of a workgroup
+    int experts;
+};
+
+// A pair's bucket: its expert, or the last one where it has none.
+template <typename Id>
+__device__ __forceinline__ int bucket_of(const SortParams &p, int64_t pair)
+{
+    const Id id = static_cast<const Id *>(p.ids)[pair];
+    return id >= 0 && id < p.experts ? static_cast<int>(id) : p.experts;
+}
+
+template <typename Id>
+__global__ __launch_bounds__(1024) void expert_count_kernel(SortParams p)
+{
+    extern __shared__ int32_t count[];
+    for (int e = threadIdx.x; e <= p.experts; e += blockDim.x) count[e] = 0;
+    __syncthreads();
+    const int64_t begin = blockIdx.x * p.run, end = min(begin + p.run, p.pairs);
+    for (int64_t i = begin + threadIdx.x; i < end; i += blockDim.x) atomicAdd(&count[bucket_of<Id>(p, i)], 1);
+    __syncthreads();
+    for (int e = threadIdx.x; e <= p.experts; e += blockDim.x)
+        p.counts[static_cast<int64_t>(blockIdx.x) * (p.experts + 1) + e] = count[e];
+}
+
+// Lanes of the wave whose pair has the same bucket as this lane's; `bits` bits tell buckets apart.
+__device__ __forceinline__ uint64_t same_bucket(int bucket, int bits, uint64_t active)
+{
+    uint64_t same = active;
+    for (int b = 0; b < bits; ++b) {
+        const uint64_t set = __ballot((bucket >> b) & 1);
+        same &= (bucket >> b) & 1 ? set : ~set;
+    }
+    return same;
+}
+
+template <typename Id>
+__global__ __launch_bounds__(1024) void expert_place_kernel(SortParams p)
+{
+    extern __shared__ int32_t start[];  // [waves x buckets]: counts, then the next place
+    __shared__ int32_t wave_total[16];
+    const int waves = blockDim.x / 64, wave = threadIdx.x / 64, lane = threadIdx.x % 64;
+    const int buckets = p.experts + 1;
+    for (int i = threadIdx.x; i < waves * buckets; i += blockDim.x) start[i] = 0;
+    __syncthreads();
+    const int64_t run_begin = blockIdx.x * p.run, run_end = min(run_begin + p.run, p.pairs);
+    const int64_t part = (p.run / 64 + waves - 1) / waves * 64;
+    const int64_t begin = min(run_begin + wave * part, run_end), end = min(begin + part, run_end);
+    int32_t *const mine = start + wave * buckets;
+    for (int64_t i = begin + lane; i < end; i += 64) atomicAdd(&mine[bucket_of<Id>(p, i)], 1);
+    __syncthreads();
+
+    // each thread has a few neighbouring buckets: their totals, and the pairs of earlier runs
+    const int each = (buckets + blockDim.x - 1) / blockDim.x, first = threadIdx.x * each;
+    int32_t total = 0;
+    for (int e = first; e < min(first + each, buckets); ++e) {
+        if (gridDim.x == 1)
+            for (int w = 0; w < waves; ++w) total += start[w * buckets + e];
+        else
+            for (unsigned r = 0; r < gridDim.x; ++r) total += p.counts[static_cast<int64_t>(r) * buckets + e];
+    }
+    int32_t upto = total;
+    for (int d = 1; d < 64; d <<= 1) {
+        const int32_t o = __shfl_up(upto, d);
+        if (lane >= d) upto += o;
+    }
+    if (lane == 63) wave_total[wave] = upto;
+    __syncthreads();
+    int32_t base = upto - total;
+    for (int w = 0; w < wave; ++w) base += wave_total[w];
+    for (int e = first; e < min(first + each, buckets); ++e) {
+        if (blockIdx.x == 0) p.offsets[e] = base;
+        int32_t at = base;
+        if (gridDim.x > 1)
+            for (unsigned r = 0; r < gridDim.x; ++r) {
+                const int32_t n = p.counts[static_cast<int64_t>(r) * buckets + e];
+                if (r < blockIdx.x) at += n;
+                base += n;
+            }
+        for (int w = 0; w < waves; ++w) {
+            const int32_t n = start[w * buckets + e];
+            start[w * buckets + e] = at;
+            at += n;
+            if (gridDim.x == 1) base += n;
+        }
+    }
+    __syncthreads();
+
+    const int bits = 32 - __builtin_clz(p.experts);
+    for (int64_t i0 = begin; i0 < end; i0 += 64) {
+        const int64_t i = i0 + lane;
+        const bool has = i < end;
+        const int bucket = has ? bucket_of<Id>(p, i) : 0;
+        const uint64_t same = same_bucket(bucket, bits, __ballot(has));
+        if (has) {
+            const int ahead = __builtin_popcountll(same & ((uint64_t(1) << lane) - 1));
+            const int32_t place = mine[bucket] + ahead;
+            // all lanes of the wave have read before one adds, and it has before the next round reads
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            if (ahead == 0) mine[bucket] = place + __builtin_popcountll(same);
+            p.order[place] = static_cast<int32_t>(i);
+            p.position[i] = bucket == p.experts ? -1 : place;
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    }
+}
+
+// ---- rows ----
+//
+// All of these are bound by memory: 16 bytes of a row to a thread, 2^row_log2 threads to a row of up to 2048 elements and
+// 256 to a longer one.
+
+struct RowsParams {
+    const char *in;       // x | y | dout
+    const char *y;        // backward
+    char *out;            // dispatched rows | sums | dy
+    const int32_t *position;
+    const float *weights;
+    float *dweights;
+    int64_t tokens, rows;
+    int top_k, pieces;    // 16-byte pieces of a row
+    int row_log2;
+};
+
+static constexpr int kMost = 8;  // pairs of a token that are worked on at a time
+
+__device__ __forceinline__ u32x4 row_piece(const char *base, int64_t row, int pieces, int c)
+{
+    return *reinterpret_cast<const u32x4 *>(base + (row * pieces + c) * 16);
+}
+
+// The places of pairs [k0, k0 + kMost) of a token, -1 for none.
+__device__ __forceinline__ void places(const RowsParams &p, int64_t token, int k0, int32_t (&at)[kMost])
+{
+#pragma unroll
+    for (int k = 0; k < kMost; ++k) {
+        at[k] = -1;
+        if (k0 + k < p.top_k) {
+            const int32_t s = p.position[token * p.top_k + k0 + k];
+            if (s >= 0 && s < p.rows) at[k] = s;
+        }
+    }
+}
+
+__global__ __launch_bounds__(256) void expert_dispatch_kernel(RowsParams p)
+{
+    const int threads = 1 << p.row_log2;
+    const int64_t token = static_cast<int64_t>(blockIdx.x) * (256 >> p.row_log2) + (threadIdx.x >> p.row_log2);
+    if (token >= p.tokens) return;
+    for (int k0 = 0; k0 < p.top_k; k0 += kMost) {
+        int32_t at[kMost];
+        places(p, token, k0, at);
+        for (int c = threadIdx.x & (threads - 1); c < p.pieces; c += threads) {
+            const u32x4 x = row_piece(p.in, token, p.pieces, c);
+#pragma unroll
+            for (int k = 0; k < kMost; ++k)
+                if (at[k] >= 0) *reinterpret_cast<u32x4 *>(p.out + (static_cast<int64_t>(at[k]) * p.pieces + c) * 16) = x;
+        }
+    }
+}
+
+template <bool WEIGHTED>
+__global__ __launch_bounds__(256) void expert_combine_kernel(RowsParams p)
+{
+    const int threads = 1 << p.row_log2;
+    const int64_t token = static_cast<int64_t>(blockIdx.x) * (256 >> p.row_log2) + (threadIdx.x >> p.row_log2);
+    if (token >= p.tokens) return;
+    for (int c = threadIdx.x & (threads - 1); c < p.pieces; c += threads) {
+        float sum[8] = {};
+        for (int k0 = 0; k0 < p.top_k; k0 += kMost) {
+            int32_t at[kMost];
+            places(p, token, k0, at);
+            u32x4 v[kMost] = {};
+#pragma unroll
+            for (int k = 0; k < kMost; ++k)
+                if (at[k] >= 0) v[k] = row_piece(p.in, at[k], p.pieces, c);
+#pragma unroll
+            for (int k = 0; k < kMost; ++k) {
+                if (at[k] < 0) continue;
+                if constexpr (WEIGHTED) {
+                    const float w = p.weights[token * p.top_k + k0 + k];
+                    float f[8];
+                    unpack8(v[k], f);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) sum[i] = fmaf(w, f[i], sum[i]);
+                } else {
+                    add8(v[k], sum);
+                }
+            }
+        }
+        *reinterpret_cast<u32x4 *>(p.out + (token * p.pieces + c) * 16) = pack8(sum);
+    }
+}
+
+__global__ __launch_bounds__(256) void expert_combine_backward_kernel(RowsParams p)
+{
+    __shared__ float wave_dot[4][kMost];
+    const int threads = 1 << p.row_log2, in_row = threadIdx.x & (threads - 1);
+    const int64_t token = static_cast<int64_t>(blockIdx.x) * (256 >> p.row_log2) + (threadIdx.x >> p.row_log2);
+    const bool has = token < p.tokens;
+    for (int k0 = 0; k0 < p.top_k; k0 += kMost) {
+        int32_t at[kMost];
+        float w[kMost], dot[kMost] = {};
+#pragma unroll
+        for (int k = 0; k < kMost; ++k) at[k] = -1;
+        if (has) places(p, token, k0, at);
+#pragma unroll
+        for (int k = 0; k < kMost; ++k) w[k] = at[k] >= 0 ? p.weights[token * p.top_k + k0 + k] : 0.0f;
+        if (has)
+            for (int c = in_row; c < p.pieces; c += threads) {
+                float d[8];
+                unpack8(row_piece(p.in, token, p.pieces, c), d);
+                u32x4 v[kMost] = {};
+#pragma unroll
+                for (int k = 0; k < kMost; ++k)
+                    if (at[k] >= 0) v[k] = row_piece(p.y, at[k], p.pieces, c);
+#pragma unroll
+                for (int k = 0; k < kMost; ++k) {
+                    if (at[k] < 0) continue;
+                    float f[8];
+                    unpack8(v[k], f);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        dot[k] = fmaf(f[i], d[i], dot[k]);
+                        f[i] = w[k] * d[i];
+                    }
+                    *reinterpret_cast<u32x4 *>(p.out + (static_cast<int64_t>(at[k]) * p.pieces + c) * 16) = pack8(f);
+                }
+            }
+        // a row's dot products: over its lanes, then over its waves in order
+#pragma unroll
+        for (int k = 0; k < kMost; ++k) dot[k] = group_sum(dot[k], min(p.row_log2, 6));
+        if (p.row_log2 > 6) {
+            if ((threadIdx.x & 63) == 0)
+#pragma unroll
+                for (int k = 0; k < kMost; ++k) wave_dot[threadIdx.x >> 6][k] = dot[k];
+            __syncthreads();
+            const int first = (threadIdx.x >> p.row_log2) << (p.row_log2 - 6);
+#pragma unroll
+            for (int k = 0; k < kMost; ++k) {
+                dot[k] = wave_dot[first][k];
+                for (int w2 = 1; w2 < threads / 64; ++w2) dot[k] += wave_dot[first + w2][k];
+            }
+            __syncthreads();
+        }
+        if (has)
+#pragma unroll
+            for (int k = 0; k < kMost; ++k)
+                if (in_row == k && k0 + k < p.top_k) p.dweights[token * p.top_k + k0 + k] = dot[k];
+    }
+}
+
+// ---- host ----
+
+static tw_status pair_sizes(int64_t N, int top_k)
+{
+    if (N < 0 || top_k < 1) return TW_ERR_SHAPE;
+    if (top_k > TW_MAX_TOP_K || N > INT32_MAX / top_k) return TW_ERR_UNSUPPORTED;
+    return TW_OK;
+}
+
+static tw_status sort_sizes(int64_t N, int top_k, int n_experts)
+{
+    TW_TRY(pair_sizes(N, top_k));
+    if (n_experts < 1) return TW_ERR_SHAPE;
+    return n_experts > TW_MAX_EXPERTS ? TW_ERR_UNSUPPORTED : TW_OK;
+}
+
+static int64_t sort_runs(int64_t pairs) { return std::max<int64_t>(1, std::min<int64_t>(kMaxRuns, pairs / kRun)); }
+
+static tw_status row_sizes(int64_t N, int top_k, int64_t H, int64_t rows)
+{
+    TW_TRY(pair_sizes(N, top_k));
+    if (H < 1 || rows < 0) return TW_ERR_SHAPE;
+    if (H % 8 != 0 || H > TW_MAX_H || rows > INT32_MAX) return TW_ERR_UNSUPPORTED;
+    return TW_OK;
+}
+
+static bool aligned4(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
+
+static void row_layout(int64_t H, RowsParams *p)
+{
+    p->pieces = static_cast<int>(H / 8);
+    p->row_log2 = 0;
+    while (p->row_log2 < 8 && (1 << p->row_log2) < p->pieces) ++p->row_log2;
+    p->row_log2 = std::max(p->row_log2, 3);  // eight threads at least: one to each pair's gradient
+}
+
+static tw_status launch_rows(void (*kernel)(RowsParams), const RowsParams &p, void *stream)
+{
+    const int64_t per_group = 256 >> p.row_log2;
+    TW_HIP(launch_kernel(kernel, dim3(static_cast<uint32_t>((p.tokens + per_group - 1) / per_group)), dim3(256), 0,
+                         static_cast<hipStream_t>(stream), p));
+    return TW_OK;
+}
+
+template <typename Id>
+static tw_status launch_sort(const SortParams &p, int64_t runs, hipStream_t stream)
+{
+    const unsigned buckets = static_cast<unsigned>(p.experts + 1);
+    const unsigned threads = p.experts <= 512 ? 1024 : 512;  // (more waves' counts than these do not fit 64 KiB)
+    if (runs > 1)
+        TW_HIP(launch_kernel(expert_count_kernel<Id>, dim3(static_cast<uint32_t>(runs)), dim3(1024), buckets * 4, stream, p));
+    TW_HIP(launch_kernel(expert_place_kernel<Id>, dim3(static_cast<uint32_t>(runs)), dim3(threads), threads / 64 * buckets * 4, stream, p));
+    return TW_OK;
+}
+
+}  // namespace tw
+
+using namespace tw;
+
+extern "C" {
+
+int64_t tw_expert_sort_workspace_bytes(int64_t N, int top_k, int n_experts)
+{
+    if (sort_sizes(N, top_k, n_experts) != TW_OK) return -1;
+    const int64_t runs = sort_runs(N * top_k);
+    return runs == 1 ? 0 : runs * (n_experts + 1) * 4;
+}
+
+tw_status tw_expert_sort(const void *expert_ids, int id_bytes, int64_t N, int top_k, int n_experts, int32_t *order,
+                         int32_t *position, int32_t *offsets, void *workspace, int64_t workspace_bytes, void *stream)
+{
+    TW_TRY(sort_sizes(N, top_k, n_experts));
+    if (id_bytes != 4 && id_bytes != 8) return TW_ERR_UNSUPPORTED;
+    const int64_t pairs = N * top_k, need = tw_expert_sort_workspace_bytes(N, top_k, n_experts);
+    if (!offsets || (pairs > 0 && (!expert_ids || !order || !position)) || (need > 0 && !workspace)) return TW_ERR_NULL;
+    if (!aligned4(offsets) || !aligned4(order) || !aligned4(position) || (need > 0 && !aligned4(workspace)) ||
+        (reinterpret_cast<uintptr_t>(expert_ids) & (id_bytes - 1)))
+        return TW_ERR_ALIGN;
+    if (workspace_bytes < need) return TW_ERR_SHAPE;
+    const uint64_t list = static_cast<uint64_t>(pairs) * 4u;
+    const struct {
+        const void *p;
+        uint64_t bytes;
+    } all[] = {{expert_ids, static_cast<uint64_t>(pairs) * id_bytes},
+               {order, list},
+               {position, list},
+               {offsets, (n_experts + 1) * 4u},
+               {workspace, static_cast<uint64_t>(need)}};
+    for (int i = 1; i < 5; ++i)
+        for (int j = 0; j < i; ++j)
+            if (ranges_overlap(all[i].p, all[i].bytes, all[j].p, all[j].bytes)) return TW_ERR_ALIAS;
+    SortParams p;
+    p.ids = expert_ids;
+    p.order = order;
+    p.position = position;
+    p.offsets = offsets;
+    p.counts = static_cast<int32_t *>(workspace);
+    p.pairs = pairs;
+    p.experts = n_experts;
+    const int64_t runs = sort_runs(pairs);
+    p.run = ((pairs + runs - 1) / runs + 63) / 64 * 64;
+    const hipStream_t s = static_cast<hipStream_t>(stream);
+    return id_bytes == 4 ? launch_sort<int32_t>(p, runs, s) : launch_sort<int64_t>(p, runs, s);
+}
+
+tw_status tw_expert_dispatch(const void *x, const int32_t *position, int64_t N, int top_k, int64_t H, void *out,
+                             int64_t rows, void *stream)
+{
+    TW_TRY(row_sizes(N, top_k, H, rows));
+    if (N == 0 || rows == 0) return TW_OK;
+    if (!x || !position || !out) return TW_ERR_NULL;
+    if (!aligned16(x) || !aligned16(out) || !aligned4(position)) return TW_ERR_ALIGN;
+    const uint64_t tokens_b = static_cast<uint64_t>(N) * H * 2u, rows_b = static_cast<uint64_t>(rows) * H * 2u;
+    const uint64_t pairs_b = static_cast<uint64_t>(N) * top_k * 4u;
+    if (ranges_overlap(out, rows_b, x, tokens_b) || ranges_overlap(out, rows_b, position, pairs_b)) return TW_ERR_ALIAS;
+    RowsParams p = {};
+    p.in = static_cast<const char *>(x);
+    p.out = static_cast<char *>(out);
+    p.position = position;
+    p.tokens = N;
+    p.rows = rows;
+    p.top_k = top_k;
+    row_layout(H, &p);
+    return launch_rows(expert_dispatch_kernel, p, stream);
+}
+
+tw_status tw_expert_combine(const void *y, int64_t rows, const int32_t *position, const float *weights, int64_t N,
+                            int top_k, int64_t H, void *out, void *stream)
+{
+    TW_TRY(row_sizes(N, top_k, H, rows));
+    if (N == 0) return TW_OK;
+    if ((rows > 0 && !y) || !position || !out) return TW_ERR_NULL;
+    if (!aligned16(y) || !aligned16(out) || !aligned4(position) || !aligned4(weights)) return TW_ERR_ALIGN;
+    const uint64_t tokens_b = static_cast<uint64_t>(N) * H * 2u, rows_b = static_cast<uint64_t>(rows) * H * 2u;
+    const uint64_t pairs_b = static_cast<uint64_t>(N) * top_k * 4u;
+    if (ranges_overlap(out, tokens_b, y, rows_b) || ranges_overlap(out, tokens_b, position, pairs_b) ||
+        (weights && ranges_overlap(out, tokens_b, weights, pairs_b)))
+        return TW_ERR_ALIAS;
+    RowsParams p = {};
+    p.in = static_cast<const char *>(y);
+    p.out = static_cast<char *>(out);
+    p.position = position;
+    p.weights = weights;
+    p.tokens = N;
+    p.rows = rows;
+    p.top_k = top_k;
+    row_layout(H, &p);
+    return launch_rows(weights ? expert_combine_kernel<true> : expert_combine_kernel<false>, p, stream);
+}
+
+tw_status tw_expert_combine_backward(const void *dout, const void *y, int64_t rows, const int32_t *position,
+                                     const float *weights, int64_t N, int top_k, int64_t H, void *dy, float *dweights,
+                                     void *stream)
+{
+    TW_TRY(row_sizes(N, top_k, H, rows));
+    if (N == 0) return TW_OK;
+    if (!dout || (rows > 0 && (!y || !dy)) || !position || !weights || !dweights) return TW_ERR_NULL;
+    if (!aligned16(dout) || !aligned16(y) || !aligned16(dy) || !aligned4(position) || !aligned4(weights) || !aligned4(dweights))
+        return TW_ERR_ALIGN;
+    const uint64_t tokens_b = static_cast<uint64_t>(N) * H * 2u, rows_b = static_cast<uint64_t>(rows) * H * 2u;
+    const uint64_t pairs_b = static_cast<uint64_t>(N) * top_k * 4u;
+    const struct {
+        const void *p;
+        uint64_t bytes;
+    } read[] = {{dout, tokens_b}, {position, pairs_b}, {weights, pairs_b}};
+    for (const auto &r : read)
+        if (ranges_overlap(dy, rows_b, r.p, r.bytes) || ranges_overlap(dweights, pairs_b, r.p, r.bytes)) return TW_ERR_ALIAS;
+    if (ranges_overlap(dweights, pairs_b, y, rows_b) || ranges_overlap(dweights, pairs_b, dy, rows_b) ||
+        (dy != y && ranges_overlap(dy, rows_b, y, rows_b)))
+        return TW_ERR_ALIAS;
+    RowsParams p = {};
+    p.in = static_cast<const char *>(dout);
+    p.y = static_cast<const char *>(y);
+    p.out = static_cast<char *>(dy);
+    p.position = position;
+    p.weights = weights;
+    p.dweights = dweights;
+    p.tokens = N;
+    p.rows = rows;
+    p.top_k = top_k;
+    row_layout(H, &p);
+    return launch_rows(expert_combine_backward_kernel, p, stream);
+}
+
+}  // extern "C"

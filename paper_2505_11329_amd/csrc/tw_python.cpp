@@ -13,9 +13,11 @@
 #include <Python.h>
 
 #include <ATen/ATen.h>
+#include <c10/hip/HIPFunctions.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <cmath>
 #include <new>
 #include <vector>
 
@@ -558,6 +560,262 @@ PyObject *py_weave_train(PyObject *, PyObject *const *v, Py_ssize_t n)
     });
 }
 
+// ---- attention and experts ----
+
+// These also refuse tensors of another device than the current one, where the kernels would run.
+const at::Tensor &here(const at::Tensor &t, const Name &n)
+{
+    if (t.get_device() != c10::hip::current_device()) bad_tensor(PyExc_ValueError, "%U must be on the current device", n);
+    return t;
+}
+
+const at::Tensor &typed(PyObject *o, const Name &n, at::ScalarType type, const char *type_name)
+{
+    const at::Tensor &t = here(gpu_tensor(o, n), n);
+    if (t.scalar_type() != type) {
+        Ref dt = attr_str(o, "dtype"), want(PyUnicode_FromString(type_name));
+        bad_tensor(PyExc_TypeError, "%U must be %U, got %S", n, want.o, dt.o);
+    }
+    return t;
+}
+
+void check_shape(PyObject *o, const at::Tensor &t, const Name &n, at::IntArrayRef want)
+{
+    if (t.sizes() == want) return;
+    Ref sh = attr_str(o, "shape"), got(PySequence_Tuple(sh.o)), expected(PyTuple_New(static_cast<Py_ssize_t>(want.size())));
+    if (!got.o || !expected.o) fail();
+    for (size_t i = 0; i < want.size(); ++i) PyTuple_SET_ITEM(expected.o, i, PyLong_FromLongLong(want[i]));
+    bad_tensor(PyExc_ValueError, "%U has shape %S, expected %S", n, got.o, expected.o);
+}
+
+// Device pointer of a contiguous tensor of this type and shape.
+void *array_ptr(PyObject *o, const Name &n, at::ScalarType type, const char *type_name, at::IntArrayRef shape)
+{
+    const at::Tensor &t = typed(o, n, type, type_name);
+    if (!t.is_contiguous()) bad_tensor(PyExc_ValueError, "%U must be contiguous", n);
+    check_shape(o, t, n, shape);
+    return t.data_ptr();
+}
+void *bf16_array(PyObject *o, const Name &n, at::IntArrayRef shape) { return array_ptr(o, n, at::kBFloat16, "bfloat16", shape); }
+int32_t *int32_array(PyObject *o, const Name &n, at::IntArrayRef shape)
+{
+    return static_cast<int32_t *>(array_ptr(o, n, at::kInt, "int32", shape));
+}
+float *float_array(PyObject *o, const Name &n, at::IntArrayRef shape)
+{
+    return static_cast<float *>(array_ptr(o, n, at::kFloat, "float32", shape));
+}
+
+// The given tensor, or a new contiguous one.
+Ref given_or_empty(PyObject *o, const at::Tensor &like, at::IntArrayRef shape, at::ScalarType type)
+{
+    if (o != Py_None) {
+        Py_INCREF(o);
+        return Ref(o);
+    }
+    Ref t(THPVariable_Wrap(at::empty(shape, at::TensorOptions().device(like.device()).dtype(type))));
+    if (!t.o) fail();
+    return t;
+}
+
+// A tensor whose sizes others are checked against.
+const at::Tensor &sized(PyObject *o, const Name &n, int64_t dims, const char *message)
+{
+    const at::Tensor &t = gpu_tensor(o, n);
+    if (t.dim() != dims) fail(PyExc_ValueError, "%s", message);
+    return t;
+}
+
+// Rows of heads: [rows, heads, dim], the heads of a row next to each other. Returns the row stride.
+int64_t heads_stride(const at::Tensor &t, const Name &n)
+{
+    const int64_t heads = t.size(1), dim = t.size(2);
+    if (t.numel() && ((dim > 1 && t.stride(2) != 1) || (heads > 1 && t.stride(1) != dim)))
+        bad_tensor(PyExc_ValueError, "%U must have each row's heads next to each other", n);
+    return t.size(0) > 1 ? t.stride(0) : heads * dim;
+}
+
+// Workspace of a call: the caller's, or one from torch's allocator that belongs to the call's stream, so that it can go
+// back to the allocator when the call has been made.
+struct Workspace {
+    at::Tensor made;
+    void *p = nullptr;
+    int64_t bytes = 0;
+    void fill(PyObject *o, int64_t need, const at::Tensor &like, void *stream)
+    {
+        if (o != Py_None) {
+            const at::Tensor &t = here(gpu_tensor(o, {"workspace"}), {"workspace"});
+            if (!t.is_contiguous()) bad_tensor(PyExc_ValueError, "%U must be contiguous", {"workspace"});
+            p = t.data_ptr();
+            bytes = static_cast<int64_t>(t.nbytes());
+        } else if (need > 0) {
+            struct Restore {
+                c10::hip::HIPStream was = c10::hip::getCurrentHIPStream();
+                ~Restore() { c10::hip::setCurrentHIPStream(was); }
+            } restore;
+            if (restore.was.stream() != stream)
+                c10::hip::setCurrentHIPStream(
+                    c10::hip::getStreamFromExternal(static_cast<hipStream_t>(stream), c10::hip::current_device()));
+            made = at::empty({need}, at::TensorOptions().device(like.device()).dtype(at::kByte));
+            p = made.data_ptr();
+            bytes = need;
+        }
+    }
+};
+
+struct Attention {
+    tw_attention_args a;
+    Ref out, lse;
+    void fill(PyObject *Q, PyObject *K, PyObject *V, PyObject *q_offsets, PyObject *k_offsets, PyObject *causal, PyObject *scale,
+              PyObject *o, PyObject *e)
+    {
+        const at::Tensor &q = sized(Q, {"q"}, 3, "q must be [rows, q_heads, head_dim]");
+        const at::Tensor &k = sized(K, {"k"}, 3, "k must be [rows, kv_heads, head_dim]");
+        const int64_t rows = q.size(0), heads = q.size(1), dim = q.size(2);
+        typed(Q, {"q"}, at::kBFloat16, "bfloat16");
+        typed(K, {"k"}, at::kBFloat16, "bfloat16");
+        const at::Tensor &v = typed(V, {"v"}, at::kBFloat16, "bfloat16");
+        check_shape(K, k, {"k"}, {k.size(0), k.size(1), dim});
+        check_shape(V, v, {"v"}, k.sizes());
+        const at::Tensor &at_q = sized(q_offsets, {"q_offsets"}, 1, "q_offsets must be [n_seqs + 1]");
+        const int64_t count = at_q.size(0);
+        if (count < 1) fail(PyExc_ValueError, "q_offsets must be [n_seqs + 1]");
+        if (heads > INT32_MAX || k.size(1) > INT32_MAX || dim > INT32_MAX) fail(PyExc_ValueError, "too many heads");
+        out = given_or_empty(o, q, {rows, heads, dim}, at::kBFloat16);
+        lse = given_or_empty(e, q, {rows, heads}, at::kFloat);
+        const at::Tensor &to = typed(out.o, {"out"}, at::kBFloat16, "bfloat16");
+        check_shape(out.o, to, {"out"}, {rows, heads, dim});
+        a.q = q.data_ptr();
+        a.k = k.data_ptr();
+        a.v = v.data_ptr();
+        a.out = to.data_ptr();
+        a.lse = float_array(lse.o, {"lse"}, {rows, heads});
+        a.q_offsets = int32_array(q_offsets, {"q_offsets"}, {count});
+        a.k_offsets = int32_array(k_offsets, {"k_offsets"}, {count});
+        a.n_seqs = count - 1;
+        a.q_rows = rows;
+        a.k_rows = k.size(0);
+        a.q_stride = heads_stride(q, {"q"});
+        a.k_stride = heads_stride(k, {"k"});
+        a.v_stride = heads_stride(v, {"v"});
+        a.out_stride = heads_stride(to, {"out"});
+        a.q_heads = static_cast<int>(heads);
+        a.kv_heads = static_cast<int>(k.size(1));
+        a.head_dim = static_cast<int>(dim);
+        a.scale = scale == Py_None ? 1.0f / std::sqrt(static_cast<float>(dim)) : as_float(scale);
+        a.causal = as_bool(causal);
+    }
+};
+
+// q, k, v, q_offsets, k_offsets, causal, scale, out, lse, workspace, stream
+PyObject *py_attention(PyObject *, PyObject *const *v, Py_ssize_t n)
+{
+    return entry("attention", n, 11, [&] {
+        Attention t;
+        t.fill(v[0], v[1], v[2], v[3], v[4], v[5], v[6], v[7], v[8]);
+        void *s = stream_handle(v[10]);
+        Workspace w;
+        w.fill(v[9], tw_attention_workspace_bytes(&t.a), THPVariable_Unpack(v[0]), s);
+        call("tw_attention", [&] { return tw_attention(&t.a, w.p, w.bytes, s); });
+        return pair(t.out, t.lse);
+    });
+}
+
+// expert_ids, n_experts, order, position, offsets, workspace, stream
+PyObject *py_expert_sort(PyObject *, PyObject *const *v, Py_ssize_t n)
+{
+    return entry("expert_sort", n, 7, [&] {
+        const at::Tensor &ids = here(sized(v[0], {"expert_ids"}, 2, "expert_ids must be [N, top_k]"), {"expert_ids"});
+        if (ids.scalar_type() != at::kInt && ids.scalar_type() != at::kLong) {
+            Ref dt = attr_str(v[0], "dtype");
+            bad_tensor(PyExc_TypeError, "%U must be int32 or int64, got %S", {"expert_ids"}, dt.o);
+        }
+        if (!ids.is_contiguous()) bad_tensor(PyExc_ValueError, "%U must be contiguous", {"expert_ids"});
+        const int64_t N = ids.size(0), top_k = ids.size(1), experts = as_int(v[1]);
+        if (top_k > INT32_MAX || experts < 0 || experts >= INT32_MAX) fail(PyExc_ValueError, "too many experts");
+        Ref order = given_or_empty(v[2], ids, {N * top_k}, at::kInt), position = given_or_empty(v[3], ids, {N, top_k}, at::kInt),
+            offsets = given_or_empty(v[4], ids, {experts + 1}, at::kInt);
+        int32_t *const o = int32_array(order.o, {"order"}, {N * top_k}), *const p = int32_array(position.o, {"position"}, {N, top_k}),
+                *const f = int32_array(offsets.o, {"offsets"}, {experts + 1});
+        void *s = stream_handle(v[6]);
+        Workspace w;
+        w.fill(v[5], tw_expert_sort_workspace_bytes(N, static_cast<int>(top_k), static_cast<int>(experts)), ids, s);
+        call("tw_expert_sort", [&] {
+            return tw_expert_sort(ids.data_ptr(), ids.scalar_type() == at::kInt ? 4 : 8, N, static_cast<int>(top_k),
+                                  static_cast<int>(experts), o, p, f, w.p, w.bytes, s);
+        });
+        return PyTuple_Pack(3, order.o, position.o, offsets.o);
+    });
+}
+
+struct Pairs {
+    int64_t N, H;
+    int top_k;
+    const int32_t *position;
+    void fill(PyObject *at, int64_t tokens, int64_t width)
+    {
+        const at::Tensor &t = sized(at, {"position"}, 2, "position must be [N, top_k]");
+        if (t.size(1) > INT32_MAX) fail(PyExc_ValueError, "position must be [N, top_k]");
+        N = tokens < 0 ? t.size(0) : tokens;
+        H = width;
+        top_k = static_cast<int>(t.size(1));
+        position = int32_array(at, {"position"}, {N, t.size(1)});
+    }
+};
+
+// x, position, out, stream
+PyObject *py_expert_dispatch(PyObject *, PyObject *const *v, Py_ssize_t n)
+{
+    return entry("expert_dispatch", n, 4, [&] {
+        const at::Tensor &x = sized(v[0], {"x"}, 2, "x must be [N, H]");
+        Pairs p;
+        p.fill(v[1], x.size(0), x.size(1));
+        Ref out = given_or_empty(v[2], x, {p.N * p.top_k, p.H}, at::kBFloat16);
+        const int64_t rows = sized(out.o, {"out"}, 2, "out must be [rows, H]").size(0);
+        const void *from = bf16_array(v[0], {"x"}, {p.N, p.H});
+        void *to = bf16_array(out.o, {"out"}, {rows, p.H}), *s = stream_handle(v[3]);
+        call("tw_expert_dispatch", [&] { return tw_expert_dispatch(from, p.position, p.N, p.top_k, p.H, to, rows, s); });
+        return out.release();
+    });
+}
+
+// y, position, weights, out, stream
+PyObject *py_expert_combine(PyObject *, PyObject *const *v, Py_ssize_t n)
+{
+    return entry("expert_combine", n, 5, [&] {
+        const at::Tensor &y = sized(v[0], {"y"}, 2, "y must be [rows, H]");
+        const int64_t rows = y.size(0);
+        Pairs p;
+        p.fill(v[1], -1, y.size(1));
+        Ref out = given_or_empty(v[3], y, {p.N, p.H}, at::kBFloat16);
+        const void *from = bf16_array(v[0], {"y"}, {rows, p.H});
+        const float *w = v[2] == Py_None ? nullptr : float_array(v[2], {"weights"}, {p.N, p.top_k});
+        void *to = bf16_array(out.o, {"out"}, {p.N, p.H}), *s = stream_handle(v[4]);
+        call("tw_expert_combine", [&] { return tw_expert_combine(from, rows, p.position, w, p.N, p.top_k, p.H, to, s); });
+        return out.release();
+    });
+}
+
+// dout, y, position, weights, dy, dweights, stream
+PyObject *py_expert_combine_backward(PyObject *, PyObject *const *v, Py_ssize_t n)
+{
+    return entry("expert_combine_backward", n, 7, [&] {
+        const at::Tensor &y = sized(v[1], {"y"}, 2, "y must be [rows, H]");
+        const int64_t rows = y.size(0);
+        Pairs p;
+        p.fill(v[2], -1, y.size(1));
+        Ref dy = given_or_empty(v[4], y, {rows, p.H}, at::kBFloat16), dw = given_or_empty(v[5], y, {p.N, p.top_k}, at::kFloat);
+        const void *d = bf16_array(v[0], {"dout"}, {p.N, p.H}), *from = bf16_array(v[1], {"y"}, {rows, p.H});
+        const float *w = float_array(v[3], {"weights"}, {p.N, p.top_k});
+        void *to = bf16_array(dy.o, {"dy"}, {rows, p.H}), *s = stream_handle(v[6]);
+        float *to_w = float_array(dw.o, {"dweights"}, {p.N, p.top_k});
+        call("tw_expert_combine_backward", [&] {
+            return tw_expert_combine_backward(d, from, rows, p.position, w, p.N, p.top_k, p.H, to, to_w, s);
+        });
+        return pair(dy, dw);
+    });
+}
+
 // ---- for the entry points that binding.py calls through ctypes ----
 
 struct Buffer {
@@ -635,7 +893,9 @@ PyMethodDef g_methods[] = {TW_METHOD(reduce_add_rmsnorm), TW_METHOD(split_launch
                            TW_METHOD(overlap_launch),     TW_METHOD(weave_layer),      TW_METHOD(weave_layer_cuts),
                            TW_METHOD(weave_layer_auto),   TW_METHOD(weave_train),      TW_METHOD(fill_fused),
                            TW_METHOD(fill_layer),         TW_METHOD(bf16_ptr),         TW_METHOD(stream_handle),
-                           TW_METHOD(set_error),          {nullptr, nullptr, 0, nullptr}};
+                           TW_METHOD(set_error),          TW_METHOD(attention),        TW_METHOD(expert_sort),
+                           TW_METHOD(expert_dispatch),    TW_METHOD(expert_combine),   TW_METHOD(expert_combine_backward),
+                           {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_twpy", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -1,0 +1,204 @@
+"""tw_attention against the plain 64-bit form: lengths, heads, head sizes, masks, strides, and what it leaves alone."""
+import math
+
+import pytest
+import torch
+
+import operator_reference as R
+
+pytestmark = pytest.mark.gpu
+
+
+def inputs(q_lens, k_lens, heads, kv_heads, dim, seed=0, tail=0, spread=1.0):
+    """bf16 normals on the GPU; `tail` rows more than the sequences have, before and behind them."""
+    g = torch.Generator().manual_seed(seed)
+    T, Tk = sum(q_lens) + 2 * tail, sum(k_lens) + 2 * tail
+
+    def normal(*shape):
+        return (torch.randn(*shape, generator=g) * spread).bfloat16().cuda()
+
+    return (normal(T, heads, dim), normal(Tk, kv_heads, dim), normal(Tk, kv_heads, dim), R.offsets(q_lens, tail).cuda(),
+            R.offsets(k_lens, tail).cuda())
+
+
+def check(tw, q, k, v, qo, ko, causal=True, scale=None, what="", **more):
+    out, lse = tw.attention(q, k, v, qo, ko, causal=causal, scale=scale, **more)
+    torch.cuda.synchronize()
+    c = 1.0 / math.sqrt(q.shape[2]) if scale is None else scale
+    want, want_lse, tol, tol_lse = R.attention(q, k, v, qo, ko, causal, c)
+    a, b = int(qo[0]), int(qo[-1])
+    R.assert_close(out[a:b], want[a:b], tol[a:b], what + " out")
+    R.assert_close(lse[a:b], want_lse[a:b], tol_lse[a:b], what + " lse")
+    return out, lse
+
+
+LENGTHS = [
+    ([1], [1]), ([1], [0]), ([2], [1]), ([63], [63]), ([65], [64]), ([5, 0, 1, 130], [5, 7, 33, 130]),
+    ([1, 1, 1, 1, 1], [1, 31, 32, 129, 700]), ([257], [257]), ([40, 300], [900, 301]), ([7, 9], [3, 0]), ([0, 0, 3], [4, 0, 3]),
+]
+HEADS = [(1, 1, 64), (4, 2, 128), (8, 1, 128), (6, 2, 72), (3, 3, 8), (32, 1, 64), (5, 1, 96)]
+
+
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("heads,kv_heads,dim", HEADS)
+def test_lengths_and_heads(tw, heads, kv_heads, dim, causal):
+    for n, (q_lens, k_lens) in enumerate(LENGTHS):
+        print(heads, kv_heads, dim, causal, q_lens, k_lens, flush=True)
+        args = inputs(q_lens, k_lens, heads, kv_heads, dim, seed=n)
+        check(tw, *args, causal=causal, what="%s %s" % (q_lens, k_lens))
+
+
+@pytest.mark.parametrize("q_lens,k_lens,heads,kv_heads,dim", [
+    ([1, 1, 1], [5000, 3, 1300], 8, 1, 128),        # few rows, long keys: the keys are cut into chunks
+    ([1], [20011], 4, 4, 64),
+    ([100], [4100], 16, 2, 128),                    # a chunk of a prompt, cut too
+    ([2, 3, 1, 4], [600, 2049, 1, 1024], 8, 2, 80),
+    ([1000, 40], [1000, 2040], 8, 2, 128),          # a prompt and a chunk
+    ([300] * 4, [300] * 4, 16, 16, 64),
+])
+def test_long_keys(tw, q_lens, k_lens, heads, kv_heads, dim):
+    for causal in (True, False):
+        print(q_lens, k_lens, causal, flush=True)
+        check(tw, *inputs(q_lens, k_lens, heads, kv_heads, dim, seed=7), causal=causal, what=str(k_lens))
+
+
+@pytest.mark.parametrize("q_lens,k_lens", [([1, 1], [40, 2000]), ([150, 3], [150, 90])])
+def test_scores_far_apart_and_scale(tw, q_lens, k_lens):
+    # scores of some hundreds: one key has all the weight, and the running maximum changes from tile to tile
+    check(tw, *inputs(q_lens, k_lens, 4, 2, 128, seed=3, spread=6.0), what="far apart")
+    check(tw, *inputs(q_lens, k_lens, 4, 2, 64, seed=4), scale=0.02, what="flat")
+    # a maximum that grows with every key, and one that comes first
+    for order in (1, -1):
+        q, k, v, qo, ko = inputs(q_lens, k_lens, 2, 1, 64, seed=5)
+        ramp = torch.linspace(-4, 4, k.shape[0], device="cuda")[::1 if order == 1 else -1] if order == 1 else torch.linspace(4, -4, k.shape[0], device="cuda")
+        k = ramp[:, None, None].expand_as(k).bfloat16().contiguous()
+        check(tw, q.abs(), k, v, qo, ko, what="ramp")
+
+
+def test_rows_and_memory_outside_the_sequences_are_left_alone(tw):
+    for q_lens, k_lens, heads in (([3, 70], [90, 70], 4), ([1, 1], [900, 1500], 4)):
+        q, k, v, qo, ko = inputs(q_lens, k_lens, heads, 2, 64, tail=5)
+        out, lse = torch.full_like(q, 7.0), torch.full(q.shape[:2], 7.0, device="cuda")
+        for t in (k, v):        # NaN around the sequences' keys
+            t[:5], t[-5:] = math.nan, math.nan
+        check(tw, q, k, v, qo, ko, out=out, lse=lse, what="tail")
+        for t in (out, lse):
+            assert bool((t[:5] == 7).all()) and bool((t[-5:] == 7).all())
+
+
+@pytest.mark.parametrize("bad", [math.nan, math.inf, -math.inf])
+@pytest.mark.parametrize("q_lens,k_lens,heads,dim", [([130, 20], [130, 90], 2, 128), ([2, 2, 4], [33, 900, 64], 8, 64),
+                                                    ([4], [3000], 4, 128)])
+def test_keys_that_a_row_does_not_see_have_no_part_in_it(tw, bad, q_lens, k_lens, heads, dim):
+    """Inf and NaN at the last key of each sequence: seen by its last row only."""
+    q, k, v, qo, ko = inputs(q_lens, k_lens, heads, 2, dim, seed=11)
+    ends = (ko[1:] - 1).long()
+    rows = (qo[1:] - 1).long()
+    clean, clean_lse = tw.attention(q, k, v, qo, ko)
+    v2, k2 = v.clone(), k.clone()
+    v2[ends, :, 1::2] = bad
+    out, lse = check(tw, q, k, v2, qo, ko, what="v")
+    others = torch.ones(q.shape[0], dtype=torch.bool, device="cuda")
+    others[rows] = False
+    assert torch.equal(out[others], clean[others]) and torch.equal(lse, clean_lse)
+    assert not bool(torch.isfinite(out[rows][:, :, 1::2]).any())
+    k2[ends] = bad
+    out, lse = tw.attention(q, k2, v, qo, ko)
+    assert torch.equal(out[others], clean[others]) and torch.equal(lse[others], clean_lse[others])
+
+
+def test_nan_in_a_query_row_stays_there(tw):
+    for q_lens, k_lens in (([70], [70]), ([1, 1], [50, 60])):
+        q, k, v, qo, ko = inputs(q_lens, k_lens, 4, 2, 64, seed=2)
+        clean, _ = tw.attention(q, k, v, qo, ko)
+        q2 = q.clone()
+        q2[-1, 2] = math.nan
+        out, lse = tw.attention(q2, k, v, qo, ko)
+        assert bool(torch.isnan(out[-1, 2]).all()) and bool(torch.isnan(lse[-1, 2]))
+        out[-1, 2] = clean[-1, 2]
+        assert torch.equal(out, clean)
+
+
+def test_columns_of_one_projection(tw):
+    for T, heads, kv_heads, dim in ((77, 6, 2, 64), (300, 8, 4, 128), (1, 4, 1, 24)):
+        g = torch.Generator().manual_seed(T)
+        qkv = torch.randn(T, heads + 2 * kv_heads, dim, generator=g).bfloat16().cuda()
+        q, k, v = qkv.split([heads, kv_heads, kv_heads], dim=1)
+        both = torch.zeros(T, 2 * heads, dim, dtype=torch.bfloat16, device="cuda")
+        o = R.offsets([T]).cuda()
+        check(tw, q, k, v, o, o, out=both[:, heads:], what="packed")
+        assert not bool(both[:, :heads].any())
+
+
+def test_keys_and_values_beyond_32_bit_offsets(tw):
+    """Rows 8 MiB apart: the last ones lie more than 4 GiB from the first."""
+    T, stride = 600, 1 << 22
+    big = torch.empty(T * stride, dtype=torch.bfloat16, device="cuda")
+    k, v = big.as_strided((T, 2, 64), (stride, 64, 1)), big.as_strided((T, 2, 64), (stride, 64, 1), 1024)
+    q, k0, v0, qo, ko = inputs([3, 200], [350, 250], 4, 2, 64)
+    k.copy_(k0)
+    v.copy_(v0)
+    out, lse = tw.attention(q, k, v, qo, ko)
+    want, want_lse = tw.attention(q, k0, v0, qo, ko)
+    assert torch.equal(out, want) and torch.equal(lse, want_lse)
+    check(tw, q, k0, v0, qo, ko)
+
+
+def test_offsets_outside_the_tensors_count_as_their_nearest_row(tw):
+    q, k, v, _, _ = inputs([50, 20], [90, 30], 4, 2, 64)
+    wild = torch.tensor([-5, 50, 1 << 30], dtype=torch.int32, device="cuda")
+    tame = R.offsets([50, 20]).cuda()
+    wild_k, tame_k = torch.tensor([-(1 << 31), 90, (1 << 31) - 1], dtype=torch.int32, device="cuda"), R.offsets([90, 30]).cuda()
+    for x, y in zip(tw.attention(q, k, v, wild, wild_k), tw.attention(q, k, v, tame, tame_k)):
+        assert torch.equal(x, y)
+
+
+def test_a_batch_split_between_its_sequences_and_inside_one_gives_the_same_bits(tw):
+    """The token split: the second half's rows attend to the first half's keys. All three calls have one form."""
+    heads, kv_heads, dim = 64, 32, 64
+    q, k, v, qo, ko = inputs([1700, 3100], [1900, 3100], heads, kv_heads, dim, seed=9)
+    cut, k_cut = 1700 + 1100, 1900 + 1100       # inside the second sequence, with its keys up to there
+    forms = [tw.attention_plan(*n, heads, kv_heads, dim) for n in ((2, 4800, 5000), (2, cut, k_cut), (1, 2000, 5000))]
+    assert len({(f.tile_rows, f.key_waves, f.chunks) for f in forms}) == 1 and forms[0].chunks == 1
+    whole, whole_lse = tw.attention(q, k, v, qo, ko)
+    a, a_lse = tw.attention(q[:cut], k[:k_cut], v[:k_cut], R.offsets([1700, 1100]).cuda(), R.offsets([1900, 1100]).cuda())
+    b, b_lse = tw.attention(q[cut:], k, v, R.offsets([2000]).cuda(), R.offsets([3100], 1900).cuda())
+    assert torch.equal(torch.cat([a, b]), whole) and torch.equal(torch.cat([a_lse, b_lse]), whole_lse)
+
+
+def test_streams_workspaces_and_graphs(tw):
+    """Two streams at once, the workspace from torch or the caller, and a captured call replayed among eager ones."""
+    cases = [inputs([1, 1, 1], [3000, 40, 1800], 8, 2, 128, seed=s) for s in (1, 2)] + [inputs([90, 200], [90, 300], 8, 2, 64, seed=3)]
+    want = [tw.attention(*c) for c in cases]
+    streams = [torch.cuda.Stream() for _ in cases]
+    torch.cuda.synchronize()
+    got = []
+    for _ in range(3):
+        got = []
+        for c, s in zip(cases, streams):
+            out, lse = torch.zeros_like(c[0]), torch.zeros(c[0].shape[:2], device="cuda")
+            s.wait_stream(torch.cuda.current_stream())
+            got.append(tw.attention(*c, out=out, lse=lse, stream=s))
+        torch.cuda.synchronize()
+        for x, y in zip(got, want):
+            assert torch.equal(x[0], y[0]) and torch.equal(x[1], y[1])
+    q, k, v, qo, ko = cases[0]
+    need = tw.attention_workspace_bytes(3, q.shape[0], k.shape[0], 8, 2, 128)
+    assert need > 0
+    space = torch.empty(need, dtype=torch.uint8, device="cuda")
+    with pytest.raises(tw.TwError) as e:
+        tw.attention(*cases[0], workspace=space[:-1])
+    assert e.value.status == 2
+    out, lse = torch.zeros_like(q), torch.zeros(q.shape[:2], device="cuda")
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        tw.attention(*cases[0], out=out, lse=lse, workspace=space)
+    for n in range(4):
+        out.fill_(n)
+        graph.replay()
+        other = tw.attention(*cases[1])
+        torch.cuda.synchronize()
+        assert torch.equal(out, want[0][0]) and torch.equal(lse, want[0][1]) and torch.equal(other[0], want[1][0])
+        q.copy_(cases[1][0] if n % 2 == 0 else inputs([1, 1, 1], [3000, 40, 1800], 8, 2, 128, seed=1)[0])
+        want[0] = tw.attention(*cases[0])
