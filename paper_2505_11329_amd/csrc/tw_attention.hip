@@ -38,6 +38,7 @@ struct AttentionParams {
 };
 
 static constexpr float kMinusInf = -__builtin_inff();
+static constexpr float kLag = 8.0f;
 static constexpr float kLn2 = 0.693147180559945309f;
 
 // The matrix instruction of M x M results, depth 512 / M: operands are 8 values of one row (or column) to a lane, lane l
@@ -243,8 +244,7 @@ __global__ __launch_bounds__(64 * WR * WK, 2) void attention_kernel(AttentionPar
         const int last = real ? min(p.causal ? pos + past : s.k_len - 1, keys.end - 1) : -1;
         const int last_pos = (min((tile + 1) * Shape::kRows, list) - 1) / p.group;
         const int end = min(keys.end, p.causal ? last_pos + past + 1 : s.k_len);
-        // the first row of the wave, and of the tile, sees the fewest keys
-        const int first_last = __builtin_amdgcn_readfirstlane(last);
+        // the first row of the tile sees the fewest keys
         const int tile_first_last = min(keys.end - 1, p.causal ? tile * Shape::kRows / p.group + past : s.k_len - 1);
 
         bf16x8 qf[kSteps];
@@ -318,11 +318,20 @@ __global__ __launch_bounds__(64 * WR * WK, 2) void attention_kernel(AttentionPar
 #pragma unroll
                 for (int i = 0; i < kAcc; ++i) top = fmaxf(top, sc[n][i]);
             top = row_max<M>(top) * p.c;
-            const float m_new = fmaxf(m, top);
-            const float m_use = m_new == kMinusInf ? 0.0f : m_new;
-            const float alpha = __builtin_amdgcn_exp2f(m - m_use);
-            m = m_new;
-            l *= alpha;
+            // The maximum that is taken off follows the row's true one only when that is more than 2^8 ahead: p stays below
+            // 2^8, which changes no relative error, and the sums seldom have to be rescaled. Each row decides for itself.
+            const bool ahead = top > m + kLag;
+            if (__any(ahead)) {
+                const float m_new = ahead ? top : m;
+                const float alpha = ahead ? __builtin_amdgcn_exp2f(m - m_new) : 1.0f;
+                m = m_new;
+                l *= alpha;
+#pragma unroll
+                for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+                    for (int i = 0; i < kAcc; ++i) o[b][i] *= alpha;
+            }
+            const float m_use = m == kMinusInf ? 0.0f : m;
 #pragma unroll
             for (int n = 0; n < kKeyBlocks; ++n)
 #pragma unroll
@@ -330,10 +339,6 @@ __global__ __launch_bounds__(64 * WR * WK, 2) void attention_kernel(AttentionPar
                     sc[n][i] = __builtin_amdgcn_exp2f(fmaf(sc[n][i], p.c, -m_use));
                     l += sc[n][i];
                 }
-#pragma unroll
-            for (int b = 0; b < kBlocks; ++b)
-#pragma unroll
-                for (int i = 0; i < kAcc; ++i) o[b][i] *= alpha;
             auto add_values = [&](auto clean) {
 #pragma unroll
                 for (int t = 0; t < kSlices; ++t) {
@@ -396,15 +401,26 @@ __global__ __launch_bounds__(64 * WR * WK, 2) void attention_kernel(AttentionPar
         int stage = 0;
         if (key_begin < end) {
             load(key_begin);
-            for (int key0 = key_begin; key0 < end; key0 += Shape::kKeys) {
+            int key0 = key_begin;
+            auto next_tile = [&] {
                 store(stage, key0);
                 if (key0 + Shape::kKeys < end) load(key0 + Shape::kKeys);
                 __syncthreads();
-                const int wave_key0 = key0 + wk * KEYS;
-                if (first_last >= wave_key0 + KEYS - 1) compute(key0, stage, std::false_type{});
-                else if (__any(last >= wave_key0)) compute(key0, stage, std::true_type{});
+            };
+            auto tile_done = [&] {
+                key0 += Shape::kKeys;
                 if (STAGES == 1) __syncthreads();
                 else stage ^= 1;
+            };
+            while (key0 + Shape::kKeys - 1 <= tile_first_last) {  // every row sees all of these
+                next_tile();
+                compute(key0, stage, std::false_type{});
+                tile_done();
+            }
+            while (key0 < end) {
+                next_tile();
+                if (__any(last >= key0 + wk * KEYS)) compute(key0, stage, std::true_type{});
+                tile_done();
             }
         }
         l = row_sum<M>(l);
