@@ -32,10 +32,15 @@ struct AttentionParams {
     float *part_ml;
     int64_t q_rows, k_rows;
     int64_t q_stride, k_stride, v_stride, out_stride;  // bytes
+    uint32_t group_magic;  // r / group = r * group_magic >> group_shift
+    int group_shift;
     int n_seqs, q_heads, kv_heads, group, dim, causal;
     int chunks, min_chunk;
     float c;
 };
+
+// The kernels' parts are lambdas: all of them belong into the loop they are called from.
+#define TW_INLINE __attribute__((always_inline))
 
 static constexpr float kMinusInf = -__builtin_inff();
 static constexpr float kLag = 8.0f;
@@ -81,6 +86,12 @@ __device__ __forceinline__ float row_sum(float v)
     return swap_add32(M == 16 ? swap_add16(v) : v);
 }
 
+// The query row, and the head of the group, of row r of a group's list.
+__device__ __forceinline__ int list_pos(const AttentionParams &p, int r)
+{
+    return static_cast<int>(static_cast<uint64_t>(static_cast<uint32_t>(r)) * p.group_magic >> p.group_shift);
+}
+
 // Sequence b's rows, clamped to the tensors whatever the offsets say.
 struct Sequence {
     int64_t q0, k0;
@@ -98,38 +109,6 @@ __device__ __forceinline__ Sequence sequence(const AttentionParams &p, int b)
     const int k0 = clamp_row(__builtin_amdgcn_readfirstlane(p.k_offsets[b]), 0, p.k_rows);
     const int k1 = clamp_row(__builtin_amdgcn_readfirstlane(p.k_offsets[b + 1]), k0, p.k_rows);
     return {q0, k0, q1 - q0, k1 - k0};
-}
-
-// The sequence that the `tile`-th tile of TILE rows of the batch is of, and its place there; false past the last one.
-// Every wave finds it by itself: 64 sequences at a time, a lane each.
-template <int TILE>
-__device__ __forceinline__ bool find_tile(const AttentionParams &p, int64_t tile, int *seq, int *at)
-{
-    const int lane = threadIdx.x & 63;
-    for (int b0 = 0; b0 < p.n_seqs; b0 += 64) {
-        const int b = b0 + lane;
-        int n = 0;
-        if (b < p.n_seqs) {
-            const int q0 = clamp_row(p.q_offsets[b], 0, p.q_rows), q1 = clamp_row(p.q_offsets[b + 1], q0, p.q_rows);
-            n = ((q1 - q0) * p.group + TILE - 1) / TILE;
-        }
-        int upto = n;
-        for (int d = 1; d < 64; d <<= 1) {
-            const int o = __shfl_up(upto, d);
-            if (lane >= d) upto += o;
-        }
-        const int total = __builtin_amdgcn_readlane(upto, 63);
-        if (tile < total) {
-            const int first = __builtin_ctzll(__ballot(upto > tile));
-            *seq = b0 + first;
-            const int of = __builtin_amdgcn_readlane(n, first);
-            // the last tiles first: under a causal mask they have the most keys
-            *at = of - 1 - static_cast<int>(tile - (__builtin_amdgcn_readlane(upto, first) - of));
-            return true;
-        }
-        tile -= total;
-    }
-    return false;
 }
 
 // The keys [begin, end) of chunk c of a sequence.
@@ -187,7 +166,66 @@ __device__ __forceinline__ uint32_t finite_bf16x2(uint32_t x)
     return x & ~((bad - (bad >> 15)) | bad);
 }
 
-template <int DP, int M, int WR, int WK, int KEYS, int STAGES, bool SCAN>
+// One tile's step of the softmax: sc holds a lane's scores and gets p; m and l are the row's. Returns the factor of what was
+// summed before, 1 for most tiles: the maximum that is taken off follows the row's true one only when that is more than 2^8
+// ahead, so that p stays below 2^8, which changes no relative error, and the sums seldom have to be rescaled. Each row
+// decides for itself. (Four chains of maxima and sums: a chain's next instruction waits for eight clocks.)
+template <int M, int N>
+__device__ __forceinline__ float softmax_step(typename Mfma<M>::acc (&sc)[N], float c, float *m, float *l)
+{
+    constexpr int kAcc = M * M / 64;
+    float tops[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) tops[i] = sc[0][i];
+#pragma unroll
+    for (int n = 0; n < N; ++n)
+#pragma unroll
+        for (int i = n == 0 ? 4 : 0; i < kAcc; ++i) tops[i % 4] = fmaxf(tops[i % 4], sc[n][i]);
+    const float top = row_max<M>(fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]))) * c;
+    float alpha = 1.0f;
+    if (top > *m + kLag) {
+        alpha = __builtin_amdgcn_exp2f(*m - top);
+        *m = top;
+        *l *= alpha;
+    }
+    const float m_use = *m == kMinusInf ? 0.0f : *m;
+    float sums[4] = {*l, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int n = 0; n < N; ++n)
+#pragma unroll
+        for (int i = 0; i < kAcc; ++i) {
+            sc[n][i] = __builtin_amdgcn_exp2f(fmaf(sc[n][i], c, -m_use));
+            sums[i % 4] += sc[n][i];
+        }
+    *l = (sums[0] + sums[1]) + (sums[2] + sums[3]);
+    return alpha;
+}
+
+// A row's maximum and sum, by one lane of it, and four of its columns: the result, or a chunk's part of it.
+__device__ __forceinline__ void put_row(const AttentionParams &p, int chunk, int64_t at, float m, float l, bool by_this_lane)
+{
+    if (!by_this_lane) return;
+    if (p.chunks > 1) {
+        float *const to = p.part_ml + (chunk * p.q_rows * p.q_heads + at) * 2;
+        to[0] = m;
+        to[1] = l;
+    } else if (p.lse) {
+        p.lse[at] = l == 0.0f ? kMinusInf : (m + __builtin_amdgcn_logf(l)) * kLn2;
+    }
+}
+__device__ __forceinline__ void put4(const AttentionParams &p, int chunk, int64_t row, int head, int col, f32x4 x, float inv)
+{
+    if (col >= p.dim) return;
+    if (p.chunks > 1) {
+        const int64_t slot = (chunk * p.q_rows + row) * p.q_heads + head;
+        *reinterpret_cast<f32x4 *>(p.part + slot * p.dim + col) = x;
+    } else {
+        const u32x2 y = {pack_bf16x2(x[0] * inv, x[1] * inv), pack_bf16x2(x[2] * inv, x[3] * inv)};
+        *reinterpret_cast<u32x2 *>(p.out + row * p.out_stride + (static_cast<int64_t>(head) * p.dim + col) * 2) = y;
+    }
+}
+
+template <int DP, int M, int WR, int WK, int KEYS, int STAGES>
 __global__ __launch_bounds__(64 * WR * WK, 2) void attention_kernel(AttentionParams p)
 {
     using Shape = AttentionShape<DP, M, WR, WK, KEYS, STAGES>;
@@ -207,13 +245,8 @@ __global__ __launch_bounds__(64 * WR * WK, 2) void attention_kernel(AttentionPar
     const int kv_head = blockIdx.x % p.kv_heads;
     const int rest = blockIdx.x / p.kv_heads;
     const int chunk = rest % p.chunks;
-    int seq = rest / p.chunks, tile = 0;
-    if constexpr (SCAN) {
-        if (!find_tile<Shape::kRows>(p, rest / p.chunks, &seq, &tile)) return;
-        seq = __builtin_amdgcn_readfirstlane(seq);
-        tile = __builtin_amdgcn_readfirstlane(tile);
-    }
-    const Sequence s = sequence(p, seq);
+    int tile = 0;
+    const Sequence s = sequence(p, rest / p.chunks);
     const int list = s.q_len * p.group;  // rows of the group's list
     const Keys keys = chunk_keys(p, s.k_len, chunk);
     const int past = s.k_len - s.q_len;
@@ -234,7 +267,7 @@ __global__ __launch_bounds__(64 * WR * WK, 2) void attention_kernel(AttentionPar
     const int v_frag = Shape::kTileBytes + v_row * Shape::kRowBytes + (i16 & 1) * 8;
     const int v_piece = (((lane / 16) % (M / 16) * 2 + ((i16 & 3) >> 1)) ^ v_swizzle<DP>(v_row)) << 4;
 
-    // In the form without a scan a workgroup has all tiles of its sequence (one, as a rule).
+    // A workgroup has all tiles of its sequence, one as a rule.
     for (;; ++tile) {
         if (tile * Shape::kRows >= list) return;
         const int r = tile * Shape::kRows + wr * M + row_lane;
@@ -312,33 +345,13 @@ __global__ __launch_bounds__(64 * WR * WK, 2) void attention_kernel(AttentionPar
                     for (int i = 0; i < kAcc; ++i)
                         if (n * M + kUnit * (i / 4) + i % 4 > seen) sc[n][i] = kMinusInf;
             }
-            float top = sc[0][0];
-#pragma unroll
-            for (int n = 0; n < kKeyBlocks; ++n)
-#pragma unroll
-                for (int i = 0; i < kAcc; ++i) top = fmaxf(top, sc[n][i]);
-            top = row_max<M>(top) * p.c;
-            // The maximum that is taken off follows the row's true one only when that is more than 2^8 ahead: p stays below
-            // 2^8, which changes no relative error, and the sums seldom have to be rescaled. Each row decides for itself.
-            const bool ahead = top > m + kLag;
-            if (__any(ahead)) {
-                const float m_new = ahead ? top : m;
-                const float alpha = ahead ? __builtin_amdgcn_exp2f(m - m_new) : 1.0f;
-                m = m_new;
-                l *= alpha;
+            const float alpha = softmax_step<M>(sc, p.c, &m, &l);
+            if (__any(alpha != 1.0f)) {
 #pragma unroll
                 for (int b = 0; b < kBlocks; ++b)
 #pragma unroll
                     for (int i = 0; i < kAcc; ++i) o[b][i] *= alpha;
             }
-            const float m_use = m == kMinusInf ? 0.0f : m;
-#pragma unroll
-            for (int n = 0; n < kKeyBlocks; ++n)
-#pragma unroll
-                for (int i = 0; i < kAcc; ++i) {
-                    sc[n][i] = __builtin_amdgcn_exp2f(fmaf(sc[n][i], p.c, -m_use));
-                    l += sc[n][i];
-                }
             auto add_values = [&](auto clean) {
 #pragma unroll
                 for (int t = 0; t < kSlices; ++t) {
@@ -425,31 +438,11 @@ __global__ __launch_bounds__(64 * WR * WK, 2) void attention_kernel(AttentionPar
         }
         l = row_sum<M>(l);
 
-        // a row's maximum and sum, and four of its columns
-        auto put_row = [&](int64_t at, float m_row, float l_row) {
-            if (p.chunks > 1) {
-                float *const to = p.part_ml + (chunk * p.q_rows * p.q_heads + at) * 2;
-                to[0] = m_row;
-                to[1] = l_row;
-            } else if (p.lse) {
-                p.lse[at] = l_row == 0.0f ? kMinusInf : (m_row + __builtin_amdgcn_logf(l_row)) * kLn2;
-            }
-        };
-        auto put4 = [&](int64_t row, int of_head, int col, f32x4 x, float inv) {
-            if (col >= p.dim) return;
-            if (p.chunks > 1) {
-                const int64_t slot = (chunk * p.q_rows + row) * p.q_heads + of_head;
-                *reinterpret_cast<f32x4 *>(p.part + slot * p.dim + col) = x;
-            } else {
-                const u32x2 y = {pack_bf16x2(x[0] * inv, x[1] * inv), pack_bf16x2(x[2] * inv, x[3] * inv)};
-                *reinterpret_cast<u32x2 *>(p.out + row * p.out_stride + (static_cast<int64_t>(of_head) * p.dim + col) * 2) = y;
-            }
-        };
         // (a chunk of no keys has no columns to put: the sum of 0 says so)
         const bool put_columns = p.chunks == 1 || keys.begin < keys.end;
         if constexpr (WK == 1) {
             if (real) {
-                if (part8 == 0) put_row((s.q0 + pos) * p.q_heads + head, m, l);
+                put_row(p, chunk, (s.q0 + pos) * p.q_heads + head, m, l, part8 == 0);
                 // a row that sees no key has l = 0
                 const float inv = l == 0.0f ? 0.0f : 1.0f / l;
                 if (put_columns) {
@@ -457,7 +450,7 @@ __global__ __launch_bounds__(64 * WR * WK, 2) void attention_kernel(AttentionPar
                     for (int b = 0; b < kBlocks; ++b)
 #pragma unroll
                         for (int g = 0; g < kQuads; ++g)
-                            put4(s.q0 + pos, head, b * M + g * kUnit + part8 * 4,
+                            put4(p, chunk, s.q0 + pos, head, b * M + g * kUnit + part8 * 4,
                                  f32x4{o[b][g * 4], o[b][g * 4 + 1], o[b][g * 4 + 2], o[b][g * 4 + 3]}, inv);
                 }
             }
@@ -500,16 +493,351 @@ __global__ __launch_bounds__(64 * WR * WK, 2) void attention_kernel(AttentionPar
                 }
                 const int64_t row = s.q0 + r_join / p.group;
                 const int of_head = kv_head * p.group + r_join % p.group;
-                if (j16 == 0) put_row(row * p.q_heads + of_head, top, sum);
+                put_row(p, chunk, row * p.q_heads + of_head, top, sum, j16 == 0);
                 const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
                 if (put_columns) {
 #pragma unroll
-                    for (int b = 0; b < kFours; ++b) put4(row, of_head, (b * 16 + j16) * 4, x[b], inv);
+                    for (int b = 0; b < kFours; ++b) put4(p, chunk, row, of_head, (b * 16 + j16) * 4, x[b], inv);
                 }
             }
         }
-        if constexpr (SCAN) return;
         __syncthreads();
+    }
+}
+
+// A batch of many rows: 32 rows of a group's list to a wave, and tiles of 64 keys that come straight into the LDS while the
+// tile before is worked on.
+//
+// 128 columns leave room for two waves of a SIMD: eight waves that share their keys (4096 rows of a 16384-token prompt, 64 /
+// 8 heads: 1.64 ms; two workgroups of four: 1.79). 64 columns leave room for three workgroups of four (8192 tokens, 32 heads:
+// 305 us; two of eight: 322).
+template <int DP>
+struct WideShape {
+    static constexpr int kWaves = DP == 128 ? 8 : 4;
+    static constexpr int kThreads = 64 * kWaves, kRows = 32 * kWaves, kKeys = 64;
+    static constexpr int kRowBytes = DP * 2, kTileBytes = kKeys * kRowBytes;
+    static constexpr int kPieces = DP / 8;
+    static constexpr int kLoads = kTileBytes / (16 * kThreads);  // of 16 bytes to a lane, for K or V of a tile
+    static constexpr int kLoadRows = 64 / kPieces;               // rows of a wave's load
+    static constexpr int kStageBytes = 2 * kTileBytes;           // K, V
+    // The rows of q pass through the second stage before its first tile comes, or a place of their own if they are too many;
+    // the results pass through the LDS in the end.
+    static constexpr int kQBytes = kRows * kRowBytes, kQAt = kQBytes <= kStageBytes ? kStageBytes : 2 * kStageBytes;
+    static constexpr int kLds = kQAt + (kQBytes > kStageBytes ? kQBytes : kStageBytes);
+};
+
+// Sum over this lane and those before it.
+__device__ __forceinline__ int sum_upto(int v)
+{
+    v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, true);   // row_shr 1, 2, 4, 8
+    v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, true);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, true);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, true);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false);  // the last of each 16 lanes to the next 16
+    v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);  // lane 31 to lanes 32 ... 63
+    return v;
+}
+
+// The place of a workgroup's tile: its sequence, the tile's number in it.
+struct Place {
+    Sequence s;
+    int tile;
+    bool found;
+};
+// Every wave finds it by itself, 64 sequences at a time, a lane each: the tile-th tile of TILE rows of the batch.
+template <int TILE>
+__device__ __forceinline__ Place find_place(const AttentionParams &p, int tile)
+{
+    const int lane = threadIdx.x & 63;
+    Place at = {};
+    for (int b0 = 0; b0 < p.n_seqs; b0 += 64) {
+        const int b = min(b0 + lane, p.n_seqs - 1);
+        const int qa = p.q_offsets[b], qb = p.q_offsets[b + 1], ka = p.k_offsets[b], kb = p.k_offsets[b + 1];
+        const int q0 = clamp_row(qa, 0, p.q_rows), q1 = clamp_row(qb, q0, p.q_rows);
+        const int k0 = clamp_row(ka, 0, p.k_rows), k1 = clamp_row(kb, k0, p.k_rows);
+        const int n = b0 + lane < p.n_seqs ? ((q1 - q0) * p.group + TILE - 1) / TILE : 0;
+        const int upto = sum_upto(n);
+        const int total = __builtin_amdgcn_readlane(upto, 63);
+        if (tile < total) {
+            const int l = __builtin_ctzll(__ballot(upto > tile));
+            const int of = __builtin_amdgcn_readlane(n, l);
+            at.s.q0 = __builtin_amdgcn_readlane(q0, l);
+            at.s.k0 = __builtin_amdgcn_readlane(k0, l);
+            at.s.q_len = __builtin_amdgcn_readlane(q1, l) - static_cast<int>(at.s.q0);
+            at.s.k_len = __builtin_amdgcn_readlane(k1, l) - static_cast<int>(at.s.k0);
+            // the last tiles first: under a causal mask they have the most keys
+            at.tile = of - 1 - (tile - (__builtin_amdgcn_readlane(upto, l) - of));
+            at.found = true;
+            return at;
+        }
+        tile -= total;
+    }
+    return at;
+}
+
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+
+// 16 bytes to a lane from a buffer to LDS address `to` + 16 lane; the caller waits (vmcnt) before anybody reads them.
+__device__ __forceinline__ void load_to_lds(i32x4 rsrc, uint32_t from, uint32_t scalar_from, uint32_t to)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds"
+                 :
+                 : "s"(to), "v"(from), "s"(rsrc), "s"(scalar_from)
+                 : "memory");
+}
+__device__ __forceinline__ i32x4 buffer_of(const char *p, uint32_t bytes)
+{
+    const uint64_t a = reinterpret_cast<uint64_t>(p);
+    return {static_cast<int>(a), static_cast<int>((a >> 32) & 0xffff), static_cast<int>(bytes), 0x00020000};
+}
+
+template <int DP>
+__global__ __launch_bounds__(WideShape<DP>::kThreads, 2) void attention_wide_kernel(AttentionParams p)
+{
+    using Shape = WideShape<DP>;
+    constexpr int kSteps = DP / 16, kBlocks = DP / 32;
+    extern __shared__ __align__(16) char lds[];
+    __shared__ int flags[Shape::kWaves];  // a wave's pieces of the V tile held Inf or NaN; where rows see a part of the tile
+    const int lane = threadIdx.x & 63, half = lane >> 5, row_lane = lane & 31;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+
+    const int kv_head = blockIdx.x % p.kv_heads;
+    const int rest = blockIdx.x / p.kv_heads;
+    const int chunk = rest % p.chunks;
+    const Place at = find_place<Shape::kRows>(p, rest / p.chunks);
+    if (!at.found) return;
+    const Sequence &s = at.s;
+    const int list = s.q_len * p.group;
+    const Keys keys = chunk_keys(p, s.k_len, chunk);
+    const int past = s.k_len - s.q_len;
+
+    const int r0 = at.tile * Shape::kRows;
+    const int last_pos = list_pos(p, min(r0 + Shape::kRows, list) - 1), first_pos = list_pos(p, r0);
+    const int end = min(keys.end, p.causal ? last_pos + past + 1 : s.k_len);
+    const int first_last = min(keys.end - 1, p.causal ? first_pos + past : s.k_len - 1);  // the last key that the first row sees
+    const int visible = end - keys.begin;  // rows past them read as zeros
+    const int tiles = visible > 0 ? (visible + Shape::kKeys - 1) / Shape::kKeys : 0;
+    const int whole = min(tiles, max(0, first_last + 1 - keys.begin) / Shape::kKeys);  // tiles that every row sees all of
+
+    // where this lane's 16 bytes of a load come from: the piece that lies in its place of the swizzled tile
+    const int load_row = wave * Shape::kLoadRows + lane / Shape::kPieces, place = lane % Shape::kPieces;
+    const int k_piece_from = place ^ k_swizzle<DP>(load_row), v_piece_from = place ^ v_swizzle<DP>(load_row);
+    static_assert((Shape::kWaves * Shape::kLoadRows) % 16 == 0, "a lane's rows have one swizzle");
+    const uint32_t k_from = k_piece_from * 8 < p.dim ? static_cast<uint32_t>(load_row * p.k_stride + k_piece_from * 16) : kPastTensor;
+    const uint32_t v_from = v_piece_from * 8 < p.dim ? static_cast<uint32_t>(load_row * p.v_stride + v_piece_from * 16) : kPastTensor;
+    const char *const k_head = p.k + (s.k0 + keys.begin) * p.k_stride + static_cast<int64_t>(kv_head) * p.dim * 2;
+    const char *const v_head = p.v + (s.k0 + keys.begin) * p.v_stride + static_cast<int64_t>(kv_head) * p.dim * 2;
+    const uint32_t lds_at = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((lds_char_ptr_t)lds));
+    auto load_tile = [&](int t) TW_INLINE {
+        const int rows = min(Shape::kKeys, visible - t * Shape::kKeys);
+        const int64_t row0 = static_cast<int64_t>(t) * Shape::kKeys;
+        const i32x4 rk = buffer_of(k_head + row0 * p.k_stride, static_cast<uint32_t>((rows - 1) * p.k_stride + p.dim * 2));
+        const i32x4 rv = buffer_of(v_head + row0 * p.v_stride, static_cast<uint32_t>((rows - 1) * p.v_stride + p.dim * 2));
+        const uint32_t to = lds_at + (t & 1) * Shape::kStageBytes + wave * 1024;
+#pragma unroll
+        for (int i = 0; i < Shape::kLoads; ++i) {
+            const int64_t rows_on = i * Shape::kWaves * Shape::kLoadRows;
+            load_to_lds(rk, k_from, static_cast<uint32_t>(rows_on * p.k_stride), to + i * Shape::kWaves * 1024);
+            load_to_lds(rv, v_from, static_cast<uint32_t>(rows_on * p.v_stride), to + Shape::kTileBytes + i * Shape::kWaves * 1024);
+        }
+    };
+    if (tiles > 0) load_tile(0);
+
+    // q's rows come by whole rows, too (fragments straight from memory would be 32 rows' 32 bytes at a time)
+    const uint32_t q_at = lds_at + Shape::kQAt + wave * (32 * Shape::kRowBytes);
+    if (tiles > 0) {
+        const i32x4 q_buffer = buffer_of(p.q + (s.q0 + first_pos) * p.q_stride + static_cast<int64_t>(kv_head) * p.group * p.dim * 2, 0x7fffffffu);
+#pragma unroll
+        for (int i = 0; i < 32 / Shape::kLoadRows; ++i) {
+            const int in_wave = i * Shape::kLoadRows + lane / Shape::kPieces, rq = r0 + wave * 32 + in_wave;
+            const int pq = list_pos(p, rq), col = (place ^ k_swizzle<DP>(in_wave)) * 8;
+            const uint32_t from = static_cast<uint32_t>((pq - first_pos) * p.q_stride + ((rq - pq * p.group) * p.dim + col) * 2);
+            load_to_lds(q_buffer, rq < list && col < p.dim ? from : kPastTensor, 0, q_at + i * 1024);
+        }
+    }
+
+    const int r = r0 + wave * 32 + row_lane, pos = list_pos(p, r), head = kv_head * p.group + r - pos * p.group;
+    // keys [0, last] are visible to this lane's row
+    const int last = r < list ? min(p.causal ? pos + past : s.k_len - 1, keys.end - 1) : -1;
+    f32x16 o[kBlocks];
+#pragma unroll
+    for (int b = 0; b < kBlocks; ++b) o[b] = f32x16{};
+    float m = kMinusInf, l = 0.0f;
+
+    // fragments' places
+    const int i16 = lane & 15, v_row = 4 * half + (i16 >> 2);
+    const int k_piece = (half ^ k_swizzle<DP>(row_lane)) << 4;
+    const int v_piece = ((((lane / 16) & 1) * 2 + ((i16 & 3) >> 1)) ^ v_swizzle<DP>(v_row)) << 4;
+    const char *k_frag[kSteps], *v_frag[kBlocks][2];
+#pragma unroll
+    for (int t = 0; t < kSteps; ++t) k_frag[t] = lds + row_lane * Shape::kRowBytes + (k_piece ^ (t * 32));
+#pragma unroll
+    for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+        for (int e = 0; e < 2; ++e)  // a unit of eight rows on, the swizzle of 128 columns differs by a piece
+            v_frag[b][e] = lds + Shape::kTileBytes + (v_row + 8 * e) * Shape::kRowBytes + (i16 & 1) * 8 +
+                           (v_piece ^ (b * 64) ^ (DP == 128 ? e << 4 : 0));
+
+    bf16x8 qf[kSteps];
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+#pragma unroll
+    for (int x = 0; x < kSteps; ++x) qf[x] = *reinterpret_cast<const bf16x8 *>(k_frag[x] + Shape::kQAt + wave * 32 * Shape::kRowBytes);
+
+    auto compute = [&](int t, auto stage_, auto masked) TW_INLINE {
+        constexpr int kStage = decltype(stage_)::value;
+        constexpr bool kMasked = decltype(masked)::value;
+        f32x16 sc[2] = {};
+#pragma unroll
+        for (int n = 0; n < 2; ++n)
+#pragma unroll
+            for (int x = 0; x < kSteps; ++x) {
+                const bf16x8 kf = *reinterpret_cast<const bf16x8 *>(k_frag[x] + kStage * Shape::kStageBytes + n * 32 * Shape::kRowBytes);
+                sc[n] = Mfma<32>::run(kf, qf[x], sc[n]);
+            }
+        if constexpr (kMasked) {
+            const int seen = last - (keys.begin + t * Shape::kKeys) - 4 * half;
+#pragma unroll
+            for (int n = 0; n < 2; ++n)
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    if (n * 32 + 8 * (i / 4) + i % 4 > seen) sc[n][i] = kMinusInf;
+        }
+        const float alpha = softmax_step<32>(sc, p.c, &m, &l);
+        if (__any(alpha != 1.0f)) {
+#pragma unroll
+            for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) o[b][i] *= alpha;
+        }
+#pragma unroll
+        for (int t4 = 0; t4 < 4; ++t4) {
+            u32x4 pf;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) pf[i] = pack_bf16x2(sc[t4 / 2][(t4 & 1) * 8 + 2 * i], sc[t4 / 2][(t4 & 1) * 8 + 2 * i + 1]);
+#pragma unroll
+            for (int b = 0; b < kBlocks; ++b) {
+                u32x4 vf;
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const u32x2 x = __builtin_bit_cast(
+                        u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4bf16(
+                                   (lds_bf16x4_ptr_t)(v_frag[b][e] + kStage * Shape::kStageBytes + t4 * 16 * Shape::kRowBytes)));
+                    vf[2 * e] = x[0];
+                    vf[2 * e + 1] = x[1];
+                }
+                o[b] = Mfma<32>::run(__builtin_bit_cast(bf16x8, vf), __builtin_bit_cast(bf16x8, pf), o[b]);
+            }
+        }
+    };
+
+    // Inf and NaN of hidden keys must not meet a p of zero: a tile that is not whole has zeros put in their place, and the rows
+    // that see them get them added (p > 0 times one of them is the same).
+    auto clean_values = [&](int t) TW_INLINE {
+        char *const mine = lds + (t & 1) * Shape::kStageBytes + Shape::kTileBytes + threadIdx.x * 16;
+        uint32_t bad = 0;
+#pragma unroll
+        for (int i = 0; i < Shape::kLoads; ++i) {
+            u32x4 *const x = reinterpret_cast<u32x4 *>(mine + i * Shape::kWaves * 1024);
+            u32x4 v = *x;
+            uint32_t here = 0;
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+                here |= infinite_bf16x2(v[w]);
+                v[w] = finite_bf16x2(v[w]);
+            }
+            if (here) *x = v;
+            bad |= here;
+        }
+        const bool any = __any(bad != 0);
+        if (lane == 0) flags[wave] = any;
+        __syncthreads();
+        bool infinite = false;
+#pragma unroll
+        for (int w = 0; w < Shape::kWaves; ++w) infinite |= flags[w] != 0;
+        if (__builtin_expect(__builtin_amdgcn_readfirstlane(infinite), 0)) {
+#pragma unroll 1
+            for (int j = t * Shape::kKeys; j < min((t + 1) * Shape::kKeys, visible); ++j) {
+                const char *const row = v_head + j * p.v_stride;
+                const bool sees = keys.begin + j <= last;
+#pragma unroll
+                for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+                    for (int g = 0; g < 4; ++g) {
+                        const int col = b * 32 + g * 8 + half * 4;
+                        u32x2 x = {0, 0};
+                        if (col < p.dim) x = *reinterpret_cast<const u32x2 *>(row + col * 2);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const uint32_t bits = i & 1 ? x[i >> 1] & 0xffff0000u : x[i >> 1] << 16;
+                            const float v = (bits & 0x7f800000u) == 0x7f800000u ? __uint_as_float(bits) : 0.0f;
+                            o[b][g * 4 + i] += sees ? v : 0.0f;
+                        }
+                    }
+            }
+        }
+    };
+
+    // Between two barriers the next tile comes in, into the other half of the LDS.
+    auto turn = [&](int t, auto stage, auto masked) TW_INLINE {
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __syncthreads();
+        if (t + 1 < tiles) load_tile(t + 1);
+        if constexpr (decltype(masked)::value) {
+            clean_values(t);
+            if (!__any(last >= keys.begin + t * Shape::kKeys)) return;
+        }
+        compute(t, stage, masked);
+    };
+    using Stage0 = std::integral_constant<int, 0>;
+    using Stage1 = std::integral_constant<int, 1>;
+    int t = 0;
+    for (; t + 1 < whole; t += 2) {
+        turn(t, Stage0{}, std::false_type{});
+        turn(t + 1, Stage1{}, std::false_type{});
+    }
+    if (t < whole) {
+        turn(t, Stage0{}, std::false_type{});
+        ++t;
+    }
+    for (; t < tiles; ++t) {
+        if (t & 1) turn(t, Stage1{}, std::true_type{});
+        else turn(t, Stage0{}, std::true_type{});
+    }
+
+    l = row_sum<32>(l);
+    if (r < list) put_row(p, chunk, (s.q0 + pos) * p.q_heads + head, m, l, half == 0);
+    if (p.chunks > 1) {
+        // (a chunk of no keys has no columns to put: the sum of 0 says so)
+        if (r < list && keys.begin < keys.end) {
+#pragma unroll
+            for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+                for (int g = 0; g < 4; ++g)
+                    put4(p, chunk, s.q0 + pos, head, b * 32 + g * 8 + half * 4,
+                         f32x4{o[b][g * 4], o[b][g * 4 + 1], o[b][g * 4 + 2], o[b][g * 4 + 3]}, 0.0f);
+        }
+        return;
+    }
+    // Results leave by whole rows: a wave's go through its own part of the LDS.
+    __syncthreads();
+    char *const mine = lds + wave * (32 * Shape::kRowBytes);
+    // a row that sees no key has a sum of 0
+    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+#pragma unroll
+    for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            const u32x2 x = {pack_bf16x2(o[b][g * 4] * inv, o[b][g * 4 + 1] * inv), pack_bf16x2(o[b][g * 4 + 2] * inv, o[b][g * 4 + 3] * inv)};
+            *reinterpret_cast<u32x2 *>(mine + row_lane * Shape::kRowBytes + (((b * 4 + g) ^ k_swizzle<DP>(row_lane)) << 4) + half * 8) = x;
+        }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+#pragma unroll
+    for (int i = 0; i < 32 / Shape::kLoadRows; ++i) {
+        const int in_wave = i * Shape::kLoadRows + lane / Shape::kPieces, ro = r0 + wave * 32 + in_wave, po = list_pos(p, ro);
+        if (ro >= list || place * 8 >= p.dim) continue;
+        const u32x4 x = *reinterpret_cast<const u32x4 *>(mine + in_wave * Shape::kRowBytes + ((place ^ k_swizzle<DP>(in_wave)) << 4));
+        char *const to = p.out + (s.q0 + po) * p.out_stride + (static_cast<int64_t>(kv_head) * p.group + ro - po * p.group) * p.dim * 2;
+        *reinterpret_cast<u32x4 *>(to + place * 16) = x;
     }
 }
 
@@ -604,24 +932,33 @@ static int64_t attention_workspace(const tw_attention_args &a)
     return plan.chunks == 1 ? 0 : static_cast<int64_t>(plan.chunks) * a.q_rows * a.q_heads * (a.head_dim + 2) * 4;
 }
 
-template <int DP, int M, int WR, int WK, int KEYS, int STAGES, bool SCAN>
-static tw_status launch_attention(const AttentionParams &p, int64_t tiles, hipStream_t stream)
+static tw_status launch_attention(void (*kernel)(AttentionParams), std::atomic<int> *allowed, int threads, int lds_bytes,
+                                  const AttentionParams &p, int64_t tiles, hipStream_t stream)
 {
-    using Shape = AttentionShape<DP, M, WR, WK, KEYS, STAGES>;
-    static std::atomic<int> allowed[kMaxDevices];
-    auto kernel = attention_kernel<DP, M, WR, WK, KEYS, STAGES, SCAN>;
-    TW_TRY(allow_dynamic_lds(reinterpret_cast<const void *>(kernel), Shape::kLds, allowed));
+    TW_TRY(allow_dynamic_lds(reinterpret_cast<const void *>(kernel), lds_bytes, allowed));
     const int64_t grid = tiles * p.chunks * p.kv_heads;
     if (grid > INT32_MAX) return TW_ERR_UNSUPPORTED;
-    TW_HIP(launch_kernel(kernel, dim3(static_cast<uint32_t>(grid)), dim3(Shape::kThreads), Shape::kLds, stream, p));
+    TW_HIP(launch_kernel(kernel, dim3(static_cast<uint32_t>(grid)), dim3(static_cast<uint32_t>(threads)),
+                         static_cast<unsigned>(lds_bytes), stream, p));
     return TW_OK;
 }
 
 template <int DP>
+static std::atomic<int> allowed_few[kMaxDevices];
+template <int DP>
+static std::atomic<int> allowed_wide[kMaxDevices];
+
+template <int DP>
 static tw_status launch_attention_for(const AttentionParams &p, const AttentionPlan &plan, hipStream_t stream)
 {
-    if (plan.few) return launch_attention<DP, 16, 1, 4, 32, 1, false>(p, p.n_seqs, stream);
-    return launch_attention<DP, 32, 8, 1, 64, 2, true>(p, p.q_rows * p.group / 256 + p.n_seqs, stream);
+    if (plan.few) {
+        using Shape = AttentionShape<DP, 16, 1, 4, 32, 1>;
+        return launch_attention(attention_kernel<DP, 16, 1, 4, 32, 1>, allowed_few<DP>, Shape::kThreads, Shape::kLds, p, p.n_seqs,
+                                stream);
+    }
+    using Shape = WideShape<DP>;
+    return launch_attention(attention_wide_kernel<DP>, allowed_wide<DP>, Shape::kThreads, Shape::kLds, p,
+                            p.q_rows * p.group / Shape::kRows + p.n_seqs, stream);
 }
 
 }  // namespace tw
@@ -643,7 +980,7 @@ tw_status tw_attention_plan(const tw_attention_args *args, tw_attention_launch *
     *launch = {};
     if (args->n_seqs == 0 || args->q_rows == 0) return TW_OK;
     const AttentionPlan plan = attention_plan(*args);
-    launch->tile_rows = plan.few ? 16 : 256;
+    launch->tile_rows = plan.few ? 16 : args->head_dim > 64 ? WideShape<128>::kRows : WideShape<64>::kRows;
     launch->key_waves = plan.few ? 4 : 1;
     launch->chunks = plan.chunks;
     launch->min_chunk = plan.min_chunk;
@@ -705,6 +1042,10 @@ tw_status tw_attention(const tw_attention_args *args, void *workspace, int64_t w
     p.q_heads = a.q_heads;
     p.kv_heads = a.kv_heads;
     p.group = a.q_heads / a.kv_heads;
+    // exact for r < 2^31: floor(2^(31 + s) / G) + 1 with 2^s >= G
+    p.group_shift = 31;
+    while ((1 << (p.group_shift - 31)) < p.group) ++p.group_shift;
+    p.group_magic = static_cast<uint32_t>((uint64_t(1) << p.group_shift) / p.group + 1);
     p.dim = a.head_dim;
     p.causal = a.causal != 0;
     p.chunks = plan.chunks;
