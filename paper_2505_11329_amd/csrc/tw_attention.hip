@@ -124,26 +124,6 @@ __device__ __forceinline__ Keys chunk_keys(const AttentionParams &p, int k_len, 
     return {static_cast<int>(b), static_cast<int>(min(b + each, static_cast<int64_t>(k_len)))};
 }
 
-// DP: head size padded to 64 or 128. M: rows of a wave (and the matrix instruction). WR waves of a workgroup have M rows
-// each, and each such group of rows has WK waves that share the keys: of a tile of WK * KEYS keys in LDS, KEYS for each.
-template <int DP, int M, int WR, int WK, int KEYS, int STAGES>
-struct AttentionShape {
-    static constexpr int kWaves = WR * WK;
-    static constexpr int kThreads = 64 * kWaves;
-    static constexpr int kRows = M * WR;
-    static constexpr int kKeys = WK * KEYS;
-    static constexpr int kRowBytes = DP * 2;
-    static constexpr int kTileBytes = kKeys * kRowBytes;  // K or V
-    static constexpr int kStageBytes = 2 * kTileBytes;
-    static constexpr int kPieces = DP / 8;  // 16-byte pieces of a row
-    static constexpr int kRowsPerPass = kThreads / kPieces;
-    static constexpr int kPasses = kKeys / kRowsPerPass;
-    static constexpr int kJoinBytes = WK == 1 ? 0 : kRows * WK * (DP + 2) * 4;
-    static constexpr int kLds = STAGES * kStageBytes > kJoinBytes ? STAGES * kStageBytes : kJoinBytes;
-    static_assert(kRowsPerPass % 16 == 0 && kPasses * kRowsPerPass == kKeys, "a thread's pieces have one swizzle");
-    static_assert(WK == 1 || 64 * WK / M == 16, "sixteen threads join a row");
-};
-
 // Where piece c of row r of a tile lies: at c XOR the row's swizzle. K's rows are read one piece of each of 16 rows at a
 // time, V's by 8-byte halves, 32 or 64 bytes of each of eight rows, four neighbouring ones among them. What is read together
 // lies in different LDS banks.
@@ -201,6 +181,27 @@ __device__ __forceinline__ float softmax_step(typename Mfma<M>::acc (&sc)[N], fl
     return alpha;
 }
 
+// Adds a key's values that are Inf or NaN, read from memory, to the sums of a lane whose row sees it.
+template <int M, int N>
+__device__ __forceinline__ void add_infinite(typename Mfma<M>::acc (&o)[N], const char *values, int dim, int part, bool sees)
+{
+    constexpr int kUnit = 256 / M, kQuads = M * M / 256;
+#pragma unroll
+    for (int b = 0; b < N; ++b)
+#pragma unroll
+        for (int g = 0; g < kQuads; ++g) {
+            const int col = b * M + g * kUnit + part * 4;
+            u32x2 x = {0, 0};
+            if (col < dim) x = *reinterpret_cast<const u32x2 *>(values + col * 2);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const uint32_t bits = i & 1 ? x[i >> 1] & 0xffff0000u : x[i >> 1] << 16;
+                o[b][g * 4 + i] += sees && (bits & 0x7f800000u) == 0x7f800000u ? __uint_as_float(bits) : 0.0f;
+            }
+            __builtin_amdgcn_sched_barrier(0);  // (one load at a time: registers are scarce here, and time is not)
+        }
+}
+
 // A row's maximum and sum, by one lane of it, and four of its columns: the result, or a chunk's part of it.
 __device__ __forceinline__ void put_row(const AttentionParams &p, int chunk, int64_t at, float m, float l, bool by_this_lane)
 {
@@ -225,280 +226,249 @@ __device__ __forceinline__ void put4(const AttentionParams &p, int chunk, int64_
     }
 }
 
-template <int DP, int M, int WR, int WK, int KEYS, int STAGES>
-__global__ __launch_bounds__(64 * WR * WK, 2) void attention_kernel(AttentionParams p)
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+
+// 16 bytes to a lane from a buffer to LDS address `to` + 16 lane; the caller waits (vmcnt) before anybody reads them.
+// STREAMED: not to be kept in the caches.
+template <bool STREAMED>
+__device__ __forceinline__ void load_to_lds(i32x4 rsrc, uint32_t from, uint32_t scalar_from, uint32_t to)
 {
-    using Shape = AttentionShape<DP, M, WR, WK, KEYS, STAGES>;
-    using Acc = typename Mfma<M>::acc;
-    constexpr int kDepth = 512 / M, kUnit = 256 / M;  // of a product; keys (or columns of O) to four values of a lane
-    constexpr int kSteps = DP / kDepth;                // products in a block of Q K^T
-    constexpr int kKeyBlocks = KEYS / M;               // blocks of S
-    constexpr int kBlocks = DP / M;                    // blocks of columns of O
-    constexpr int kAcc = M * M / 64, kQuads = kAcc / 4;
-    constexpr int kSlices = KEYS / kDepth;             // products in a block of O
+    if constexpr (STREAMED)
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen nt lds"
+                     :
+                     : "s"(to), "v"(from), "s"(rsrc), "s"(scalar_from)
+                     : "memory");
+    else
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds"
+                     :
+                     : "s"(to), "v"(from), "s"(rsrc), "s"(scalar_from)
+                     : "memory");
+}
+__device__ __forceinline__ i32x4 buffer_of(const char *p, uint32_t bytes)
+{
+    const uint64_t a = reinterpret_cast<uint64_t>(p);
+    return {static_cast<int>(a), static_cast<int>((a >> 32) & 0xffff), static_cast<int>(bytes), 0x00020000};
+}
+
+// Few rows to a sequence, single tokens as a rule: tiles of 16 or 32 rows of a group's list, whose keys four waves share. Bound
+// by what comes from memory. Each wave has keys of its own, 32 at a time, and a place in the LDS for them: the next ones are
+// asked for as soon as a product has read the ones before, and nothing but the result ties the waves to each other. Two
+// workgroups to a compute unit keep up to 128 KB on their way.
+template <int DP, int RB>
+struct FewShape {
+    static constexpr int kWaves = 4, kThreads = 64 * kWaves, kRows = 16 * RB, kKeys = 32;
+    static constexpr int kRowBytes = DP * 2, kTileBytes = kKeys * kRowBytes;
+    static constexpr int kPieces = DP / 8, kLoadRows = 64 / kPieces, kLoads = kKeys / kLoadRows;
+    static constexpr int kJoinBytes = kWaves * kRows * (DP + 2) * 4;
+    static constexpr int kLds = kWaves * 2 * kTileBytes > kJoinBytes ? kWaves * 2 * kTileBytes : kJoinBytes;
+};
+
+template <int N>
+__device__ __forceinline__ void all_but_landed()  // the N newest loads may be under way
+{
+    asm volatile("s_waitcnt vmcnt(%0)" : : "n"(N) : "memory");
+}
+__device__ __forceinline__ void lds_read() { asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory"); }
+
+template <int DP, int RB, bool STREAMED>
+__global__ __launch_bounds__(256, 2) void attention_few_kernel(AttentionParams p)
+{
+    using Shape = FewShape<DP, RB>;
+    constexpr int kSteps = DP / 32, kBlocks = DP / 16;
     extern __shared__ __align__(16) char lds[];
-    __shared__ int flags[STAGES * Shape::kWaves];  // a wave's part of the V tile holds Inf or NaN; where rows see a part of the tile
-    const int lane = threadIdx.x & 63, part8 = lane / M, row_lane = lane % M;
+    const int lane = threadIdx.x & 63, part = lane / 16, row_lane = lane % 16;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int wr = wave / WK, wk = wave % WK;
 
     const int kv_head = blockIdx.x % p.kv_heads;
     const int rest = blockIdx.x / p.kv_heads;
     const int chunk = rest % p.chunks;
-    int tile = 0;
     const Sequence s = sequence(p, rest / p.chunks);
-    const int list = s.q_len * p.group;  // rows of the group's list
+    const int list = s.q_len * p.group;
     const Keys keys = chunk_keys(p, s.k_len, chunk);
     const int past = s.k_len - s.q_len;
 
-    // where this thread's 16-byte pieces of a K and a V tile come from, and go to
-    const int piece = threadIdx.x % Shape::kPieces, piece_row = threadIdx.x / Shape::kPieces;
-    const uint32_t k_from = piece * 8 < p.dim ? static_cast<uint32_t>(piece_row * p.k_stride + piece * 16) : kPastTensor;
-    const uint32_t v_from = piece * 8 < p.dim ? static_cast<uint32_t>(piece_row * p.v_stride + piece * 16) : kPastTensor;
-    const int k_to = piece_row * Shape::kRowBytes + ((piece ^ k_swizzle<DP>(piece_row)) << 4);
-    const int v_to = Shape::kTileBytes + piece_row * Shape::kRowBytes + ((piece ^ v_swizzle<DP>(piece_row)) << 4);
+    // where this lane's 16 bytes of a load come from: the piece that lies in its place of the swizzled tile
+    const int load_row = lane / Shape::kPieces, place = lane % Shape::kPieces;
     const char *const k_head = p.k + s.k0 * p.k_stride + static_cast<int64_t>(kv_head) * p.dim * 2;
     const char *const v_head = p.v + s.k0 * p.v_stride + static_cast<int64_t>(kv_head) * p.dim * 2;
+    char *const mine = lds + wave * 2 * Shape::kTileBytes;
+    const uint32_t k_at = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((lds_char_ptr_t)mine)), v_at = k_at + Shape::kTileBytes;
 
-    // fragments' places in a tile
-    const int k_frag = (wk * KEYS + row_lane) * Shape::kRowBytes;
-    const int k_piece = (part8 ^ k_swizzle<DP>(row_lane)) << 4;  // a step on is a step's pieces on: XOR
-    const int i16 = lane & 15, v_row = wk * KEYS + 4 * part8 + (i16 >> 2);
-    const int v_frag = Shape::kTileBytes + v_row * Shape::kRowBytes + (i16 & 1) * 8;
-    const int v_piece = (((lane / 16) % (M / 16) * 2 + ((i16 & 3) >> 1)) ^ v_swizzle<DP>(v_row)) << 4;
+    // fragments' places
+    const int i16 = lane & 15, v_row = 4 * part + (i16 >> 2);
+    const char *k_frag[kSteps], *v_frag[kBlocks];
+#pragma unroll
+    for (int x = 0; x < kSteps; ++x) k_frag[x] = mine + row_lane * Shape::kRowBytes + (((4 * x + part) ^ k_swizzle<DP>(row_lane)) << 4);
+#pragma unroll
+    for (int b = 0; b < kBlocks; ++b)
+        v_frag[b] = mine + Shape::kTileBytes + v_row * Shape::kRowBytes + (((2 * b + ((i16 & 3) >> 1)) ^ v_swizzle<DP>(v_row)) << 4) + (i16 & 1) * 8;
 
-    // A workgroup has all tiles of its sequence, one as a rule.
-    for (;; ++tile) {
-        if (tile * Shape::kRows >= list) return;
-        const int r = tile * Shape::kRows + wr * M + row_lane;
-        const int pos = r / p.group, head = kv_head * p.group + r % p.group;
-        const bool real = r < list;
-        // keys [0, last] are visible to this lane's row
-        const int last = real ? min(p.causal ? pos + past : s.k_len - 1, keys.end - 1) : -1;
-        const int last_pos = (min((tile + 1) * Shape::kRows, list) - 1) / p.group;
+    for (int r0 = 0; r0 < list; r0 += Shape::kRows) {  // one tile as a rule
+        const int last_pos = list_pos(p, min(r0 + Shape::kRows, list) - 1);
         const int end = min(keys.end, p.causal ? last_pos + past + 1 : s.k_len);
-        // the first row of the tile sees the fewest keys
-        const int tile_first_last = min(keys.end - 1, p.causal ? tile * Shape::kRows / p.group + past : s.k_len - 1);
+        const int first_last = min(keys.end - 1, p.causal ? list_pos(p, r0) + past : s.k_len - 1);  // the last key that the first row sees
 
-        bf16x8 qf[kSteps];
+        auto load_rows = [&](const char *base, int64_t stride, int key0, uint32_t to, auto swizzle) TW_INLINE {
+            const int rows = min(Shape::kKeys, end - key0);
+            const i32x4 rsrc = buffer_of(base + key0 * stride, rows > 0 ? static_cast<uint32_t>((rows - 1) * stride + p.dim * 2) : 0);
 #pragma unroll
-        for (int t = 0; t < kSteps; ++t) {
-            u32x4 x = {0, 0, 0, 0};
-            const int col = t * kDepth + part8 * 8;
-            if (real && col < p.dim)
-                x = *reinterpret_cast<const u32x4 *>(p.q + (s.q0 + pos) * p.q_stride + (static_cast<int64_t>(head) * p.dim + col) * 2);
-            qf[t] = __builtin_bit_cast(bf16x8, x);
-        }
-        Acc o[kBlocks];
-#pragma unroll
-        for (int b = 0; b < kBlocks; ++b) o[b] = Acc{};
-        float m = kMinusInf, l = 0.0f;
-
-        u32x4 kr[Shape::kPasses], vr[Shape::kPasses];
-        auto load = [&](int key0) {
-            const int rows = min(Shape::kKeys, end - key0);  // rows past the last visible key read as zeros
-            const auto rk = make_rsrc(k_head + static_cast<int64_t>(key0) * p.k_stride,
-                                      rows > 0 ? static_cast<uint32_t>((rows - 1) * p.k_stride + p.dim * 2) : 0);
-            const auto rv = make_rsrc(v_head + static_cast<int64_t>(key0) * p.v_stride,
-                                      rows > 0 ? static_cast<uint32_t>((rows - 1) * p.v_stride + p.dim * 2) : 0);
-#pragma unroll
-            for (int i = 0; i < Shape::kPasses; ++i) {
-                kr[i] = __builtin_amdgcn_raw_buffer_load_b128(rk, k_from, static_cast<int>(i * Shape::kRowsPerPass * p.k_stride), 0);
-                vr[i] = __builtin_amdgcn_raw_buffer_load_b128(rv, v_from, static_cast<int>(i * Shape::kRowsPerPass * p.v_stride), 0);
+            for (int i = 0; i < Shape::kLoads; ++i) {
+                const int col = (place ^ swizzle(i * Shape::kLoadRows + load_row)) * 8;
+                load_to_lds<STREAMED>(rsrc, col < p.dim ? static_cast<uint32_t>(load_row * stride + col * 2) : kPastTensor,
+                                      static_cast<uint32_t>(i * Shape::kLoadRows * stride), to + i * 1024);
             }
         };
-        auto store = [&](int stage, int key0) {
-            if (key0 + Shape::kKeys - 1 > tile_first_last) {  // a tile that some row sees a part of
+        auto load_keys = [&](int key0) TW_INLINE { load_rows(k_head, p.k_stride, key0, k_at, [](int row) { return k_swizzle<DP>(row); }); };
+        auto load_values = [&](int key0) TW_INLINE { load_rows(v_head, p.v_stride, key0, v_at, [](int row) { return v_swizzle<DP>(row); }); };
+
+        int key0 = keys.begin + wave * Shape::kKeys;
+        constexpr int kOn = Shape::kWaves * Shape::kKeys;
+        load_keys(key0);
+        load_values(key0);
+        int last[RB];  // keys [0, last] are visible to this lane's rows
+        bf16x8 qf[RB][kSteps];
+        f32x4 o[RB][kBlocks] = {};
+        float m[RB], l[RB];
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb) {
+            const int r = r0 + rb * 16 + row_lane, pos = list_pos(p, r), head = kv_head * p.group + r - pos * p.group;
+            last[rb] = r < list ? min(p.causal ? pos + past : s.k_len - 1, keys.end - 1) : -1;
+            m[rb] = kMinusInf;
+            l[rb] = 0.0f;
+#pragma unroll
+            for (int x = 0; x < kSteps; ++x) {
+                u32x4 q = {0, 0, 0, 0};
+                const int col = x * 32 + part * 8;
+                if (r < list && col < p.dim)
+                    q = *reinterpret_cast<const u32x4 *>(p.q + (s.q0 + pos) * p.q_stride + (static_cast<int64_t>(head) * p.dim + col) * 2);
+                qf[rb][x] = __builtin_bit_cast(bf16x8, q);
+            }
+        }
+        for (; key0 < end; key0 += kOn) {
+            f32x4 sc[RB][2] = {};
+            all_but_landed<Shape::kLoads>();
+#pragma unroll
+            for (int x = 0; x < kSteps; ++x)
+#pragma unroll
+                for (int n = 0; n < 2; ++n) {
+                    const bf16x8 kf = *reinterpret_cast<const bf16x8 *>(k_frag[x] + n * 16 * Shape::kRowBytes);
+#pragma unroll
+                    for (int rb = 0; rb < RB; ++rb) sc[rb][n] = Mfma<16>::run(kf, qf[rb][x], sc[rb][n]);
+                }
+            lds_read();
+            load_keys(key0 + kOn);  // (past the end: no bytes, but as many loads to wait for)
+            const bool masked = first_last < key0 + Shape::kKeys - 1;
+            if (masked) {
+#pragma unroll
+                for (int rb = 0; rb < RB; ++rb) {
+                    const int seen = last[rb] - key0 - 4 * part;
+#pragma unroll
+                    for (int n = 0; n < 2; ++n)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            if (n * 16 + i > seen) sc[rb][n][i] = kMinusInf;
+                }
+            }
+            u32x4 pf[RB];
+#pragma unroll
+            for (int rb = 0; rb < RB; ++rb) {
+                const float alpha = softmax_step<16>(sc[rb], p.c, &m[rb], &l[rb]);
+                if (__any(alpha != 1.0f)) {
+#pragma unroll
+                    for (int b = 0; b < kBlocks; ++b) o[rb][b] *= alpha;
+                }
+                pf[rb] = {pack_bf16x2(sc[rb][0][0], sc[rb][0][1]), pack_bf16x2(sc[rb][0][2], sc[rb][0][3]),
+                          pack_bf16x2(sc[rb][1][0], sc[rb][1][1]), pack_bf16x2(sc[rb][1][2], sc[rb][1][3])};
+            }
+            all_but_landed<Shape::kLoads>();
+            if (masked) {
+                // Inf and NaN of hidden keys must not meet a p of zero: zeros in their place, and the rows that see them get
+                // them added (p > 0 times one of them is the same)
                 uint32_t bad = 0;
 #pragma unroll
-                for (int i = 0; i < Shape::kPasses; ++i)
+                for (int i = 0; i < Shape::kLoads; ++i) {
+                    u32x4 *const x = reinterpret_cast<u32x4 *>(mine + Shape::kTileBytes + i * 1024 + lane * 16);
+                    u32x4 v = *x;
+                    uint32_t here = 0;
 #pragma unroll
-                    for (int w = 0; w < 4; ++w) bad |= infinite_bf16x2(vr[i][w]);
-                const bool any = __any(bad != 0);
-                if (lane == 0) flags[stage * Shape::kWaves + wave] = any;
-            }
-#pragma unroll
-            for (int i = 0; i < Shape::kPasses; ++i) {
-                const int at = stage * Shape::kStageBytes + i * Shape::kRowsPerPass * Shape::kRowBytes;
-                *reinterpret_cast<u32x4 *>(lds + at + k_to) = kr[i];
-                *reinterpret_cast<u32x4 *>(lds + at + v_to) = vr[i];
-            }
-        };
-        auto compute = [&](int key0, int stage, auto masked) {
-            const char *const base = lds + stage * Shape::kStageBytes;
-            Acc sc[kKeyBlocks];
-#pragma unroll
-            for (int n = 0; n < kKeyBlocks; ++n) {
-                sc[n] = Acc{};
-#pragma unroll
-                for (int t = 0; t < kSteps; ++t) {
-                    const bf16x8 kf = *reinterpret_cast<const bf16x8 *>(base + k_frag + n * M * Shape::kRowBytes + (k_piece ^ (t * kDepth * 2)));
-                    sc[n] = Mfma<M>::run(kf, qf[t], sc[n]);
-                }
-            }
-            const int wave_key0 = key0 + wk * KEYS;
-            if constexpr (decltype(masked)::value) {
-                const int seen = last - wave_key0 - 4 * part8;
-#pragma unroll
-                for (int n = 0; n < kKeyBlocks; ++n)
-#pragma unroll
-                    for (int i = 0; i < kAcc; ++i)
-                        if (n * M + kUnit * (i / 4) + i % 4 > seen) sc[n][i] = kMinusInf;
-            }
-            const float alpha = softmax_step<M>(sc, p.c, &m, &l);
-            if (__any(alpha != 1.0f)) {
-#pragma unroll
-                for (int b = 0; b < kBlocks; ++b)
-#pragma unroll
-                    for (int i = 0; i < kAcc; ++i) o[b][i] *= alpha;
-            }
-            auto add_values = [&](auto clean) {
-#pragma unroll
-                for (int t = 0; t < kSlices; ++t) {
-                    u32x4 pf;
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const int at = t * 8 + 2 * i;  // among all the lane's values of S
-                        pf[i] = pack_bf16x2(sc[at / kAcc][at % kAcc], sc[(at + 1) / kAcc][(at + 1) % kAcc]);
+                    for (int w = 0; w < 4; ++w) {
+                        here |= infinite_bf16x2(v[w]);
+                        v[w] = finite_bf16x2(v[w]);
                     }
-#pragma unroll
-                    for (int b = 0; b < kBlocks; ++b) {
-                        u32x4 vf;
-#pragma unroll
-                        for (int e = 0; e < 2; ++e) {
-                            // a unit of eight rows on, the swizzle of 128 columns differs by a piece
-                            const int at = (t * kDepth + e * kUnit) * Shape::kRowBytes + (v_piece ^ (b * M * 2) ^ (DP == 128 && M == 32 ? e << 4 : 0));
-                            const u32x2 x = __builtin_bit_cast(
-                                u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4_ptr_t)(base + v_frag + at)));
-                            vf[2 * e] = decltype(clean)::value ? finite_bf16x2(x[0]) : x[0];
-                            vf[2 * e + 1] = decltype(clean)::value ? finite_bf16x2(x[1]) : x[1];
-                        }
-                        o[b] = Mfma<M>::run(__builtin_bit_cast(bf16x8, vf), __builtin_bit_cast(bf16x8, pf), o[b]);
-                    }
+                    if (here) *x = v;
+                    bad |= here;
                 }
-            };
-            if constexpr (decltype(masked)::value) {
-                bool infinite = false;
-#pragma unroll
-                for (int w = 0; w < Shape::kWaves; ++w) infinite |= flags[stage * Shape::kWaves + w] != 0;
-                if (__builtin_expect(__builtin_amdgcn_readfirstlane(infinite), 0)) {
-                    // Inf and NaN of hidden keys must not meet a p of zero: left out of the product, and added to the
-                    // rows that see them (p > 0 times one of them is the same)
-                    add_values(std::true_type{});
+                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+                if (__builtin_expect(__any(bad != 0), 0)) {
 #pragma unroll 1
-                    for (int j = 0; j < KEYS; ++j) {
-                        const int row = wk * KEYS + j;
-                        const bool sees = wave_key0 + j <= last;
+                    for (int j = key0; j < min(key0 + Shape::kKeys, end); ++j)
 #pragma unroll
-                        for (int b = 0; b < kBlocks; ++b)
-#pragma unroll
-                            for (int g = 0; g < kQuads; ++g) {
-                                const int col = b * M + g * kUnit + part8 * 4;
-                                const u32x2 x = *reinterpret_cast<const u32x2 *>(
-                                    base + Shape::kTileBytes + row * Shape::kRowBytes + (((col >> 3) ^ v_swizzle<DP>(row)) << 4) + (col & 4) * 2);
-#pragma unroll
-                                for (int i = 0; i < 4; ++i) {
-                                    const uint32_t bits = i & 1 ? x[i >> 1] & 0xffff0000u : x[i >> 1] << 16;
-                                    o[b][g * 4 + i] += sees && (bits & 0x7f800000u) == 0x7f800000u ? __uint_as_float(bits) : 0.0f;
-                                }
-                            }
-                    }
-                    return;
+                        for (int rb = 0; rb < RB; ++rb) add_infinite<16, kBlocks>(o[rb], v_head + j * p.v_stride, p.dim, part, j <= last[rb]);
                 }
             }
-            add_values(std::false_type{});
-        };
-
-        // this chunk's tiles; a tile of keys that no row sees is not read
-        const int key_begin = keys.begin;
-        int stage = 0;
-        if (key_begin < end) {
-            load(key_begin);
-            int key0 = key_begin;
-            auto next_tile = [&] {
-                store(stage, key0);
-                if (key0 + Shape::kKeys < end) load(key0 + Shape::kKeys);
-                __syncthreads();
-            };
-            auto tile_done = [&] {
-                key0 += Shape::kKeys;
-                if (STAGES == 1) __syncthreads();
-                else stage ^= 1;
-            };
-            while (key0 + Shape::kKeys - 1 <= tile_first_last) {  // every row sees all of these
-                next_tile();
-                compute(key0, stage, std::false_type{});
-                tile_done();
+#pragma unroll
+            for (int b = 0; b < kBlocks; ++b) {
+                u32x4 vf;
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const u32x2 x = __builtin_bit_cast(
+                        u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4_ptr_t)(v_frag[b] + e * 16 * Shape::kRowBytes)));
+                    vf[2 * e] = x[0];
+                    vf[2 * e + 1] = x[1];
+                }
+#pragma unroll
+                for (int rb = 0; rb < RB; ++rb)
+                    o[rb][b] = Mfma<16>::run(__builtin_bit_cast(bf16x8, vf), __builtin_bit_cast(bf16x8, pf[rb]), o[rb][b]);
             }
-            while (key0 < end) {
-                next_tile();
-                if (__any(last >= key0 + wk * KEYS)) compute(key0, stage, std::true_type{});
-                tile_done();
+            lds_read();
+            load_values(key0 + kOn);
+        }
+
+        // the waves' maxima, sums and sums of v pass through the LDS and are joined in the order of the waves, by sixteen
+        // threads to a row
+        all_but_landed<0>();
+        __syncthreads();
+        float *const sums = reinterpret_cast<float *>(lds);
+        float *const ml = sums + Shape::kWaves * Shape::kRows * DP;
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb) {
+            const int slot = wave * Shape::kRows + rb * 16 + row_lane;
+            const float sum = row_sum<16>(l[rb]);
+#pragma unroll
+            for (int b = 0; b < kBlocks; ++b) *reinterpret_cast<f32x4 *>(sums + slot * DP + ((b * 4 + part) ^ (row_lane & 7)) * 4) = o[rb][b];
+            if (part == 0) {
+                ml[slot * 2] = m[rb];
+                ml[slot * 2 + 1] = sum;
             }
         }
-        l = row_sum<M>(l);
-
-        // (a chunk of no keys has no columns to put: the sum of 0 says so)
-        const bool put_columns = p.chunks == 1 || keys.begin < keys.end;
-        if constexpr (WK == 1) {
-            if (real) {
-                put_row(p, chunk, (s.q0 + pos) * p.q_heads + head, m, l, part8 == 0);
-                // a row that sees no key has l = 0
-                const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-                if (put_columns) {
+        __syncthreads();
+        constexpr int kFours = DP / 64;  // of a thread's columns
 #pragma unroll
-                    for (int b = 0; b < kBlocks; ++b)
+        for (int rb = 0; rb < RB; ++rb) {
+            const int jr = rb * 16 + (threadIdx.x >> 4), j16 = threadIdx.x & 15, r = r0 + jr;
+            if (r >= list) continue;
+            float top = kMinusInf, sum = 0.0f;
 #pragma unroll
-                        for (int g = 0; g < kQuads; ++g)
-                            put4(p, chunk, s.q0 + pos, head, b * M + g * kUnit + part8 * 4,
-                                 f32x4{o[b][g * 4], o[b][g * 4 + 1], o[b][g * 4 + 2], o[b][g * 4 + 3]}, inv);
-                }
+            for (int w = 0; w < Shape::kWaves; ++w) top = fmaxf(top, ml[(w * Shape::kRows + jr) * 2]);
+            const float top_use = top == kMinusInf ? 0.0f : top;
+            f32x4 x[kFours] = {};
+#pragma unroll
+            for (int w = 0; w < Shape::kWaves; ++w) {
+                const int from = w * Shape::kRows + jr;
+                const float f = __builtin_amdgcn_exp2f(ml[from * 2] - top_use);
+                sum += f * ml[from * 2 + 1];
+#pragma unroll
+                for (int b = 0; b < kFours; ++b)
+                    x[b] += f * *reinterpret_cast<const f32x4 *>(sums + from * DP + ((b * 16 + j16) ^ (jr & 7)) * 4);
             }
-        } else {
-            // the waves' maxima, sums and sums of v pass through the LDS and are joined in the order of the waves, by
-            // sixteen threads to a row
-            __syncthreads();
-            float *const part = reinterpret_cast<float *>(lds);
-            float *const ml = part + WK * Shape::kRows * DP;
-            const int slot = wk * Shape::kRows + wr * M + row_lane;
+            const int pos = list_pos(p, r), head = kv_head * p.group + r - pos * p.group;
+            put_row(p, chunk, (s.q0 + pos) * p.q_heads + head, top, sum, j16 == 0);
+            // a row that sees no key has a sum of 0
+            const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+            // (a chunk of no keys has no columns to put: the sum of 0 says so)
+            if (p.chunks == 1 || keys.begin < keys.end) {
 #pragma unroll
-            for (int b = 0; b < kBlocks; ++b)
-#pragma unroll
-                for (int g = 0; g < kQuads; ++g) {
-                    const int c = ((b * M + g * kUnit) / 4 + part8) ^ (row_lane & 7);
-                    *reinterpret_cast<f32x4 *>(part + slot * DP + c * 4) =
-                        f32x4{o[b][g * 4], o[b][g * 4 + 1], o[b][g * 4 + 2], o[b][g * 4 + 3]};
-                }
-            if (part8 == 0) {
-                ml[slot * 2] = m;
-                ml[slot * 2 + 1] = l;
-            }
-            __syncthreads();
-            constexpr int kFours = DP / 64;  // of a thread's columns
-            const int jr = threadIdx.x >> 4, j16 = threadIdx.x & 15, r_join = tile * Shape::kRows + jr;
-            if (r_join < list) {
-                float top = kMinusInf, sum = 0.0f;
-#pragma unroll
-                for (int w = 0; w < WK; ++w) top = fmaxf(top, ml[(w * Shape::kRows + jr) * 2]);
-                const float top_use = top == kMinusInf ? 0.0f : top;
-                f32x4 x[kFours] = {};
-#pragma unroll
-                for (int w = 0; w < WK; ++w) {
-                    const int from = w * Shape::kRows + jr;
-                    const float f = __builtin_amdgcn_exp2f(ml[from * 2] - top_use);
-                    sum += f * ml[from * 2 + 1];
-#pragma unroll
-                    for (int b = 0; b < kFours; ++b)
-                        x[b] += f * *reinterpret_cast<const f32x4 *>(part + from * DP + ((b * 16 + j16) ^ (jr & 7)) * 4);
-                }
-                const int64_t row = s.q0 + r_join / p.group;
-                const int of_head = kv_head * p.group + r_join % p.group;
-                put_row(p, chunk, row * p.q_heads + of_head, top, sum, j16 == 0);
-                const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-                if (put_columns) {
-#pragma unroll
-                    for (int b = 0; b < kFours; ++b) put4(p, chunk, row, of_head, (b * 16 + j16) * 4, x[b], inv);
-                }
+                for (int b = 0; b < kFours; ++b) put4(p, chunk, s.q0 + pos, head, (b * 16 + j16) * 4, x[b], inv);
             }
         }
         __syncthreads();
@@ -508,12 +478,12 @@ __global__ __launch_bounds__(64 * WR * WK, 2) void attention_kernel(AttentionPar
 // A batch of many rows: 32 rows of a group's list to a wave, and tiles of 64 keys that come straight into the LDS while the
 // tile before is worked on.
 //
-// 128 columns leave room for two waves of a SIMD: eight waves that share their keys (4096 rows of a 16384-token prompt, 64 /
-// 8 heads: 1.64 ms; two workgroups of four: 1.79). 64 columns leave room for three workgroups of four (8192 tokens, 32 heads:
-// 305 us; two of eight: 322).
-template <int DP>
+// 128 columns leave room for two waves of a SIMD. Eight that share their keys are faster where there are rows enough (4096 rows of a
+// 16384-token prompt, 64 / 8 heads: 1.64 ms; two workgroups of four: 1.79). 64 columns leave room for three workgroups of four
+// (8192 tokens, 32 heads: 305 us; two of eight: 322).
+template <int DP, int WAVES>
 struct WideShape {
-    static constexpr int kWaves = DP == 128 ? 8 : 4;
+    static constexpr int kWaves = WAVES;
     static constexpr int kThreads = 64 * kWaves, kRows = 32 * kWaves, kKeys = 64;
     static constexpr int kRowBytes = DP * 2, kTileBytes = kKeys * kRowBytes;
     static constexpr int kPieces = DP / 8;
@@ -605,26 +575,10 @@ __device__ __forceinline__ Place find_place(const AttentionParams &p, int i)
     return at;
 }
 
-typedef int i32x4 __attribute__((ext_vector_type(4)));
-
-// 16 bytes to a lane from a buffer to LDS address `to` + 16 lane; the caller waits (vmcnt) before anybody reads them.
-__device__ __forceinline__ void load_to_lds(i32x4 rsrc, uint32_t from, uint32_t scalar_from, uint32_t to)
+template <int DP, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, 2) void attention_wide_kernel(AttentionParams p)
 {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds"
-                 :
-                 : "s"(to), "v"(from), "s"(rsrc), "s"(scalar_from)
-                 : "memory");
-}
-__device__ __forceinline__ i32x4 buffer_of(const char *p, uint32_t bytes)
-{
-    const uint64_t a = reinterpret_cast<uint64_t>(p);
-    return {static_cast<int>(a), static_cast<int>((a >> 32) & 0xffff), static_cast<int>(bytes), 0x00020000};
-}
-
-template <int DP>
-__global__ __launch_bounds__(WideShape<DP>::kThreads, 2) void attention_wide_kernel(AttentionParams p)
-{
-    using Shape = WideShape<DP>;
+    using Shape = WideShape<DP, WAVES>;
     constexpr int kSteps = DP / 16, kBlocks = DP / 32;
     extern __shared__ __align__(16) char lds[];
     __shared__ int flags[Shape::kWaves];  // a wave's pieces of the V tile held Inf or NaN; where rows see a part of the tile
@@ -667,8 +621,8 @@ __global__ __launch_bounds__(WideShape<DP>::kThreads, 2) void attention_wide_ker
 #pragma unroll
         for (int i = 0; i < Shape::kLoads; ++i) {
             const int64_t rows_on = i * Shape::kWaves * Shape::kLoadRows;
-            load_to_lds(rk, k_from, static_cast<uint32_t>(rows_on * p.k_stride), to + i * Shape::kWaves * 1024);
-            load_to_lds(rv, v_from, static_cast<uint32_t>(rows_on * p.v_stride), to + Shape::kTileBytes + i * Shape::kWaves * 1024);
+            load_to_lds<false>(rk, k_from, static_cast<uint32_t>(rows_on * p.k_stride), to + i * Shape::kWaves * 1024);
+            load_to_lds<false>(rv, v_from, static_cast<uint32_t>(rows_on * p.v_stride), to + Shape::kTileBytes + i * Shape::kWaves * 1024);
         }
     };
     if (tiles > 0) load_tile(0);
@@ -682,7 +636,7 @@ __global__ __launch_bounds__(WideShape<DP>::kThreads, 2) void attention_wide_ker
             const int in_wave = i * Shape::kLoadRows + lane / Shape::kPieces, rq = r0 + wave * 32 + in_wave;
             const int pq = list_pos(p, rq), col = (place ^ k_swizzle<DP>(in_wave)) * 8;
             const uint32_t from = static_cast<uint32_t>((pq - first_pos) * p.q_stride + ((rq - pq * p.group) * p.dim + col) * 2);
-            load_to_lds(q_buffer, rq < list && col < p.dim ? from : kPastTensor, 0, q_at + i * 1024);
+            load_to_lds<false>(q_buffer, rq < list && col < p.dim ? from : kPastTensor, 0, q_at + i * 1024);
         }
     }
 
@@ -761,7 +715,7 @@ __global__ __launch_bounds__(WideShape<DP>::kThreads, 2) void attention_wide_ker
     };
 
     // Inf and NaN of hidden keys must not meet a p of zero: a tile that is not whole has zeros put in their place, and the rows
-    // that see them get them added (p > 0 times one of them is the same).
+    // that see them get them added behind its step (p > 0 times one of them is the same).
     auto clean_values = [&](int t) TW_INLINE {
         char *const mine = lds + (t & 1) * Shape::kStageBytes + Shape::kTileBytes + threadIdx.x * 16;
         uint32_t bad = 0;
@@ -781,32 +735,19 @@ __global__ __launch_bounds__(WideShape<DP>::kThreads, 2) void attention_wide_ker
         const bool any = __any(bad != 0);
         if (lane == 0) flags[wave] = any;
         __syncthreads();
+    };
+    auto add_cleaned = [&](int t) TW_INLINE {
         bool infinite = false;
 #pragma unroll
         for (int w = 0; w < Shape::kWaves; ++w) infinite |= flags[w] != 0;
         if (__builtin_expect(__builtin_amdgcn_readfirstlane(infinite), 0)) {
 #pragma unroll 1
-            for (int j = t * Shape::kKeys; j < min((t + 1) * Shape::kKeys, visible); ++j) {
-                const char *const row = v_head + j * p.v_stride;
-                const bool sees = keys.begin + j <= last;
-#pragma unroll
-                for (int b = 0; b < kBlocks; ++b)
-#pragma unroll
-                    for (int g = 0; g < 4; ++g) {
-                        const int col = b * 32 + g * 8 + half * 4;
-                        u32x2 x = {0, 0};
-                        if (col < p.dim) x = *reinterpret_cast<const u32x2 *>(row + col * 2);
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            const uint32_t bits = i & 1 ? x[i >> 1] & 0xffff0000u : x[i >> 1] << 16;
-                            const float v = (bits & 0x7f800000u) == 0x7f800000u ? __uint_as_float(bits) : 0.0f;
-                            o[b][g * 4 + i] += sees ? v : 0.0f;
-                        }
-                    }
-            }
+            for (int j = t * Shape::kKeys; j < min((t + 1) * Shape::kKeys, visible); ++j)
+                add_infinite<32, kBlocks>(o, v_head + j * p.v_stride, p.dim, half, keys.begin + j <= last);
         }
     };
 
+    const bool has_rows = r0 + wave * 32 < list;
     // Between two barriers the next tile comes in, into the other half of the LDS.
     auto turn = [&](int t, auto stage, auto masked) TW_INLINE {
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
@@ -815,8 +756,11 @@ __global__ __launch_bounds__(WideShape<DP>::kThreads, 2) void attention_wide_ker
         if constexpr (decltype(masked)::value) {
             clean_values(t);
             if (!__any(last >= keys.begin + t * Shape::kKeys)) return;
+        } else if (!has_rows) {
+            return;
         }
         compute(t, stage, masked);
+        if constexpr (decltype(masked)::value) add_cleaned(t);
     };
     using Stage0 = std::integral_constant<int, 0>;
     using Stage1 = std::integral_constant<int, 1>;
@@ -892,15 +836,20 @@ __global__ __launch_bounds__(256) void attention_join_kernel(AttentionParams p)
     const float sum = group_sum(empty && l == 0.0f ? 0.0f : f * l, 6);
     const int c0 = lane * 2;
     float a = 0.0f, b = 0.0f;
-    uint64_t live = __ballot(!(empty && l == 0.0f));
-    while (live) {
-        const int c = __builtin_ctzll(live);
-        live &= live - 1;
-        const float w = __shfl(f, c);
-        if (c0 < p.dim) {
-            const float2 x = *reinterpret_cast<const float2 *>(p.part + (c * step + at) * p.dim + c0);
-            a = fmaf(w, x.x, a);
-            b = fmaf(w, x.y, b);
+    const uint64_t live = __ballot(!(empty && l == 0.0f));  // (the others' columns were not put)
+    for (int c = 0; c < p.chunks; c += 8) {  // eight loads under way
+        float2 x[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            x[i] = {0.0f, 0.0f};
+            if (c0 < p.dim && c + i < p.chunks && (live >> (c + i)) & 1)
+                x[i] = *reinterpret_cast<const float2 *>(p.part + ((c + i) * step + at) * p.dim + c0);
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float w = __shfl(f, (c + i) & 63);
+            a = fmaf(w, x[i].x, a);
+            b = fmaf(w, x[i].y, b);
         }
     }
     const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
@@ -936,7 +885,10 @@ static tw_status attention_sizes(const tw_attention_args &a)
 
 // How a call is launched.
 struct AttentionPlan {
-    bool few;       // tiles of 16 rows whose four waves share the keys; otherwise 256 rows, each wave 32 of its own
+    int few;        // blocks of 16 rows of a tile whose four waves share the keys; 0: a wave for each 32 rows of a larger tile
+    int waves;
+    bool streamed;  // few: the keys and values are more than the last-level cache holds
+    int tile_rows;
     int chunks;     // parts of each sequence's keys, joined by a second kernel where there are more than one
     int min_chunk;  // fewest keys of a part but the last
 };
@@ -945,12 +897,22 @@ static AttentionPlan attention_plan(const tw_attention_args &a)
 {
     AttentionPlan plan;
     const int64_t group = a.q_heads / a.kv_heads, list = a.q_rows * group;
-    plan.few = list <= 16 * a.n_seqs;
-    const int64_t tiles = (plan.few ? a.n_seqs : list / 256 + 1) * a.kv_heads;
-    const int64_t keys = a.k_rows / a.n_seqs;
+    // A row for each sequence is a batch of single tokens. (With more, some sequences may have many: the other form has a
+    // workgroup for each of their tiles.)
+    plan.few = a.q_rows > a.n_seqs || group > 32 ? 0 : group > 16 ? 2 : 1;
+    // Four waves, two workgroups to a compute unit, where eight would have no rows: 32 sequences of 4 rows on average, keys of up
+    // to 6K, 64 / 8 heads: 94 us, 112 with eight.
+    plan.waves = plan.few || a.head_dim <= 64 || list <= 128 * a.n_seqs ? 4 : 8;
+    plan.tile_rows = plan.few ? 16 * plan.few : 32 * plan.waves;
+    plan.streamed = a.k_rows * a.kv_heads * a.head_dim * 4 > kLastLevelCacheBytes;
+    // Keys are cut where the tiles are too few for the device. A part's sums are written and read again: those of many rows
+    // are worth one workgroup for each compute unit and no more (512 rows over 8192 keys, 64 / 8 heads: 155 us, for
+    // twice as many 165, for four times 189), those of a single token's rows several.
+    const int64_t tiles = (plan.few ? a.n_seqs : list / plan.tile_rows + 1) * a.kv_heads;
+    const int64_t keys = a.k_rows / a.n_seqs, enough = plan.few ? 512 : 256, wanted = plan.few ? 2048 : 256;
     plan.min_chunk = 512;
     int64_t chunks = 1;
-    if (tiles < 512) chunks = std::min<int64_t>((1024 + tiles - 1) / tiles, (keys + plan.min_chunk - 1) / plan.min_chunk);
+    if (tiles < enough) chunks = std::min((wanted + tiles - 1) / tiles, (keys + plan.min_chunk - 1) / plan.min_chunk);
     plan.chunks = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(chunks, 32)));
     return plan;
 }
@@ -973,22 +935,31 @@ static tw_status launch_attention(void (*kernel)(AttentionParams), std::atomic<i
     return TW_OK;
 }
 
-template <int DP>
-static std::atomic<int> allowed_few[kMaxDevices];
-template <int DP>
-static std::atomic<int> allowed_wide[kMaxDevices];
+template <int DP, int RB, bool STREAMED>
+static tw_status launch_few(const AttentionParams &p, hipStream_t stream)
+{
+    using Shape = FewShape<DP, RB>;
+    static std::atomic<int> allowed[kMaxDevices];
+    return launch_attention(attention_few_kernel<DP, RB, STREAMED>, allowed, Shape::kThreads, Shape::kLds, p, p.n_seqs, stream);
+}
+
+template <int DP, int WAVES>
+static tw_status launch_wide(const AttentionParams &p, hipStream_t stream)
+{
+    using Shape = WideShape<DP, WAVES>;
+    static std::atomic<int> allowed[kMaxDevices];
+    return launch_attention(attention_wide_kernel<DP, WAVES>, allowed, Shape::kThreads, Shape::kLds, p,
+                            p.q_rows * p.group / Shape::kRows + p.n_seqs, stream);
+}
 
 template <int DP>
 static tw_status launch_attention_for(const AttentionParams &p, const AttentionPlan &plan, hipStream_t stream)
 {
-    if (plan.few) {
-        using Shape = AttentionShape<DP, 16, 1, 4, 32, 1>;
-        return launch_attention(attention_kernel<DP, 16, 1, 4, 32, 1>, allowed_few<DP>, Shape::kThreads, Shape::kLds, p, p.n_seqs,
-                                stream);
-    }
-    using Shape = WideShape<DP>;
-    return launch_attention(attention_wide_kernel<DP>, allowed_wide<DP>, Shape::kThreads, Shape::kLds, p,
-                            p.q_rows * p.group / Shape::kRows + p.n_seqs, stream);
+    if (plan.few == 1) return plan.streamed ? launch_few<DP, 1, true>(p, stream) : launch_few<DP, 1, false>(p, stream);
+    if (plan.few == 2) return plan.streamed ? launch_few<DP, 2, true>(p, stream) : launch_few<DP, 2, false>(p, stream);
+    if constexpr (DP == 128)
+        if (plan.waves == 8) return launch_wide<DP, 8>(p, stream);
+    return launch_wide<DP, 4>(p, stream);
 }
 
 }  // namespace tw
@@ -1010,7 +981,7 @@ tw_status tw_attention_plan(const tw_attention_args *args, tw_attention_launch *
     *launch = {};
     if (args->n_seqs == 0 || args->q_rows == 0) return TW_OK;
     const AttentionPlan plan = attention_plan(*args);
-    launch->tile_rows = plan.few ? 16 : args->head_dim > 64 ? WideShape<128>::kRows : WideShape<64>::kRows;
+    launch->tile_rows = plan.tile_rows;
     launch->key_waves = plan.few ? 4 : 1;
     launch->chunks = plan.chunks;
     launch->min_chunk = plan.min_chunk;

@@ -62,6 +62,23 @@ def test_long_keys(tw, q_lens, k_lens, heads, kv_heads, dim):
         check(tw, *inputs(q_lens, k_lens, heads, kv_heads, dim, seed=7), causal=causal, what=str(k_lens))
 
 
+def test_more_keys_than_the_last_level_cache_holds(tw):
+    """Single tokens whose keys and values are streamed past the caches."""
+    q, k, v, qo, ko = inputs([1, 0, 1], [23000, 5, 18001], 16, 16, 128, seed=1)
+    assert k.numel() * 4 > 256 << 20
+    check(tw, q, k, v, qo, ko, what="streamed")
+
+
+def test_forms_of_the_launch(tw):
+    """Each kernel and rule is reached by the sizes of these tests."""
+    forms = {(f.tile_rows, f.key_waves, f.chunks > 1): sizes for sizes in (
+        (1, 1, 1, 8, 1, 128), (1, 1, 20011, 4, 4, 64), (1, 1, 1, 32, 1, 64), (1, 1, 9000, 32, 1, 64), (1, 63, 63, 1, 1, 64),
+        (1, 100, 4100, 16, 2, 64), (2, 1000, 1000, 4, 2, 128), (1, 100, 4100, 16, 2, 128), (4, 100, 4000, 4, 2, 128))
+        for f in (tw.attention_plan(*sizes),)}
+    assert set(forms) == {(16, 4, False), (16, 4, True), (32, 4, False), (32, 4, True), (128, 1, False), (128, 1, True), (256, 1, False),
+                          (256, 1, True)}, forms
+
+
 @pytest.mark.parametrize("q_lens,k_lens", [([1, 1], [40, 2000]), ([150, 3], [150, 90])])
 def test_scores_far_apart_and_scale(tw, q_lens, k_lens):
     # scores of some hundreds: one key has all the weight, and the running maximum changes from tile to tile
