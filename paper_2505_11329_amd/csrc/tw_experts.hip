@@ -13,8 +13,11 @@ namespace tw {
 // pair is the number of pairs of lower experts, plus those of its expert in earlier runs, in earlier waves of its own, and
 // earlier in its wave. Only counts meet between waves, so nothing depends on the order they run in.
 
-static constexpr int kRun = 4096;       // fewest pairs of a workgroup, where there is more than one
+// A workgroup's pairs where there is more than one of them, and the fewest pairs for that (128 experts: 131072 pairs in runs of
+// 1024, 2048, 4096, 8192 take 11.7, 11.0, 13.1, 16.4 us; 4096 pairs take 7.2 us in one run and 9.9 in two, 8192 pairs 10.9 and 9.8 in four).
+static constexpr int kRun = 2048, kManyPairs = 8192;
 static constexpr int kMaxRuns = 256;
+static constexpr int kFewExperts = 512;  // 16 waves' counts fit 64 KiB
 
 struct SortParams {
     const void *ids;
@@ -57,31 +60,51 @@ __device__ __forceinline__ uint64_t same_bucket(int bucket, int bits, uint64_t a
     return same;
 }
 
-template <typename Id>
-__global__ __launch_bounds__(1024) void expert_place_kernel(SortParams p)
+template <typename Id, int WAVES>
+__global__ __launch_bounds__(64 * WAVES) void expert_place_kernel(SortParams p)
 {
-    extern __shared__ int32_t start[];  // [waves x buckets]: counts, then the next place
-    __shared__ int32_t wave_total[16];
-    const int waves = blockDim.x / 64, wave = threadIdx.x / 64, lane = threadIdx.x % 64;
+    constexpr int kThreads = 64 * WAVES;
     const int buckets = p.experts + 1;
-    for (int i = threadIdx.x; i < waves * buckets; i += blockDim.x) start[i] = 0;
-    __syncthreads();
-    const int64_t run_begin = blockIdx.x * p.run, run_end = min(run_begin + p.run, p.pairs);
-    const int64_t part = (p.run / 64 + waves - 1) / waves * 64;
-    const int64_t begin = min(run_begin + wave * part, run_end), end = min(begin + part, run_end);
-    int32_t *const mine = start + wave * buckets;
-    for (int64_t i = begin + lane; i < end; i += 64) atomicAdd(&mine[bucket_of<Id>(p, i)], 1);
+    extern __shared__ int32_t start[];             // [waves x buckets]: counts, then each wave's next places
+    int32_t *const all = start + WAVES * buckets;  // pairs of a bucket in all runs
+    int32_t *const ahead = all + buckets;          // and in the runs before this one
+    __shared__ int32_t wave_total[WAVES];
+    const int wave = threadIdx.x / 64, lane = threadIdx.x % 64;
+    for (int i = threadIdx.x; i < (WAVES + 2) * buckets; i += kThreads) start[i] = 0;
     __syncthreads();
 
-    // each thread has a few neighbouring buckets: their totals, and the pairs of earlier runs
-    const int each = (buckets + blockDim.x - 1) / blockDim.x, first = threadIdx.x * each;
-    int32_t total = 0;
-    for (int e = first; e < min(first + each, buckets); ++e) {
-        if (gridDim.x == 1)
-            for (int w = 0; w < waves; ++w) total += start[w * buckets + e];
-        else
-            for (unsigned r = 0; r < gridDim.x; ++r) total += p.counts[static_cast<int64_t>(r) * buckets + e];
+    const int64_t run_begin = blockIdx.x * p.run, run_end = min(run_begin + p.run, p.pairs);
+    const int64_t part = (p.run / 64 + WAVES - 1) / WAVES * 64;
+    const int64_t begin = min(run_begin + wave * part, run_end), end = min(begin + part, run_end);
+    int32_t *const mine = start + wave * buckets;
+    // (integer sums: the order of these atomics does not show)
+    for (int64_t i = begin + lane; i < end; i += 64) {
+        const int bucket = bucket_of<Id>(p, i);
+        atomicAdd(&mine[bucket], 1);
+        if (gridDim.x == 1) atomicAdd(&all[bucket], 1);
     }
+    if (gridDim.x > 1) {
+        // as many columns of runs side by side as there are threads for
+        const int columns = max(1, kThreads / buckets), runs = gridDim.x, here = blockIdx.x;
+        for (int i = threadIdx.x; i < columns * buckets; i += kThreads) {
+            const int e = i % buckets;
+            int32_t n_all = 0, n_ahead = 0;
+#pragma unroll 8
+            for (int r = i / buckets; r < runs; r += columns) {
+                const int32_t n = p.counts[static_cast<int64_t>(r) * buckets + e];
+                n_all += n;
+                n_ahead += r < here ? n : 0;
+            }
+            atomicAdd(&all[e], n_all);
+            atomicAdd(&ahead[e], n_ahead);
+        }
+    }
+    __syncthreads();
+
+    // each thread has a few neighbouring buckets
+    const int each = (buckets + kThreads - 1) / kThreads, first = threadIdx.x * each;
+    int32_t total = 0;
+    for (int e = first; e < min(first + each, buckets); ++e) total += all[e];
     int32_t upto = total;
     for (int d = 1; d < 64; d <<= 1) {
         const int32_t o = __shfl_up(upto, d);
@@ -90,21 +113,18 @@ __global__ __launch_bounds__(1024) void expert_place_kernel(SortParams p)
     if (lane == 63) wave_total[wave] = upto;
     __syncthreads();
     int32_t base = upto - total;
-    for (int w = 0; w < wave; ++w) base += wave_total[w];
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) base += w < wave ? wave_total[w] : 0;
     for (int e = first; e < min(first + each, buckets); ++e) {
         if (blockIdx.x == 0) p.offsets[e] = base;
-        int32_t at = base;
-        if (gridDim.x > 1)
-            for (unsigned r = 0; r < gridDim.x; ++r) {
-                const int32_t n = p.counts[static_cast<int64_t>(r) * buckets + e];
-                if (r < blockIdx.x) at += n;
-                base += n;
-            }
-        for (int w = 0; w < waves; ++w) {
-            const int32_t n = start[w * buckets + e];
+        int32_t at = base + ahead[e], n[WAVES];
+        base += all[e];
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) n[w] = start[w * buckets + e];
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) {
             start[w * buckets + e] = at;
-            at += n;
-            if (gridDim.x == 1) base += n;
+            at += n[w];
         }
     }
     __syncthreads();
@@ -116,11 +136,11 @@ __global__ __launch_bounds__(1024) void expert_place_kernel(SortParams p)
         const int bucket = has ? bucket_of<Id>(p, i) : 0;
         const uint64_t same = same_bucket(bucket, bits, __ballot(has));
         if (has) {
-            const int ahead = __builtin_popcountll(same & ((uint64_t(1) << lane) - 1));
-            const int32_t place = mine[bucket] + ahead;
+            const int before = __builtin_popcountll(same & ((uint64_t(1) << lane) - 1));
+            const int32_t place = mine[bucket] + before;
             // all lanes of the wave have read before one adds, and it has before the next round reads
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-            if (ahead == 0) mine[bucket] = place + __builtin_popcountll(same);
+            if (before == 0) mine[bucket] = place + __builtin_popcountll(same);
             p.order[place] = static_cast<int32_t>(i);
             p.position[i] = bucket == p.experts ? -1 : place;
         }
@@ -147,9 +167,21 @@ struct RowsParams {
 
 static constexpr int kMost = 8;  // pairs of a token that are worked on at a time
 
+// Experts' rows are read once and not kept in the caches (the gradient of a dispatch, 2531 tokens of 8 rows of 5120: 50 us with
+// ordinary loads, 46 so). Results of more than half of what the last-level cache holds are not kept either (STREAMED; 8101 tokens
+// to 6 places of 4096: 93 us with ordinary stores, 76 so); smaller ones stay for the products that read them next.
+template <bool ONCE>
 __device__ __forceinline__ u32x4 row_piece(const char *base, int64_t row, int pieces, int c)
 {
-    return *reinterpret_cast<const u32x4 *>(base + (row * pieces + c) * 16);
+    const u32x4 *const from = reinterpret_cast<const u32x4 *>(base + (row * pieces + c) * 16);
+    return ONCE ? __builtin_nontemporal_load(from) : *from;
+}
+template <bool STREAMED>
+__device__ __forceinline__ void put_piece(char *base, int64_t row, int pieces, int c, u32x4 v)
+{
+    u32x4 *const to = reinterpret_cast<u32x4 *>(base + (row * pieces + c) * 16);
+    if constexpr (STREAMED) __builtin_nontemporal_store(v, to);
+    else *to = v;
 }
 
 // The places of pairs [k0, k0 + kMost) of a token, -1 for none.
@@ -165,6 +197,7 @@ __device__ __forceinline__ void places(const RowsParams &p, int64_t token, int k
     }
 }
 
+template <bool STREAMED>
 __global__ __launch_bounds__(256) void expert_dispatch_kernel(RowsParams p)
 {
     const int threads = 1 << p.row_log2;
@@ -174,15 +207,15 @@ __global__ __launch_bounds__(256) void expert_dispatch_kernel(RowsParams p)
         int32_t at[kMost];
         places(p, token, k0, at);
         for (int c = threadIdx.x & (threads - 1); c < p.pieces; c += threads) {
-            const u32x4 x = row_piece(p.in, token, p.pieces, c);
+            const u32x4 x = row_piece<false>(p.in, token, p.pieces, c);
 #pragma unroll
             for (int k = 0; k < kMost; ++k)
-                if (at[k] >= 0) *reinterpret_cast<u32x4 *>(p.out + (static_cast<int64_t>(at[k]) * p.pieces + c) * 16) = x;
+                if (at[k] >= 0) put_piece<STREAMED>(p.out, at[k], p.pieces, c, x);
         }
     }
 }
 
-template <bool WEIGHTED>
+template <bool WEIGHTED, bool STREAMED>
 __global__ __launch_bounds__(256) void expert_combine_kernel(RowsParams p)
 {
     const int threads = 1 << p.row_log2;
@@ -196,7 +229,7 @@ __global__ __launch_bounds__(256) void expert_combine_kernel(RowsParams p)
             u32x4 v[kMost] = {};
 #pragma unroll
             for (int k = 0; k < kMost; ++k)
-                if (at[k] >= 0) v[k] = row_piece(p.in, at[k], p.pieces, c);
+                if (at[k] >= 0) v[k] = row_piece<true>(p.in, at[k], p.pieces, c);
 #pragma unroll
             for (int k = 0; k < kMost; ++k) {
                 if (at[k] < 0) continue;
@@ -211,10 +244,11 @@ __global__ __launch_bounds__(256) void expert_combine_kernel(RowsParams p)
                 }
             }
         }
-        *reinterpret_cast<u32x4 *>(p.out + (token * p.pieces + c) * 16) = pack8(sum);
+        put_piece<STREAMED>(p.out, token, p.pieces, c, pack8(sum));
     }
 }
 
+template <bool STREAMED>
 __global__ __launch_bounds__(256) void expert_combine_backward_kernel(RowsParams p)
 {
     __shared__ float wave_dot[4][kMost];
@@ -232,11 +266,11 @@ __global__ __launch_bounds__(256) void expert_combine_backward_kernel(RowsParams
         if (has)
             for (int c = in_row; c < p.pieces; c += threads) {
                 float d[8];
-                unpack8(row_piece(p.in, token, p.pieces, c), d);
+                unpack8(row_piece<false>(p.in, token, p.pieces, c), d);
                 u32x4 v[kMost] = {};
 #pragma unroll
                 for (int k = 0; k < kMost; ++k)
-                    if (at[k] >= 0) v[k] = row_piece(p.y, at[k], p.pieces, c);
+                    if (at[k] >= 0) v[k] = row_piece<true>(p.y, at[k], p.pieces, c);
 #pragma unroll
                 for (int k = 0; k < kMost; ++k) {
                     if (at[k] < 0) continue;
@@ -247,7 +281,7 @@ __global__ __launch_bounds__(256) void expert_combine_backward_kernel(RowsParams
                         dot[k] = fmaf(f[i], d[i], dot[k]);
                         f[i] = w[k] * d[i];
                     }
-                    *reinterpret_cast<u32x4 *>(p.out + (static_cast<int64_t>(at[k]) * p.pieces + c) * 16) = pack8(f);
+                    put_piece<STREAMED>(p.out, at[k], p.pieces, c, pack8(f));
                 }
             }
         // a row's dot products: over its lanes, then over its waves in order
@@ -289,7 +323,7 @@ static tw_status sort_sizes(int64_t N, int top_k, int n_experts)
     return n_experts > TW_MAX_EXPERTS ? TW_ERR_UNSUPPORTED : TW_OK;
 }
 
-static int64_t sort_runs(int64_t pairs) { return std::max<int64_t>(1, std::min<int64_t>(kMaxRuns, pairs / kRun)); }
+static int64_t sort_runs(int64_t pairs) { return pairs < kManyPairs ? 1 : std::min<int64_t>(kMaxRuns, pairs / kRun); }
 
 static tw_status row_sizes(int64_t N, int top_k, int64_t H, int64_t rows)
 {
@@ -300,6 +334,8 @@ static tw_status row_sizes(int64_t N, int top_k, int64_t H, int64_t rows)
 }
 
 static bool aligned4(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
+
+static bool streamed(uint64_t result_bytes) { return result_bytes > static_cast<uint64_t>(kLastLevelCacheBytes / 2); }
 
 static void row_layout(int64_t H, RowsParams *p)
 {
@@ -321,10 +357,12 @@ template <typename Id>
 static tw_status launch_sort(const SortParams &p, int64_t runs, hipStream_t stream)
 {
     const unsigned buckets = static_cast<unsigned>(p.experts + 1);
-    const unsigned threads = p.experts <= 512 ? 1024 : 512;  // (more waves' counts than these do not fit 64 KiB)
     if (runs > 1)
         TW_HIP(launch_kernel(expert_count_kernel<Id>, dim3(static_cast<uint32_t>(runs)), dim3(1024), buckets * 4, stream, p));
-    TW_HIP(launch_kernel(expert_place_kernel<Id>, dim3(static_cast<uint32_t>(runs)), dim3(threads), threads / 64 * buckets * 4, stream, p));
+    if (p.experts <= kFewExperts)
+        TW_HIP(launch_kernel(expert_place_kernel<Id, 16>, dim3(static_cast<uint32_t>(runs)), dim3(1024), 18 * buckets * 4, stream, p));
+    else
+        TW_HIP(launch_kernel(expert_place_kernel<Id, 8>, dim3(static_cast<uint32_t>(runs)), dim3(512), 10 * buckets * 4, stream, p));
     return TW_OK;
 }
 
@@ -396,7 +434,7 @@ tw_status tw_expert_dispatch(const void *x, const int32_t *position, int64_t N, 
     p.rows = rows;
     p.top_k = top_k;
     row_layout(H, &p);
-    return launch_rows(expert_dispatch_kernel, p, stream);
+    return launch_rows(streamed(rows_b) ? expert_dispatch_kernel<true> : expert_dispatch_kernel<false>, p, stream);
 }
 
 tw_status tw_expert_combine(const void *y, int64_t rows, const int32_t *position, const float *weights, int64_t N,
@@ -420,7 +458,9 @@ tw_status tw_expert_combine(const void *y, int64_t rows, const int32_t *position
     p.rows = rows;
     p.top_k = top_k;
     row_layout(H, &p);
-    return launch_rows(weights ? expert_combine_kernel<true> : expert_combine_kernel<false>, p, stream);
+    if (streamed(tokens_b))
+        return launch_rows(weights ? expert_combine_kernel<true, true> : expert_combine_kernel<false, true>, p, stream);
+    return launch_rows(weights ? expert_combine_kernel<true, false> : expert_combine_kernel<false, false>, p, stream);
 }
 
 tw_status tw_expert_combine_backward(const void *dout, const void *y, int64_t rows, const int32_t *position,
@@ -454,7 +494,7 @@ tw_status tw_expert_combine_backward(const void *dout, const void *y, int64_t ro
     p.rows = rows;
     p.top_k = top_k;
     row_layout(H, &p);
-    return launch_rows(expert_combine_backward_kernel, p, stream);
+    return launch_rows(streamed(rows_b) ? expert_combine_backward_kernel<true> : expert_combine_backward_kernel<false>, p, stream);
 }
 
 }  // extern "C"

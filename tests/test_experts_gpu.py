@@ -71,6 +71,16 @@ def test_combine(tw, N, K, E, H, weighted):
     R.assert_close(tw.expert_combine(y, position, w), want, tol, "combine")
 
 
+@pytest.mark.parametrize("weighted", [True, False])
+def test_combine_into_more_than_the_caches_keep(tw, weighted):
+    N, K, H = 4400, 2, 16384
+    position, _, y, w = routed(N, K, 8, H)
+    assert N * H * 2 > 128 << 20
+    w = w if weighted else None
+    want, tol = R.combine(y, position, w)
+    R.assert_close(tw.expert_combine(y, position, w), want, tol, "combine")
+
+
 @pytest.mark.parametrize("N,K,E,H", SIZES)
 def test_combine_backward(tw, N, K, E, H):
     position, dout, y, w = routed(N, K, E, H)
