@@ -586,11 +586,11 @@ tw_status tw_weave_tune(const tw_layer_args *layer, int64_t multiple, const int6
  * the call (tw_attention_plan): calls of the same form, e.g. one batch and the same batch split in two
  * large halves, give the same bits.
  * Errors: TW_ERR_NULL, TW_ERR_SHAPE (sizes; workspace_bytes too few), TW_ERR_ALIGN, TW_ERR_ALIAS,
- * TW_ERR_UNSUPPORTED (head_dim, strides, counts beyond the above).
+ * TW_ERR_UNSUPPORTED (head_dim, strides, counts beyond the above, more than 2^23 tiles of rows and keys).
  */
 #define TW_MAX_HEAD_DIM 128
 #define TW_MAX_HEADS 1024
-#define TW_MAX_SEQS (1 << 20)
+#define TW_MAX_SEQS (1 << 14)
 #define TW_MAX_ROW_STRIDE (1 << 22)
 
 typedef struct tw_attention_args {

@@ -250,252 +250,6 @@ __device__ __forceinline__ i32x4 buffer_of(const char *p, uint32_t bytes)
     return {static_cast<int>(a), static_cast<int>((a >> 32) & 0xffff), static_cast<int>(bytes), 0x00020000};
 }
 
-// Few rows to a sequence, single tokens as a rule: tiles of 16 or 32 rows of a group's list, whose keys four waves share. Bound
-// by what comes from memory. Each wave has keys of its own, 32 at a time, and a place in the LDS for them: the next ones are
-// asked for as soon as a product has read the ones before, and nothing but the result ties the waves to each other. Two
-// workgroups to a compute unit keep up to 128 KB on their way.
-template <int DP, int RB>
-struct FewShape {
-    static constexpr int kWaves = 4, kThreads = 64 * kWaves, kRows = 16 * RB, kKeys = 32;
-    static constexpr int kRowBytes = DP * 2, kTileBytes = kKeys * kRowBytes;
-    static constexpr int kPieces = DP / 8, kLoadRows = 64 / kPieces, kLoads = kKeys / kLoadRows;
-    static constexpr int kJoinBytes = kWaves * kRows * (DP + 2) * 4;
-    static constexpr int kLds = kWaves * 2 * kTileBytes > kJoinBytes ? kWaves * 2 * kTileBytes : kJoinBytes;
-};
-
-template <int N>
-__device__ __forceinline__ void all_but_landed()  // the N newest loads may be under way
-{
-    asm volatile("s_waitcnt vmcnt(%0)" : : "n"(N) : "memory");
-}
-__device__ __forceinline__ void lds_read() { asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory"); }
-
-template <int DP, int RB, bool STREAMED>
-__global__ __launch_bounds__(256, 2) void attention_few_kernel(AttentionParams p)
-{
-    using Shape = FewShape<DP, RB>;
-    constexpr int kSteps = DP / 32, kBlocks = DP / 16;
-    extern __shared__ __align__(16) char lds[];
-    const int lane = threadIdx.x & 63, part = lane / 16, row_lane = lane % 16;
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-
-    const int kv_head = blockIdx.x % p.kv_heads;
-    const int rest = blockIdx.x / p.kv_heads;
-    const int chunk = rest % p.chunks;
-    const Sequence s = sequence(p, rest / p.chunks);
-    const int list = s.q_len * p.group;
-    const Keys keys = chunk_keys(p, s.k_len, chunk);
-    const int past = s.k_len - s.q_len;
-
-    // where this lane's 16 bytes of a load come from: the piece that lies in its place of the swizzled tile
-    const int load_row = lane / Shape::kPieces, place = lane % Shape::kPieces;
-    const char *const k_head = p.k + s.k0 * p.k_stride + static_cast<int64_t>(kv_head) * p.dim * 2;
-    const char *const v_head = p.v + s.k0 * p.v_stride + static_cast<int64_t>(kv_head) * p.dim * 2;
-    char *const mine = lds + wave * 2 * Shape::kTileBytes;
-    const uint32_t k_at = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((lds_char_ptr_t)mine)), v_at = k_at + Shape::kTileBytes;
-
-    // fragments' places
-    const int i16 = lane & 15, v_row = 4 * part + (i16 >> 2);
-    const char *k_frag[kSteps], *v_frag[kBlocks];
-#pragma unroll
-    for (int x = 0; x < kSteps; ++x) k_frag[x] = mine + row_lane * Shape::kRowBytes + (((4 * x + part) ^ k_swizzle<DP>(row_lane)) << 4);
-#pragma unroll
-    for (int b = 0; b < kBlocks; ++b)
-        v_frag[b] = mine + Shape::kTileBytes + v_row * Shape::kRowBytes + (((2 * b + ((i16 & 3) >> 1)) ^ v_swizzle<DP>(v_row)) << 4) + (i16 & 1) * 8;
-
-    for (int r0 = 0; r0 < list; r0 += Shape::kRows) {  // one tile as a rule
-        const int last_pos = list_pos(p, min(r0 + Shape::kRows, list) - 1);
-        const int end = min(keys.end, p.causal ? last_pos + past + 1 : s.k_len);
-        const int first_last = min(keys.end - 1, p.causal ? list_pos(p, r0) + past : s.k_len - 1);  // the last key that the first row sees
-
-        auto load_rows = [&](const char *base, int64_t stride, int key0, uint32_t to, auto swizzle) TW_INLINE {
-            const int rows = min(Shape::kKeys, end - key0);
-            const i32x4 rsrc = buffer_of(base + key0 * stride, rows > 0 ? static_cast<uint32_t>((rows - 1) * stride + p.dim * 2) : 0);
-#pragma unroll
-            for (int i = 0; i < Shape::kLoads; ++i) {
-                const int col = (place ^ swizzle(i * Shape::kLoadRows + load_row)) * 8;
-                load_to_lds<STREAMED>(rsrc, col < p.dim ? static_cast<uint32_t>(load_row * stride + col * 2) : kPastTensor,
-                                      static_cast<uint32_t>(i * Shape::kLoadRows * stride), to + i * 1024);
-            }
-        };
-        auto load_keys = [&](int key0) TW_INLINE { load_rows(k_head, p.k_stride, key0, k_at, [](int row) { return k_swizzle<DP>(row); }); };
-        auto load_values = [&](int key0) TW_INLINE { load_rows(v_head, p.v_stride, key0, v_at, [](int row) { return v_swizzle<DP>(row); }); };
-
-        int key0 = keys.begin + wave * Shape::kKeys;
-        constexpr int kOn = Shape::kWaves * Shape::kKeys;
-        load_keys(key0);
-        load_values(key0);
-        int last[RB];  // keys [0, last] are visible to this lane's rows
-        bf16x8 qf[RB][kSteps];
-        f32x4 o[RB][kBlocks] = {};
-        float m[RB], l[RB];
-#pragma unroll
-        for (int rb = 0; rb < RB; ++rb) {
-            const int r = r0 + rb * 16 + row_lane, pos = list_pos(p, r), head = kv_head * p.group + r - pos * p.group;
-            last[rb] = r < list ? min(p.causal ? pos + past : s.k_len - 1, keys.end - 1) : -1;
-            m[rb] = kMinusInf;
-            l[rb] = 0.0f;
-#pragma unroll
-            for (int x = 0; x < kSteps; ++x) {
-                u32x4 q = {0, 0, 0, 0};
-                const int col = x * 32 + part * 8;
-                if (r < list && col < p.dim)
-                    q = *reinterpret_cast<const u32x4 *>(p.q + (s.q0 + pos) * p.q_stride + (static_cast<int64_t>(head) * p.dim + col) * 2);
-                qf[rb][x] = __builtin_bit_cast(bf16x8, q);
-            }
-        }
-        for (; key0 < end; key0 += kOn) {
-            f32x4 sc[RB][2] = {};
-            all_but_landed<Shape::kLoads>();
-#pragma unroll
-            for (int x = 0; x < kSteps; ++x)
-#pragma unroll
-                for (int n = 0; n < 2; ++n) {
-                    const bf16x8 kf = *reinterpret_cast<const bf16x8 *>(k_frag[x] + n * 16 * Shape::kRowBytes);
-#pragma unroll
-                    for (int rb = 0; rb < RB; ++rb) sc[rb][n] = Mfma<16>::run(kf, qf[rb][x], sc[rb][n]);
-                }
-            lds_read();
-            load_keys(key0 + kOn);  // (past the end: no bytes, but as many loads to wait for)
-            const bool masked = first_last < key0 + Shape::kKeys - 1;
-            if (masked) {
-#pragma unroll
-                for (int rb = 0; rb < RB; ++rb) {
-                    const int seen = last[rb] - key0 - 4 * part;
-#pragma unroll
-                    for (int n = 0; n < 2; ++n)
-#pragma unroll
-                        for (int i = 0; i < 4; ++i)
-                            if (n * 16 + i > seen) sc[rb][n][i] = kMinusInf;
-                }
-            }
-            u32x4 pf[RB];
-#pragma unroll
-            for (int rb = 0; rb < RB; ++rb) {
-                const float alpha = softmax_step<16>(sc[rb], p.c, &m[rb], &l[rb]);
-                if (__any(alpha != 1.0f)) {
-#pragma unroll
-                    for (int b = 0; b < kBlocks; ++b) o[rb][b] *= alpha;
-                }
-                pf[rb] = {pack_bf16x2(sc[rb][0][0], sc[rb][0][1]), pack_bf16x2(sc[rb][0][2], sc[rb][0][3]),
-                          pack_bf16x2(sc[rb][1][0], sc[rb][1][1]), pack_bf16x2(sc[rb][1][2], sc[rb][1][3])};
-            }
-            all_but_landed<Shape::kLoads>();
-            if (masked) {
-                // Inf and NaN of hidden keys must not meet a p of zero: zeros in their place, and the rows that see them get
-                // them added (p > 0 times one of them is the same)
-                uint32_t bad = 0;
-#pragma unroll
-                for (int i = 0; i < Shape::kLoads; ++i) {
-                    u32x4 *const x = reinterpret_cast<u32x4 *>(mine + Shape::kTileBytes + i * 1024 + lane * 16);
-                    u32x4 v = *x;
-                    uint32_t here = 0;
-#pragma unroll
-                    for (int w = 0; w < 4; ++w) {
-                        here |= infinite_bf16x2(v[w]);
-                        v[w] = finite_bf16x2(v[w]);
-                    }
-                    if (here) *x = v;
-                    bad |= here;
-                }
-                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-                if (__builtin_expect(__any(bad != 0), 0)) {
-#pragma unroll 1
-                    for (int j = key0; j < min(key0 + Shape::kKeys, end); ++j)
-#pragma unroll
-                        for (int rb = 0; rb < RB; ++rb) add_infinite<16, kBlocks>(o[rb], v_head + j * p.v_stride, p.dim, part, j <= last[rb]);
-                }
-            }
-#pragma unroll
-            for (int b = 0; b < kBlocks; ++b) {
-                u32x4 vf;
-#pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    const u32x2 x = __builtin_bit_cast(
-                        u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4_ptr_t)(v_frag[b] + e * 16 * Shape::kRowBytes)));
-                    vf[2 * e] = x[0];
-                    vf[2 * e + 1] = x[1];
-                }
-#pragma unroll
-                for (int rb = 0; rb < RB; ++rb)
-                    o[rb][b] = Mfma<16>::run(__builtin_bit_cast(bf16x8, vf), __builtin_bit_cast(bf16x8, pf[rb]), o[rb][b]);
-            }
-            lds_read();
-            load_values(key0 + kOn);
-        }
-
-        // the waves' maxima, sums and sums of v pass through the LDS and are joined in the order of the waves, by sixteen
-        // threads to a row
-        all_but_landed<0>();
-        __syncthreads();
-        float *const sums = reinterpret_cast<float *>(lds);
-        float *const ml = sums + Shape::kWaves * Shape::kRows * DP;
-#pragma unroll
-        for (int rb = 0; rb < RB; ++rb) {
-            const int slot = wave * Shape::kRows + rb * 16 + row_lane;
-            const float sum = row_sum<16>(l[rb]);
-#pragma unroll
-            for (int b = 0; b < kBlocks; ++b) *reinterpret_cast<f32x4 *>(sums + slot * DP + ((b * 4 + part) ^ (row_lane & 7)) * 4) = o[rb][b];
-            if (part == 0) {
-                ml[slot * 2] = m[rb];
-                ml[slot * 2 + 1] = sum;
-            }
-        }
-        __syncthreads();
-        constexpr int kFours = DP / 64;  // of a thread's columns
-#pragma unroll
-        for (int rb = 0; rb < RB; ++rb) {
-            const int jr = rb * 16 + (threadIdx.x >> 4), j16 = threadIdx.x & 15, r = r0 + jr;
-            if (r >= list) continue;
-            float top = kMinusInf, sum = 0.0f;
-#pragma unroll
-            for (int w = 0; w < Shape::kWaves; ++w) top = fmaxf(top, ml[(w * Shape::kRows + jr) * 2]);
-            const float top_use = top == kMinusInf ? 0.0f : top;
-            f32x4 x[kFours] = {};
-#pragma unroll
-            for (int w = 0; w < Shape::kWaves; ++w) {
-                const int from = w * Shape::kRows + jr;
-                const float f = __builtin_amdgcn_exp2f(ml[from * 2] - top_use);
-                sum += f * ml[from * 2 + 1];
-#pragma unroll
-                for (int b = 0; b < kFours; ++b)
-                    x[b] += f * *reinterpret_cast<const f32x4 *>(sums + from * DP + ((b * 16 + j16) ^ (jr & 7)) * 4);
-            }
-            const int pos = list_pos(p, r), head = kv_head * p.group + r - pos * p.group;
-            put_row(p, chunk, (s.q0 + pos) * p.q_heads + head, top, sum, j16 == 0);
-            // a row that sees no key has a sum of 0
-            const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-            // (a chunk of no keys has no columns to put: the sum of 0 says so)
-            if (p.chunks == 1 || keys.begin < keys.end) {
-#pragma unroll
-                for (int b = 0; b < kFours; ++b) put4(p, chunk, s.q0 + pos, head, (b * 16 + j16) * 4, x[b], inv);
-            }
-        }
-        __syncthreads();
-    }
-}
-
-// A batch of many rows: 32 rows of a group's list to a wave, and tiles of 64 keys that come straight into the LDS while the
-// tile before is worked on.
-//
-// 128 columns leave room for two waves of a SIMD. Eight that share their keys are faster where there are rows enough (4096 rows of a
-// 16384-token prompt, 64 / 8 heads: 1.64 ms; two workgroups of four: 1.79). 64 columns leave room for three workgroups of four
-// (8192 tokens, 32 heads: 305 us; two of eight: 322).
-template <int DP, int WAVES>
-struct WideShape {
-    static constexpr int kWaves = WAVES;
-    static constexpr int kThreads = 64 * kWaves, kRows = 32 * kWaves, kKeys = 64;
-    static constexpr int kRowBytes = DP * 2, kTileBytes = kKeys * kRowBytes;
-    static constexpr int kPieces = DP / 8;
-    static constexpr int kLoads = kTileBytes / (16 * kThreads);  // of 16 bytes to a lane, for K or V of a tile
-    static constexpr int kLoadRows = 64 / kPieces;               // rows of a wave's load
-    static constexpr int kStageBytes = 2 * kTileBytes;           // K, V
-    // The rows of q pass through the second stage before its first tile comes, or a place of their own if they are too many;
-    // the results pass through the LDS in the end.
-    static constexpr int kQBytes = kRows * kRowBytes, kQAt = kQBytes <= kStageBytes ? kStageBytes : 2 * kStageBytes;
-    static constexpr int kLds = kQAt + (kQBytes > kStageBytes ? kQBytes : kStageBytes);
-};
-
 // Sum over this lane and those before it.
 __device__ __forceinline__ int sum_upto(int v)
 {
@@ -574,6 +328,264 @@ __device__ __forceinline__ Place find_place(const AttentionParams &p, int i)
     }
     return at;
 }
+
+// Whether every sequence has one query row, but for empty ones behind all others: the i-th tile is then the i-th sequence's.
+__device__ __forceinline__ bool single_tokens(const AttentionParams &p)
+{
+    const int lane = threadIdx.x & 63, first = p.q_offsets[0], rows = p.q_offsets[p.n_seqs] - first;
+    bool single = true;
+#pragma unroll 8
+    for (int b = lane; b < p.n_seqs; b += 64) single &= p.q_offsets[b] - first == min(b, rows);
+    return __all(single);
+}
+
+// Few rows to a sequence, single tokens as a rule: tiles of 16 or 32 rows of a group's list, whose keys four waves share. Bound
+// by what comes from memory. Each wave has keys of its own, 32 at a time, and a place in the LDS for them: the next ones are
+// asked for as soon as a product has read the ones before, and nothing but the result ties the waves to each other. Two
+// workgroups to a compute unit keep up to 128 KB on their way. Each key is read once, and not kept in the caches: 48 tokens over
+// 6000 keys, 64 / 8 heads, 115 us, 131 if kept; 4 tokens over 8192 keys 19.3, 21.1.
+template <int DP, int RB>
+struct FewShape {
+    static constexpr int kWaves = 4, kThreads = 64 * kWaves, kRows = 16 * RB, kKeys = 32;
+    static constexpr int kRowBytes = DP * 2, kTileBytes = kKeys * kRowBytes;
+    static constexpr int kPieces = DP / 8, kLoadRows = 64 / kPieces, kLoads = kKeys / kLoadRows;
+    static constexpr int kJoinBytes = kWaves * kRows * (DP + 2) * 4;
+    static constexpr int kLds = kWaves * 2 * kTileBytes > kJoinBytes ? kWaves * 2 * kTileBytes : kJoinBytes;
+};
+
+template <int N>
+__device__ __forceinline__ void all_but_landed()  // the N newest loads may be under way
+{
+    asm volatile("s_waitcnt vmcnt(%0)" : : "n"(N) : "memory");
+}
+__device__ __forceinline__ void lds_read() { asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory"); }
+
+template <int DP, int RB>
+__global__ __launch_bounds__(256, 2) void attention_few_kernel(AttentionParams p)
+{
+    using Shape = FewShape<DP, RB>;
+    constexpr int kSteps = DP / 32, kBlocks = DP / 16;
+    extern __shared__ __align__(16) char lds[];
+    const int lane = threadIdx.x & 63, part = lane / 16, row_lane = lane % 16;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+
+    const int kv_head = blockIdx.x % p.kv_heads;
+    const int rest = blockIdx.x / p.kv_heads;
+    const int chunk = rest % p.chunks;
+    Place at = {};
+    if (single_tokens(p)) at.s = sequence(p, rest / p.chunks);
+    else at = find_place<Shape::kRows>(p, rest / p.chunks);
+    const Sequence &s = at.s;
+    const int list = s.q_len * p.group, r0 = at.tile * Shape::kRows;
+    if (r0 >= list) return;  // (no tile is left for this workgroup)
+    const Keys keys = chunk_keys(p, s.k_len, chunk);
+    const int past = s.k_len - s.q_len;
+
+    // where this lane's 16 bytes of a load come from: the piece that lies in its place of the swizzled tile
+    const int load_row = lane / Shape::kPieces, place = lane % Shape::kPieces;
+    const char *const k_head = p.k + s.k0 * p.k_stride + static_cast<int64_t>(kv_head) * p.dim * 2;
+    const char *const v_head = p.v + s.k0 * p.v_stride + static_cast<int64_t>(kv_head) * p.dim * 2;
+    char *const mine = lds + wave * 2 * Shape::kTileBytes;
+    const uint32_t k_at = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((lds_char_ptr_t)mine)), v_at = k_at + Shape::kTileBytes;
+
+    // fragments' places
+    const int i16 = lane & 15, v_row = 4 * part + (i16 >> 2);
+    const char *k_frag[kSteps], *v_frag[kBlocks];
+#pragma unroll
+    for (int x = 0; x < kSteps; ++x) k_frag[x] = mine + row_lane * Shape::kRowBytes + (((4 * x + part) ^ k_swizzle<DP>(row_lane)) << 4);
+#pragma unroll
+    for (int b = 0; b < kBlocks; ++b)
+        v_frag[b] = mine + Shape::kTileBytes + v_row * Shape::kRowBytes + (((2 * b + ((i16 & 3) >> 1)) ^ v_swizzle<DP>(v_row)) << 4) + (i16 & 1) * 8;
+
+    const int last_pos = list_pos(p, min(r0 + Shape::kRows, list) - 1);
+    const int end = min(keys.end, p.causal ? last_pos + past + 1 : s.k_len);
+    const int first_last = min(keys.end - 1, p.causal ? list_pos(p, r0) + past : s.k_len - 1);  // the last key that the first row sees
+
+    auto load_rows = [&](const char *base, int64_t stride, int key0, uint32_t to, auto swizzle) TW_INLINE {
+        const int rows = min(Shape::kKeys, end - key0);
+        const i32x4 rsrc = buffer_of(base + key0 * stride, rows > 0 ? static_cast<uint32_t>((rows - 1) * stride + p.dim * 2) : 0);
+#pragma unroll
+        for (int i = 0; i < Shape::kLoads; ++i) {
+            const int col = (place ^ swizzle(i * Shape::kLoadRows + load_row)) * 8;
+            load_to_lds<true>(rsrc, col < p.dim ? static_cast<uint32_t>(load_row * stride + col * 2) : kPastTensor,
+                                  static_cast<uint32_t>(i * Shape::kLoadRows * stride), to + i * 1024);
+        }
+    };
+    auto load_keys = [&](int key0) TW_INLINE { load_rows(k_head, p.k_stride, key0, k_at, [](int row) { return k_swizzle<DP>(row); }); };
+    auto load_values = [&](int key0) TW_INLINE { load_rows(v_head, p.v_stride, key0, v_at, [](int row) { return v_swizzle<DP>(row); }); };
+
+    int key0 = keys.begin + wave * Shape::kKeys;
+    constexpr int kOn = Shape::kWaves * Shape::kKeys;
+    load_keys(key0);
+    load_values(key0);
+    int last[RB];  // keys [0, last] are visible to this lane's rows
+    bf16x8 qf[RB][kSteps];
+    f32x4 o[RB][kBlocks] = {};
+    float m[RB], l[RB];
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) {
+        const int r = r0 + rb * 16 + row_lane, pos = list_pos(p, r), head = kv_head * p.group + r - pos * p.group;
+        last[rb] = r < list ? min(p.causal ? pos + past : s.k_len - 1, keys.end - 1) : -1;
+        m[rb] = kMinusInf;
+        l[rb] = 0.0f;
+#pragma unroll
+        for (int x = 0; x < kSteps; ++x) {
+            u32x4 q = {0, 0, 0, 0};
+            const int col = x * 32 + part * 8;
+            if (r < list && col < p.dim)
+                q = *reinterpret_cast<const u32x4 *>(p.q + (s.q0 + pos) * p.q_stride + (static_cast<int64_t>(head) * p.dim + col) * 2);
+            qf[rb][x] = __builtin_bit_cast(bf16x8, q);
+        }
+    }
+    for (; key0 < end; key0 += kOn) {
+        f32x4 sc[RB][2] = {};
+        all_but_landed<Shape::kLoads>();
+#pragma unroll
+        for (int x = 0; x < kSteps; ++x)
+#pragma unroll
+            for (int n = 0; n < 2; ++n) {
+                const bf16x8 kf = *reinterpret_cast<const bf16x8 *>(k_frag[x] + n * 16 * Shape::kRowBytes);
+#pragma unroll
+                for (int rb = 0; rb < RB; ++rb) sc[rb][n] = Mfma<16>::run(kf, qf[rb][x], sc[rb][n]);
+            }
+        lds_read();
+        load_keys(key0 + kOn);  // (past the end: no bytes, but as many loads to wait for)
+        const bool masked = first_last < key0 + Shape::kKeys - 1;
+        if (masked) {
+#pragma unroll
+            for (int rb = 0; rb < RB; ++rb) {
+                const int seen = last[rb] - key0 - 4 * part;
+#pragma unroll
+                for (int n = 0; n < 2; ++n)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if (n * 16 + i > seen) sc[rb][n][i] = kMinusInf;
+            }
+        }
+        u32x4 pf[RB];
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb) {
+            const float alpha = softmax_step<16>(sc[rb], p.c, &m[rb], &l[rb]);
+            if (__any(alpha != 1.0f)) {
+#pragma unroll
+                for (int b = 0; b < kBlocks; ++b) o[rb][b] *= alpha;
+            }
+            pf[rb] = {pack_bf16x2(sc[rb][0][0], sc[rb][0][1]), pack_bf16x2(sc[rb][0][2], sc[rb][0][3]),
+                      pack_bf16x2(sc[rb][1][0], sc[rb][1][1]), pack_bf16x2(sc[rb][1][2], sc[rb][1][3])};
+        }
+        all_but_landed<Shape::kLoads>();
+        if (masked) {
+            // Inf and NaN of hidden keys must not meet a p of zero: zeros in their place, and the rows that see them get
+            // them added (p > 0 times one of them is the same)
+            uint32_t bad = 0;
+#pragma unroll
+            for (int i = 0; i < Shape::kLoads; ++i) {
+                u32x4 *const x = reinterpret_cast<u32x4 *>(mine + Shape::kTileBytes + i * 1024 + lane * 16);
+                u32x4 v = *x;
+                uint32_t here = 0;
+#pragma unroll
+                for (int w = 0; w < 4; ++w) {
+                    here |= infinite_bf16x2(v[w]);
+                    v[w] = finite_bf16x2(v[w]);
+                }
+                if (here) *x = v;
+                bad |= here;
+            }
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            if (__builtin_expect(__any(bad != 0), 0)) {
+#pragma unroll 1
+                for (int j = key0; j < min(key0 + Shape::kKeys, end); ++j)
+#pragma unroll
+                    for (int rb = 0; rb < RB; ++rb) add_infinite<16, kBlocks>(o[rb], v_head + j * p.v_stride, p.dim, part, j <= last[rb]);
+            }
+        }
+#pragma unroll
+        for (int b = 0; b < kBlocks; ++b) {
+            u32x4 vf;
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const u32x2 x = __builtin_bit_cast(
+                    u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4_ptr_t)(v_frag[b] + e * 16 * Shape::kRowBytes)));
+                vf[2 * e] = x[0];
+                vf[2 * e + 1] = x[1];
+            }
+#pragma unroll
+            for (int rb = 0; rb < RB; ++rb)
+                o[rb][b] = Mfma<16>::run(__builtin_bit_cast(bf16x8, vf), __builtin_bit_cast(bf16x8, pf[rb]), o[rb][b]);
+        }
+        lds_read();
+        load_values(key0 + kOn);
+    }
+
+    // the waves' maxima, sums and sums of v pass through the LDS and are joined in the order of the waves, by sixteen
+    // threads to a row
+    all_but_landed<0>();
+    __syncthreads();
+    float *const sums = reinterpret_cast<float *>(lds);
+    float *const ml = sums + Shape::kWaves * Shape::kRows * DP;
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) {
+        const int slot = wave * Shape::kRows + rb * 16 + row_lane;
+        const float sum = row_sum<16>(l[rb]);
+#pragma unroll
+        for (int b = 0; b < kBlocks; ++b) *reinterpret_cast<f32x4 *>(sums + slot * DP + ((b * 4 + part) ^ (row_lane & 7)) * 4) = o[rb][b];
+        if (part == 0) {
+            ml[slot * 2] = m[rb];
+            ml[slot * 2 + 1] = sum;
+        }
+    }
+    __syncthreads();
+    constexpr int kFours = DP / 64;  // of a thread's columns
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) {
+        const int jr = rb * 16 + (threadIdx.x >> 4), j16 = threadIdx.x & 15, r = r0 + jr;
+        if (r >= list) continue;
+        float top = kMinusInf, sum = 0.0f;
+#pragma unroll
+        for (int w = 0; w < Shape::kWaves; ++w) top = fmaxf(top, ml[(w * Shape::kRows + jr) * 2]);
+        const float top_use = top == kMinusInf ? 0.0f : top;
+        f32x4 x[kFours] = {};
+#pragma unroll
+        for (int w = 0; w < Shape::kWaves; ++w) {
+            const int from = w * Shape::kRows + jr;
+            const float f = __builtin_amdgcn_exp2f(ml[from * 2] - top_use);
+            sum += f * ml[from * 2 + 1];
+#pragma unroll
+            for (int b = 0; b < kFours; ++b)
+                x[b] += f * *reinterpret_cast<const f32x4 *>(sums + from * DP + ((b * 16 + j16) ^ (jr & 7)) * 4);
+        }
+        const int pos = list_pos(p, r), head = kv_head * p.group + r - pos * p.group;
+        put_row(p, chunk, (s.q0 + pos) * p.q_heads + head, top, sum, j16 == 0);
+        // a row that sees no key has a sum of 0
+        const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+        // (a chunk of no keys has no columns to put: the sum of 0 says so)
+        if (p.chunks == 1 || keys.begin < keys.end) {
+#pragma unroll
+            for (int b = 0; b < kFours; ++b) put4(p, chunk, s.q0 + pos, head, (b * 16 + j16) * 4, x[b], inv);
+        }
+    }
+}
+
+// A batch of many rows: 32 rows of a group's list to a wave, and tiles of 64 keys that come straight into the LDS while the
+// tile before is worked on.
+//
+// 128 columns leave room for two waves of a SIMD. Eight that share their keys are faster where there are rows enough (4096 rows of a
+// 16384-token prompt, 64 / 8 heads: 1.64 ms; two workgroups of four: 1.79). 64 columns leave room for three workgroups of four
+// (8192 tokens, 32 heads: 305 us; two of eight: 322).
+template <int DP, int WAVES>
+struct WideShape {
+    static constexpr int kWaves = WAVES;
+    static constexpr int kThreads = 64 * kWaves, kRows = 32 * kWaves, kKeys = 64;
+    static constexpr int kRowBytes = DP * 2, kTileBytes = kKeys * kRowBytes;
+    static constexpr int kPieces = DP / 8;
+    static constexpr int kLoads = kTileBytes / (16 * kThreads);  // of 16 bytes to a lane, for K or V of a tile
+    static constexpr int kLoadRows = 64 / kPieces;               // rows of a wave's load
+    static constexpr int kStageBytes = 2 * kTileBytes;           // K, V
+    // The rows of q pass through the second stage before its first tile comes, or a place of their own if they are too many;
+    // the results pass through the LDS in the end.
+    static constexpr int kQBytes = kRows * kRowBytes, kQAt = kQBytes <= kStageBytes ? kStageBytes : 2 * kStageBytes;
+    static constexpr int kLds = kQAt + (kQBytes > kStageBytes ? kQBytes : kStageBytes);
+};
 
 template <int DP, int WAVES>
 __global__ __launch_bounds__(64 * WAVES, 2) void attention_wide_kernel(AttentionParams p)
@@ -883,28 +895,12 @@ static uint64_t span(int64_t rows, int64_t stride, int64_t width)
     return rows == 0 ? 0 : (static_cast<uint64_t>(rows - 1) * stride + width) * 2u;
 }
 
-static tw_status attention_sizes(const tw_attention_args &a)
-{
-    if (a.n_seqs < 0 || a.q_rows < 0 || a.k_rows < 0 || a.q_heads < 1 || a.kv_heads < 1 || a.head_dim < 1) return TW_ERR_SHAPE;
-    if (a.q_heads % a.kv_heads != 0) return TW_ERR_SHAPE;
-    if (!(a.scale > 0.0f) || !(a.scale <= 3.402823466e+38f)) return TW_ERR_SHAPE;
-    if (a.head_dim % 8 != 0 || a.head_dim > TW_MAX_HEAD_DIM) return TW_ERR_UNSUPPORTED;
-    if (a.q_heads > TW_MAX_HEADS || a.n_seqs > TW_MAX_SEQS) return TW_ERR_UNSUPPORTED;
-    const int64_t wq = static_cast<int64_t>(a.q_heads) * a.head_dim, wk = static_cast<int64_t>(a.kv_heads) * a.head_dim;
-    if (a.q_stride < wq || a.out_stride < wq || a.k_stride < wk || a.v_stride < wk) return TW_ERR_SHAPE;
-    for (const int64_t s : {a.q_stride, a.k_stride, a.v_stride, a.out_stride})
-        if (s % 8 != 0 || s > TW_MAX_ROW_STRIDE) return TW_ERR_UNSUPPORTED;
-    // offsets are 32-bit, and so are the places in a group's list of rows
-    if (a.q_rows * (a.q_heads / a.kv_heads) > INT32_MAX - 1024 || a.q_rows > INT32_MAX - 1024 || a.k_rows > INT32_MAX - 1024)
-        return TW_ERR_UNSUPPORTED;
-    return TW_OK;
-}
+static constexpr int kMostChunks = 32;  // a lane each in the kernel that joins them
 
 // How a call is launched.
 struct AttentionPlan {
     int few;        // blocks of 16 rows of a tile whose four waves share the keys; 0: a wave for each 32 rows of a larger tile
     int waves;
-    bool streamed;  // few: the keys and values are more than the last-level cache holds
     int tile_rows;
     int chunks;     // parts of each sequence's keys, joined by a second kernel where there are more than one
     int min_chunk;  // fewest keys of a part but the last
@@ -921,17 +917,62 @@ static AttentionPlan attention_plan(const tw_attention_args &a)
     // to 6K, 64 / 8 heads: 94 us, 112 with eight.
     plan.waves = plan.few || a.head_dim <= 64 || list <= 128 * a.n_seqs ? 4 : 8;
     plan.tile_rows = plan.few ? 16 * plan.few : 32 * plan.waves;
-    plan.streamed = a.k_rows * a.kv_heads * a.head_dim * 4 > kLastLevelCacheBytes;
-    // Keys are cut where the tiles are too few for the device. A part's sums are written and read again: those of many rows
-    // are worth one workgroup for each compute unit and no more (512 rows over 8192 keys, 64 / 8 heads: 155 us, for
-    // twice as many 165, for four times 189), those of a single token's rows several.
-    const int64_t tiles = (plan.few ? a.n_seqs : list / plan.tile_rows + 1) * a.kv_heads;
+    // Keys are cut where the tiles are too few for the device, if that is estimated to save time: a workgroup takes 1.7 us for 100
+    // keys (1.05 in the form for few rows; 0.72 times that for up to 64 columns), and parts cost a second kernel and their sums' way through memory. (One prompt of 1500 tokens,
+    // 32 / 8 heads: 43 us whole, 63 in two parts; 512 rows over 8192 keys, 64 / 8 heads: 165 us whole, 141 in two parts, 166
+    // in four; single tokens over 2500 keys, 32 / 8 heads: 31 us whole, 13.5 in five.)
+    const int64_t tiles = (plan.few ? a.q_rows : list / plan.tile_rows + 1) * a.kv_heads;
     const int64_t keys = a.k_rows / a.n_seqs, enough = plan.few ? 512 : 256, wanted = plan.few ? 2048 : 256;
     plan.min_chunk = 512;
-    int64_t chunks = 1;
-    if (tiles < enough) chunks = std::min((wanted + tiles - 1) / tiles, (keys + plan.min_chunk - 1) / plan.min_chunk);
-    plan.chunks = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(chunks, 32)));
+    plan.chunks = 1;
+    if (tiles < enough) {
+        const int64_t most = std::min<int64_t>({kMostChunks, (wanted + tiles - 1) / tiles, (keys + plan.min_chunk - 1) / plan.min_chunk});
+        const double longest = a.n_seqs == 1 ? keys : 1.5 * keys, whole_us = longest * (plan.few ? 0.0105 : 0.017) * (a.head_dim > 64 ? 1.0 : 0.72);
+        const double sums_us = 8.0 * a.q_rows * a.q_heads * (a.head_dim + 2) / 4e6;
+        double best_us = whole_us;
+        for (int c = 2; c <= most; ++c) {
+            const double us = whole_us / c + 3.5 + c * sums_us;
+            if (us < best_us) {
+                best_us = us;
+                plan.chunks = c;
+            }
+        }
+    }
     return plan;
+}
+
+// Workgroups of a launch: no sequence has more tiles of the few rows' form than rows, and every sequence may end inside a
+// tile of the other.
+static int64_t attention_grid(const tw_attention_args &a, const AttentionPlan &plan)
+{
+    const int64_t list = a.q_rows * (a.q_heads / a.kv_heads);
+    return (plan.few ? a.q_rows : list / plan.tile_rows + a.n_seqs) * plan.chunks * a.kv_heads;
+}
+static int64_t join_grid(const tw_attention_args &a) { return (a.q_rows * a.q_heads + 3) / 4; }
+
+// A launch has fewer than 2^32 threads.
+static bool attention_launch_fits(const tw_attention_args &a)
+{
+    const AttentionPlan plan = attention_plan(a);
+    return attention_grid(a, plan) <= INT32_MAX / 256 && (plan.chunks == 1 || join_grid(a) <= INT32_MAX / 256);
+}
+
+static tw_status attention_sizes(const tw_attention_args &a)
+{
+    if (a.n_seqs < 0 || a.q_rows < 0 || a.k_rows < 0 || a.q_heads < 1 || a.kv_heads < 1 || a.head_dim < 1) return TW_ERR_SHAPE;
+    if (a.q_heads % a.kv_heads != 0) return TW_ERR_SHAPE;
+    if (!(a.scale > 0.0f) || !(a.scale <= 3.402823466e+38f)) return TW_ERR_SHAPE;
+    if (a.head_dim % 8 != 0 || a.head_dim > TW_MAX_HEAD_DIM) return TW_ERR_UNSUPPORTED;
+    if (a.q_heads > TW_MAX_HEADS || a.n_seqs > TW_MAX_SEQS) return TW_ERR_UNSUPPORTED;
+    const int64_t wq = static_cast<int64_t>(a.q_heads) * a.head_dim, wk = static_cast<int64_t>(a.kv_heads) * a.head_dim;
+    if (a.q_stride < wq || a.out_stride < wq || a.k_stride < wk || a.v_stride < wk) return TW_ERR_SHAPE;
+    for (const int64_t s : {a.q_stride, a.k_stride, a.v_stride, a.out_stride})
+        if (s % 8 != 0 || s > TW_MAX_ROW_STRIDE) return TW_ERR_UNSUPPORTED;
+    if (a.n_seqs == 0 || a.q_rows == 0) return TW_OK;
+    // offsets are 32-bit, and so are the places in a group's list of rows
+    if (a.q_rows > INT32_MAX - 1024 || a.k_rows > INT32_MAX - 1024 || a.q_rows * (a.q_heads / a.kv_heads) > INT32_MAX - 1024)
+        return TW_ERR_UNSUPPORTED;
+    return attention_launch_fits(a) ? TW_OK : TW_ERR_UNSUPPORTED;
 }
 
 static int64_t attention_workspace(const tw_attention_args &a)
@@ -942,41 +983,38 @@ static int64_t attention_workspace(const tw_attention_args &a)
 }
 
 static tw_status launch_attention(void (*kernel)(AttentionParams), std::atomic<int> *allowed, int threads, int lds_bytes,
-                                  const AttentionParams &p, int64_t tiles, hipStream_t stream)
+                                  const AttentionParams &p, int64_t grid, hipStream_t stream)
 {
     TW_TRY(allow_dynamic_lds(reinterpret_cast<const void *>(kernel), lds_bytes, allowed));
-    const int64_t grid = tiles * p.chunks * p.kv_heads;
-    if (grid > INT32_MAX) return TW_ERR_UNSUPPORTED;
     TW_HIP(launch_kernel(kernel, dim3(static_cast<uint32_t>(grid)), dim3(static_cast<uint32_t>(threads)),
                          static_cast<unsigned>(lds_bytes), stream, p));
     return TW_OK;
 }
 
-template <int DP, int RB, bool STREAMED>
-static tw_status launch_few(const AttentionParams &p, hipStream_t stream)
+template <int DP, int RB>
+static tw_status launch_few(const AttentionParams &p, int64_t grid, hipStream_t stream)
 {
     using Shape = FewShape<DP, RB>;
     static std::atomic<int> allowed[kMaxDevices];
-    return launch_attention(attention_few_kernel<DP, RB, STREAMED>, allowed, Shape::kThreads, Shape::kLds, p, p.n_seqs, stream);
+    return launch_attention(attention_few_kernel<DP, RB>, allowed, Shape::kThreads, Shape::kLds, p, grid, stream);
 }
 
 template <int DP, int WAVES>
-static tw_status launch_wide(const AttentionParams &p, hipStream_t stream)
+static tw_status launch_wide(const AttentionParams &p, int64_t grid, hipStream_t stream)
 {
     using Shape = WideShape<DP, WAVES>;
     static std::atomic<int> allowed[kMaxDevices];
-    return launch_attention(attention_wide_kernel<DP, WAVES>, allowed, Shape::kThreads, Shape::kLds, p,
-                            p.q_rows * p.group / Shape::kRows + p.n_seqs, stream);
+    return launch_attention(attention_wide_kernel<DP, WAVES>, allowed, Shape::kThreads, Shape::kLds, p, grid, stream);
 }
 
 template <int DP>
-static tw_status launch_attention_for(const AttentionParams &p, const AttentionPlan &plan, hipStream_t stream)
+static tw_status launch_attention_for(const AttentionParams &p, const AttentionPlan &plan, int64_t grid, hipStream_t stream)
 {
-    if (plan.few == 1) return plan.streamed ? launch_few<DP, 1, true>(p, stream) : launch_few<DP, 1, false>(p, stream);
-    if (plan.few == 2) return plan.streamed ? launch_few<DP, 2, true>(p, stream) : launch_few<DP, 2, false>(p, stream);
+    if (plan.few == 1) return launch_few<DP, 1>(p, grid, stream);
+    if (plan.few == 2) return launch_few<DP, 2>(p, grid, stream);
     if constexpr (DP == 128)
-        if (plan.waves == 8) return launch_wide<DP, 8>(p, stream);
-    return launch_wide<DP, 4>(p, stream);
+        if (plan.waves == 8) return launch_wide<DP, 8>(p, grid, stream);
+    return launch_wide<DP, 4>(p, grid, stream);
 }
 
 }  // namespace tw
@@ -1040,6 +1078,7 @@ tw_status tw_attention(const tw_attention_args *args, void *workspace, int64_t w
     }
 
     const AttentionPlan plan = attention_plan(a);
+    const int64_t grid = attention_grid(a, plan);
     AttentionParams p;
     p.q = static_cast<const char *>(a.q);
     p.k = static_cast<const char *>(a.k);
@@ -1070,11 +1109,9 @@ tw_status tw_attention(const tw_attention_args *args, void *workspace, int64_t w
     p.min_chunk = plan.min_chunk;
     p.c = static_cast<float>(a.scale * 1.4426950408889634);
     const hipStream_t s = static_cast<hipStream_t>(stream);
-    TW_TRY(a.head_dim > 64 ? launch_attention_for<128>(p, plan, s) : launch_attention_for<64>(p, plan, s));
+    TW_TRY(a.head_dim > 64 ? launch_attention_for<128>(p, plan, grid, s) : launch_attention_for<64>(p, plan, grid, s));
     if (plan.chunks > 1) {
-        const int64_t grid = (a.q_rows * a.q_heads + 3) / 4;
-        if (grid > INT32_MAX) return TW_ERR_UNSUPPORTED;
-        TW_HIP(launch_kernel(attention_join_kernel, dim3(static_cast<uint32_t>(grid)), dim3(256), 0, s, p));
+        TW_HIP(launch_kernel(attention_join_kernel, dim3(static_cast<uint32_t>(join_grid(a))), dim3(256), 0, s, p));
     }
     return TW_OK;
 }

@@ -161,6 +161,7 @@ struct RowsParams {
     const float *weights;
     float *dweights;
     int64_t tokens, rows;
+    int64_t first;        // token of the launch
     int top_k, pieces;    // 16-byte pieces of a row
     int row_log2;
 };
@@ -197,11 +198,17 @@ __device__ __forceinline__ void places(const RowsParams &p, int64_t token, int k
     }
 }
 
+// The token that this thread's row is of.
+__device__ __forceinline__ int64_t row_token(const RowsParams &p)
+{
+    return p.first + static_cast<int64_t>(blockIdx.x) * (256 >> p.row_log2) + (threadIdx.x >> p.row_log2);
+}
+
 template <bool STREAMED>
 __global__ __launch_bounds__(256) void expert_dispatch_kernel(RowsParams p)
 {
     const int threads = 1 << p.row_log2;
-    const int64_t token = static_cast<int64_t>(blockIdx.x) * (256 >> p.row_log2) + (threadIdx.x >> p.row_log2);
+    const int64_t token = row_token(p);
     if (token >= p.tokens) return;
     for (int k0 = 0; k0 < p.top_k; k0 += kMost) {
         int32_t at[kMost];
@@ -219,7 +226,7 @@ template <bool WEIGHTED, bool STREAMED>
 __global__ __launch_bounds__(256) void expert_combine_kernel(RowsParams p)
 {
     const int threads = 1 << p.row_log2;
-    const int64_t token = static_cast<int64_t>(blockIdx.x) * (256 >> p.row_log2) + (threadIdx.x >> p.row_log2);
+    const int64_t token = row_token(p);
     if (token >= p.tokens) return;
     for (int c = threadIdx.x & (threads - 1); c < p.pieces; c += threads) {
         float sum[8] = {};
@@ -253,7 +260,7 @@ __global__ __launch_bounds__(256) void expert_combine_backward_kernel(RowsParams
 {
     __shared__ float wave_dot[4][kMost];
     const int threads = 1 << p.row_log2, in_row = threadIdx.x & (threads - 1);
-    const int64_t token = static_cast<int64_t>(blockIdx.x) * (256 >> p.row_log2) + (threadIdx.x >> p.row_log2);
+    const int64_t token = row_token(p);
     const bool has = token < p.tokens;
     for (int k0 = 0; k0 < p.top_k; k0 += kMost) {
         int32_t at[kMost];
@@ -347,9 +354,13 @@ static void row_layout(int64_t H, RowsParams *p)
 
 static tw_status launch_rows(void (*kernel)(RowsParams), const RowsParams &p, void *stream)
 {
-    const int64_t per_group = 256 >> p.row_log2;
-    TW_HIP(launch_kernel(kernel, dim3(static_cast<uint32_t>((p.tokens + per_group - 1) / per_group)), dim3(256), 0,
-                         static_cast<hipStream_t>(stream), p));
+    // a launch has fewer than 2^32 threads
+    const int64_t per_group = 256 >> p.row_log2, most = int64_t(1) << 23;
+    RowsParams part = p;
+    for (int64_t groups = (p.tokens + per_group - 1) / per_group; groups > 0; groups -= most) {
+        TW_HIP(launch_kernel(kernel, dim3(static_cast<uint32_t>(std::min(groups, most))), dim3(256), 0, static_cast<hipStream_t>(stream), part));
+        part.first += most * per_group;
+    }
     return TW_OK;
 }
 

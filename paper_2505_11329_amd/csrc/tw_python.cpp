@@ -569,6 +569,17 @@ const at::Tensor &here(const at::Tensor &t, const Name &n)
     return t;
 }
 
+// The stream's handle; a stream of another device is refused, too.
+void *stream_here(PyObject *o)
+{
+    if (o != Py_None) {
+        Ref index(PyObject_GetAttrString(o, "device_index"));
+        if (!index.o) fail();
+        if (as_int(index.o) != c10::hip::current_device()) fail(PyExc_ValueError, "stream must be of the current device");
+    }
+    return stream_handle(o);
+}
+
 const at::Tensor &typed(PyObject *o, const Name &n, at::ScalarType type, const char *type_name)
 {
     const at::Tensor &t = here(gpu_tensor(o, n), n);
@@ -713,7 +724,7 @@ PyObject *py_attention(PyObject *, PyObject *const *v, Py_ssize_t n)
     return entry("attention", n, 11, [&] {
         Attention t;
         t.fill(v[0], v[1], v[2], v[3], v[4], v[5], v[6], v[7], v[8]);
-        void *s = stream_handle(v[10]);
+        void *s = stream_here(v[10]);
         Workspace w;
         w.fill(v[9], tw_attention_workspace_bytes(&t.a), THPVariable_Unpack(v[0]), s);
         call("tw_attention", [&] { return tw_attention(&t.a, w.p, w.bytes, s); });
@@ -737,7 +748,7 @@ PyObject *py_expert_sort(PyObject *, PyObject *const *v, Py_ssize_t n)
             offsets = given_or_empty(v[4], ids, {experts + 1}, at::kInt);
         int32_t *const o = int32_array(order.o, {"order"}, {N * top_k}), *const p = int32_array(position.o, {"position"}, {N, top_k}),
                 *const f = int32_array(offsets.o, {"offsets"}, {experts + 1});
-        void *s = stream_handle(v[6]);
+        void *s = stream_here(v[6]);
         Workspace w;
         w.fill(v[5], tw_expert_sort_workspace_bytes(N, static_cast<int>(top_k), static_cast<int>(experts)), ids, s);
         call("tw_expert_sort", [&] {
@@ -773,7 +784,7 @@ PyObject *py_expert_dispatch(PyObject *, PyObject *const *v, Py_ssize_t n)
         Ref out = given_or_empty(v[2], x, {p.N * p.top_k, p.H}, at::kBFloat16);
         const int64_t rows = sized(out.o, {"out"}, 2, "out must be [rows, H]").size(0);
         const void *from = bf16_array(v[0], {"x"}, {p.N, p.H});
-        void *to = bf16_array(out.o, {"out"}, {rows, p.H}), *s = stream_handle(v[3]);
+        void *to = bf16_array(out.o, {"out"}, {rows, p.H}), *s = stream_here(v[3]);
         call("tw_expert_dispatch", [&] { return tw_expert_dispatch(from, p.position, p.N, p.top_k, p.H, to, rows, s); });
         return out.release();
     });
@@ -790,7 +801,7 @@ PyObject *py_expert_combine(PyObject *, PyObject *const *v, Py_ssize_t n)
         Ref out = given_or_empty(v[3], y, {p.N, p.H}, at::kBFloat16);
         const void *from = bf16_array(v[0], {"y"}, {rows, p.H});
         const float *w = v[2] == Py_None ? nullptr : float_array(v[2], {"weights"}, {p.N, p.top_k});
-        void *to = bf16_array(out.o, {"out"}, {p.N, p.H}), *s = stream_handle(v[4]);
+        void *to = bf16_array(out.o, {"out"}, {p.N, p.H}), *s = stream_here(v[4]);
         call("tw_expert_combine", [&] { return tw_expert_combine(from, rows, p.position, w, p.N, p.top_k, p.H, to, s); });
         return out.release();
     });
@@ -807,7 +818,7 @@ PyObject *py_expert_combine_backward(PyObject *, PyObject *const *v, Py_ssize_t 
         Ref dy = given_or_empty(v[4], y, {rows, p.H}, at::kBFloat16), dw = given_or_empty(v[5], y, {p.N, p.top_k}, at::kFloat);
         const void *d = bf16_array(v[0], {"dout"}, {p.N, p.H}), *from = bf16_array(v[1], {"y"}, {rows, p.H});
         const float *w = float_array(v[3], {"weights"}, {p.N, p.top_k});
-        void *to = bf16_array(dy.o, {"dy"}, {rows, p.H}), *s = stream_handle(v[6]);
+        void *to = bf16_array(dy.o, {"dy"}, {rows, p.H}), *s = stream_here(v[6]);
         float *to_w = float_array(dw.o, {"dweights"}, {p.N, p.top_k});
         call("tw_expert_combine_backward", [&] {
             return tw_expert_combine_backward(d, from, rows, p.position, w, p.N, p.top_k, p.H, to, to_w, s);

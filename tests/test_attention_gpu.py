@@ -35,6 +35,7 @@ def check(tw, q, k, v, qo, ko, causal=True, scale=None, what="", **more):
 LENGTHS = [
     ([1], [1]), ([1], [0]), ([2], [1]), ([63], [63]), ([65], [64]), ([5, 0, 1, 130], [5, 7, 33, 130]),
     ([1, 1, 1, 1, 1], [1, 31, 32, 129, 700]), ([257], [257]), ([40, 300], [900, 301]), ([7, 9], [3, 0]), ([0, 0, 3], [4, 0, 3]),
+    ([2, 0, 0, 1, 0], [50, 3, 0, 700, 9]), ([1, 1, 0, 0], [600, 40, 7, 0]), ([0, 1], [3, 2]),
 ]
 HEADS = [(1, 1, 64), (4, 2, 128), (8, 1, 128), (6, 2, 72), (3, 3, 8), (32, 1, 64), (5, 1, 96)]
 
@@ -67,6 +68,16 @@ def test_more_keys_than_the_last_level_cache_holds(tw):
     q, k, v, qo, ko = inputs([1, 0, 1], [23000, 5, 18001], 16, 16, 128, seed=1)
     assert k.numel() * 4 > 256 << 20
     check(tw, q, k, v, qo, ko, what="streamed")
+
+
+@pytest.mark.parametrize("most", [0, 1, 2, 40])
+def test_more_sequences_than_lanes(tw, most):
+    """Of 150 sequences, single tokens with empty ones behind them, or up to `most` rows in any order."""
+    g = torch.Generator().manual_seed(most)
+    q_lens = [1] * 130 + [0] * 20 if most == 0 else torch.randint(0, most + 1, (150,), generator=g).tolist()
+    k_lens = [n + int(x) for n, x in zip(q_lens, torch.randint(0, 200, (150,), generator=g))]
+    check(tw, *inputs(q_lens, k_lens, 4, 2, 64, seed=most), what=str(most))
+    check(tw, *inputs(q_lens, k_lens, 24, 1, 64, seed=most), causal=False, what=str(most))
 
 
 def test_forms_of_the_launch(tw):

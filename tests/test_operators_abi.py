@@ -41,7 +41,8 @@ def test_attention_refuses():
         assert attention(**change) == E_SHAPE, change
     for change in (dict(head_dim=60), dict(head_dim=136, q_stride=2048, k_stride=512, v_stride=512, out_stride=2048),
                    dict(q_stride=516), dict(k_stride=(1 << 22) + 8), dict(q_heads=1026, q_stride=1 << 17, out_stride=1 << 17),
-                   dict(n_seqs=(1 << 20) + 1), dict(q_rows=1 << 31), dict(k_rows=1 << 31), dict(q_rows=1 << 29)):
+                   dict(n_seqs=(1 << 14) + 1), dict(q_rows=1 << 31), dict(k_rows=1 << 31), dict(q_rows=1 << 29),
+                   dict(q_rows=1 << 29, q_heads=2, q_stride=128, out_stride=128)):
         assert attention(**change) == E_UNSUP, change
     need = 2 * 8 * 66 * 4 * plan(2, 2, 9000, 8, 2, 64).chunks
     assert attention() == E_NULL                                    # no workspace
@@ -69,7 +70,7 @@ def test_attention_plan_and_workspace():
         plan(1, 1, 1, 8, 3, 64)
     assert plan(0, 5, 5, 8, 2, 64).chunks == 0 and tw.attention_workspace_bytes(0, 5, 5, 8, 2, 64) == 0
     for sizes in ((1, 1, 1, 8, 2, 64), (48, 48, 200000, 64, 8, 128), (1, 100, 9000, 16, 2, 128), (1, 4096, 16384, 64, 8, 128),
-                  (64, 64, 64, 1, 1, 8), (1, 1, 0, 4, 4, 64), (1 << 20, 1 << 20, 1 << 30, 8, 1, 128)):
+                  (64, 64, 64, 1, 1, 8), (1, 1, 0, 4, 4, 64), (1 << 14, 1 << 14, 1 << 30, 8, 1, 128)):
         f = plan(*sizes)
         assert f.chunks >= 1 and f.min_chunk >= 128 and f.tile_rows > 0
         assert tw.attention_workspace_bytes(*sizes) == (0 if f.chunks == 1 else f.chunks * sizes[1] * sizes[3] * (sizes[5] + 2) * 4)
