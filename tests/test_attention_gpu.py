@@ -56,6 +56,7 @@ def test_lengths_and_heads(tw, heads, kv_heads, dim, causal):
     ([2, 3, 1, 4], [600, 2049, 1, 1024], 8, 2, 80),
     ([1000, 40], [1000, 2040], 8, 2, 128),          # a prompt and a chunk
     ([300] * 4, [300] * 4, 16, 16, 64),
+    ([2200, 1900], [2200, 2400], 32, 8, 128),       # tiles enough for eight waves each
 ])
 def test_long_keys(tw, q_lens, k_lens, heads, kv_heads, dim):
     for causal in (True, False):
@@ -84,7 +85,7 @@ def test_forms_of_the_launch(tw):
     """Each kernel and rule is reached by the sizes of these tests."""
     forms = {(f.tile_rows, f.key_waves, f.chunks > 1): sizes for sizes in (
         (1, 1, 1, 8, 1, 128), (1, 1, 20011, 4, 4, 64), (1, 1, 1, 32, 1, 64), (1, 1, 9000, 32, 1, 64), (1, 63, 63, 1, 1, 64),
-        (1, 100, 4100, 16, 2, 64), (2, 1000, 1000, 4, 2, 128), (1, 100, 4100, 16, 2, 128), (4, 100, 4000, 4, 2, 128))
+        (1, 100, 4100, 16, 2, 64), (2, 4100, 4600, 32, 8, 128), (1, 100, 4100, 16, 2, 128), (4, 100, 4000, 4, 2, 128))
         for f in (tw.attention_plan(*sizes),)}
     assert set(forms) == {(16, 4, False), (16, 4, True), (32, 4, False), (32, 4, True), (128, 1, False), (128, 1, True), (256, 1, False),
                           (256, 1, True)}, forms
