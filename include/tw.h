@@ -580,8 +580,8 @@ tw_status tw_weave_tune(const tw_layer_args *layer, int64_t multiple, const int6
  *               case it may be NULL), 16-byte aligned, overwritten; calls that may run at the same time
  *               need one each
  *
- * Where rows and heads alone are too few for the device, each sequence's keys are cut into parts of at
- * least 512 that work side by side, and a second kernel joins them. The result bits of a row depend
+ * Where rows and heads alone are too few for the device, each sequence's keys are cut into parts that work
+ * side by side, and a second kernel joins them. The result bits of a row depend
  * on its own q, its sequence's k and v, and on the form of the launch, which follows from the sizes of
  * the call (tw_attention_plan): calls of the same form, e.g. one batch and the same batch split in two
  * large halves, give the same bits.

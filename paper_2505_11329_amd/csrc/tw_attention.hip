@@ -920,10 +920,10 @@ static AttentionPlan attention_plan(const tw_attention_args &a)
     // Keys are cut where the tiles are too few for the device, if that is estimated to save time: a workgroup takes 1.7 us for 100
     // keys (1.05 in the form for few rows; 0.72 times that for up to 64 columns), and parts cost a second kernel and their sums' way through memory. (One prompt of 1500 tokens,
     // 32 / 8 heads: 43 us whole, 63 in two parts; 512 rows over 8192 keys, 64 / 8 heads: 165 us whole, 141 in two parts, 166
-    // in four; single tokens over 2500 keys, 32 / 8 heads: 31 us whole, 13.5 in five.)
+    // in four; one token over 2500 keys, 32 / 8 heads: 31 us whole, 11 in parts.)
     const int64_t tiles = (plan.few ? a.q_rows : list / plan.tile_rows + 1) * a.kv_heads;
     const int64_t keys = a.k_rows / a.n_seqs, enough = plan.few ? 512 : 256, wanted = plan.few ? 2048 : 256;
-    plan.min_chunk = 512;
+    plan.min_chunk = plan.few ? 256 : 512;  // (parts of 256, 512 keys of one token over 1500: 10.6, 14.1 us)
     plan.chunks = 1;
     if (tiles < enough) {
         const int64_t most = std::min<int64_t>({kMostChunks, (wanted + tiles - 1) / tiles, (keys + plan.min_chunk - 1) / plan.min_chunk});
