@@ -280,8 +280,8 @@ struct Place {
     bool found;
 };
 // Every wave finds it by itself, 64 sequences at a time, a lane each: the i-th tile of TILE rows. Up to 64 sequences, the
-// tiles with the most keys come first, whatever sequence they are of, so that what runs last is short (23 prompts of 8101 tokens:
-// 76 us in the sequences' order); more of them are taken in their order, each one's last tiles first.
+// tiles with the most keys come first, whatever sequence they are of, so that what runs last is short (16 sequences of 8192 tokens,
+// 32 / 8 heads: 125 us, 130 in the sequences' order); more of them are taken in their order, each one's last tiles first.
 template <int TILE>
 __device__ __forceinline__ Place find_place(const AttentionParams &p, int i)
 {
@@ -339,11 +339,11 @@ __device__ __forceinline__ bool single_tokens(const AttentionParams &p)
     return __all(single);
 }
 
-// Few rows to a sequence, single tokens as a rule: tiles of 16 or 32 rows of a group's list, whose keys four waves share. Bound
+// Few rows to a sequence, single tokens or a few of each: tiles of 16 or 32 rows of a group's list, whose keys four waves share. Bound
 // by what comes from memory. Each wave has keys of its own, 32 at a time, and a place in the LDS for them: the next ones are
 // asked for as soon as a product has read the ones before, and nothing but the result ties the waves to each other. Two
-// workgroups to a compute unit keep up to 128 KB on their way. Each key is read once, and not kept in the caches: 48 tokens over
-// 6000 keys, 64 / 8 heads, 115 us, 131 if kept; 4 tokens over 8192 keys 19.3, 21.1.
+// workgroups to a compute unit keep up to 128 KB on their way. Where a tile has all of its sequence's rows its keys are not kept in
+// the caches: 48 tokens over 6000 keys, 64 / 8 heads, 115 us, 131 if kept; 4 tokens over 8192 keys 19.3, 21.1.
 template <int DP, int RB>
 struct FewShape {
     static constexpr int kWaves = 4, kThreads = 64 * kWaves, kRows = 16 * RB, kKeys = 32;
@@ -371,10 +371,10 @@ __global__ __launch_bounds__(256, 2) void attention_few_kernel(AttentionParams p
 
     const int kv_head = blockIdx.x % p.kv_heads;
     const int rest = blockIdx.x / p.kv_heads;
-    const int chunk = rest % p.chunks;
+    const int chunk = rest % p.chunks, i = rest / p.chunks;
     Place at = {};
-    if (single_tokens(p)) at.s = sequence(p, rest / p.chunks);
-    else at = find_place<Shape::kRows>(p, rest / p.chunks);
+    if (p.group > Shape::kRows || !single_tokens(p)) at = find_place<Shape::kRows>(p, i);
+    else if (i < p.n_seqs) at.s = sequence(p, i);
     const Sequence &s = at.s;
     const int list = s.q_len * p.group, r0 = at.tile * Shape::kRows;
     if (r0 >= list) return;  // (no tile is left for this workgroup)
@@ -401,15 +401,20 @@ __global__ __launch_bounds__(256, 2) void attention_few_kernel(AttentionParams p
     const int end = min(keys.end, p.causal ? last_pos + past + 1 : s.k_len);
     const int first_last = min(keys.end - 1, p.causal ? list_pos(p, r0) + past : s.k_len - 1);  // the last key that the first row sees
 
+    const bool alone = list <= Shape::kRows;  // no other tile has a use for these keys
     auto load_rows = [&](const char *base, int64_t stride, int key0, uint32_t to, auto swizzle) TW_INLINE {
         const int rows = min(Shape::kKeys, end - key0);
         const i32x4 rsrc = buffer_of(base + key0 * stride, rows > 0 ? static_cast<uint32_t>((rows - 1) * stride + p.dim * 2) : 0);
+        auto load = [&](auto streamed) TW_INLINE {
 #pragma unroll
-        for (int i = 0; i < Shape::kLoads; ++i) {
-            const int col = (place ^ swizzle(i * Shape::kLoadRows + load_row)) * 8;
-            load_to_lds<true>(rsrc, col < p.dim ? static_cast<uint32_t>(load_row * stride + col * 2) : kPastTensor,
-                                  static_cast<uint32_t>(i * Shape::kLoadRows * stride), to + i * 1024);
-        }
+            for (int i = 0; i < Shape::kLoads; ++i) {
+                const int col = (place ^ swizzle(i * Shape::kLoadRows + load_row)) * 8;
+                load_to_lds<decltype(streamed)::value>(rsrc, col < p.dim ? static_cast<uint32_t>(load_row * stride + col * 2) : kPastTensor,
+                                                       static_cast<uint32_t>(i * Shape::kLoadRows * stride), to + i * 1024);
+            }
+        };
+        if (alone) load(std::true_type{});
+        else load(std::false_type{});
     };
     auto load_keys = [&](int key0) TW_INLINE { load_rows(k_head, p.k_stride, key0, k_at, [](int row) { return k_swizzle<DP>(row); }); };
     auto load_values = [&](int key0) TW_INLINE { load_rows(v_head, p.v_stride, key0, v_at, [](int row) { return v_swizzle<DP>(row); }); };
@@ -900,7 +905,7 @@ static constexpr int kMostChunks = 32;  // a lane each in the kernel that joins 
 // How a call is launched.
 struct AttentionPlan {
     int few;        // blocks of 16 rows of a tile whose four waves share the keys; 0: a wave for each 32 rows of a larger tile
-    int waves;
+    int waves;      // of a workgroup
     int tile_rows;
     int chunks;     // parts of each sequence's keys, joined by a second kernel where there are more than one
     int min_chunk;  // fewest keys of a part but the last
@@ -910,28 +915,37 @@ static AttentionPlan attention_plan(const tw_attention_args &a)
 {
     AttentionPlan plan;
     const int64_t group = a.q_heads / a.kv_heads, list = a.q_rows * group;
-    // A row for each sequence is a batch of single tokens. (With more, some sequences may have many: the other form has a
-    // workgroup for each of their tiles.)
-    plan.few = a.q_rows > a.n_seqs || group > 32 ? 0 : group > 16 ? 2 : 1;
-    // Four waves, two workgroups to a compute unit, where eight would have no rows: 32 sequences of 4 rows on average, keys of up
-    // to 6K, 64 / 8 heads: 94 us, 112 with eight.
-    plan.waves = plan.few || a.head_dim <= 64 || list <= 128 * a.n_seqs ? 4 : 8;
+    // Sequences of so few rows on average that tiles of 16 or 32 hold most of them; longer ones among them have more tiles, no more
+    // than there are sequences in all. (4 rows each on average, 64 / 8 heads, keys of up to 1000, 4000, 8000: 4 sequences 17, 17, 26
+    // us, 23, 27, 30 in the other form; 32 of them 22, -, 99, 29, -, 109.)
+    plan.few = list <= 16 * a.n_seqs ? 1 : list <= 32 * a.n_seqs ? 2 : 0;
+    // Four waves, two workgroups to a compute unit, where sequences seldom fill tiles of 256 rows or are short, so that a workgroup's
+    // start, search and results are much of its time, beside which the second one works (16 heads of 128, prompts of up to 128 tokens
+    // on average, 64 and 128 of them: 44 and 45 us, 59 and 65 with eight; of 512, 16: 79, 82; 64 / 8 heads, 16 chunks of 64 rows over 2000
+    // keys: 45, 48). Long sequences of many rows are read less often by tiles of 256 rows (8 heads' 512 rows over 8000 keys of 4
+    // sequences: 67, 62).
+    const bool short_lists = list <= 256 * a.n_seqs || (list <= 1024 * a.n_seqs && a.k_rows <= 4096 * a.n_seqs);
+    plan.waves = plan.few || a.head_dim <= 64 || short_lists ? 4 : 8;
     plan.tile_rows = plan.few ? 16 * plan.few : 32 * plan.waves;
     // Keys are cut where the tiles are too few for the device, if that is estimated to save time: a workgroup takes 1.7 us for 100
-    // keys (1.05 in the form for few rows; 0.72 times that for up to 64 columns), and parts cost a second kernel and their sums' way through memory. (One prompt of 1500 tokens,
-    // 32 / 8 heads: 43 us whole, 63 in two parts; 512 rows over 8192 keys, 64 / 8 heads: 165 us whole, 141 in two parts, 166
-    // in four; one token over 2500 keys, 32 / 8 heads: 31 us whole, 11 in parts.)
-    const int64_t tiles = (plan.few ? a.q_rows : list / plan.tile_rows + 1) * a.kv_heads;
-    const int64_t keys = a.k_rows / a.n_seqs, enough = plan.few ? 512 : 256, wanted = plan.few ? 2048 : 256;
+    // keys (1.05 in the form for few rows; 0.72 times that for up to 64 columns), its parts 1.4 times their share if every compute
+    // unit had one before the cut, and parts cost a second kernel and their sums' way through memory. (One prompt of 1500 tokens,
+    // 32 / 8 heads: 43 us whole, 63 in two parts; 512 rows over 8192 keys, 64 / 8 heads: 165 us whole, 141 in two parts, 166 in four;
+    // one token over 2500 keys, 32 / 8 heads: 31 us whole, 11 in parts; 16 chunks of 32 rows over up to 8000 keys, 64 / 8 heads:
+    // 140 whole, 107 in two parts.) Of prompts under a causal mask most tiles are short: parts for each compute unit are enough.
+    const int64_t tiles = (plan.few ? a.n_seqs : std::max(list / plan.tile_rows + 1, a.n_seqs)) * a.kv_heads, keys = a.k_rows / a.n_seqs;
+    const bool pairs = plan.waves == 4 && !(a.causal && 2 * a.q_rows >= a.k_rows);
+    const int64_t enough = plan.few || pairs ? 512 : 256, wanted = plan.few ? 2048 : enough;
     plan.min_chunk = plan.few ? 256 : 512;  // (parts of 256, 512 keys of one token over 1500: 10.6, 14.1 us)
     plan.chunks = 1;
     if (tiles < enough) {
         const int64_t most = std::min<int64_t>({kMostChunks, (wanted + tiles - 1) / tiles, (keys + plan.min_chunk - 1) / plan.min_chunk});
-        const double longest = a.n_seqs == 1 ? keys : 1.5 * keys, whole_us = longest * (plan.few ? 0.0105 : 0.017) * (a.head_dim > 64 ? 1.0 : 0.72);
+        const double longest = a.n_seqs == 1 ? keys : 1.5 * keys;
+        const double whole_us = longest * (plan.few ? 0.0105 : 0.017) * (a.head_dim > 64 ? 1.0 : 0.72);
         const double sums_us = 8.0 * a.q_rows * a.q_heads * (a.head_dim + 2) / 4e6;
         double best_us = whole_us;
         for (int c = 2; c <= most; ++c) {
-            const double us = whole_us / c + 3.5 + c * sums_us;
+            const double us = whole_us / c * (!plan.few && tiles > 256 ? 1.4 : 1.0) + 3.5 + c * sums_us;
             if (us < best_us) {
                 best_us = us;
                 plan.chunks = c;
@@ -945,12 +959,12 @@ static AttentionPlan attention_plan(const tw_attention_args &a)
     return plan;
 }
 
-// Workgroups of a launch: no sequence has more tiles of the few rows' form than rows, and every sequence may end inside a
-// tile of the other.
+// Workgroups of a launch: every sequence may end inside a tile, but none has more tiles than its rows need one by one.
 static int64_t attention_grid(const tw_attention_args &a, const AttentionPlan &plan)
 {
-    const int64_t list = a.q_rows * (a.q_heads / a.kv_heads);
-    return (plan.few ? a.q_rows : list / plan.tile_rows + a.n_seqs) * plan.chunks * a.kv_heads;
+    const int64_t group = a.q_heads / a.kv_heads, list = a.q_rows * group;
+    const int64_t tiles = std::min(list / plan.tile_rows + a.n_seqs, a.q_rows * ((group + plan.tile_rows - 1) / plan.tile_rows));
+    return tiles * plan.chunks * a.kv_heads;
 }
 static int64_t join_grid(const tw_attention_args &a) { return (a.q_rows * a.q_heads + 3) / 4; }
 

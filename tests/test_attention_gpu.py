@@ -81,6 +81,20 @@ def test_more_sequences_than_lanes(tw, most):
     check(tw, *inputs(q_lens, k_lens, 24, 1, 64, seed=most), causal=False, what=str(most))
 
 
+@pytest.mark.parametrize("q_lens,k_lens,heads,kv_heads,dim,tail", [
+    ([1] * 20, [300] * 20, 8, 4, 128, 40),                              # rows enough for more tiles than there are sequences
+    ([1, 1, 0, 0, 0, 1, 0, 0], [700, 9, 4, 0, 1, 2100, 1, 1], 40, 1, 64, 0),   # a row's heads are more than a tile
+    ([60] + [1] * 39, [60] + [90] * 39, 8, 4, 64, 0),                   # one sequence of many tiles
+    ([4, 3, 5, 4], [900, 2300, 5, 1700], 16, 4, 128, 0),                # some rows each, keys in parts
+    ([9, 0, 2], [4000, 3, 300], 8, 2, 128, 2),
+])
+def test_few_rows(tw, q_lens, k_lens, heads, kv_heads, dim, tail):
+    for causal in (True, False):
+        q, k, v, qo, ko = inputs(q_lens, k_lens, heads, kv_heads, dim, seed=9, tail=tail)
+        assert tw.attention_plan(len(q_lens), q.shape[0], k.shape[0], heads, kv_heads, dim).key_waves == 4
+        check(tw, q, k, v, qo, ko, causal=causal, what=str(q_lens))
+
+
 def test_forms_of_the_launch(tw):
     """Each kernel and rule is reached by the sizes of these tests."""
     forms = {(f.tile_rows, f.key_waves, f.chunks > 1): sizes for sizes in (
