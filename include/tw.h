@@ -11,7 +11,9 @@
  *     4.1.2 "Overlapped Execution");
  *   - a bf16 GEMM standing in for the other split's projection, and the
  *     fused-kernel-next-to-GEMM launch that one step of the weave consists of
- *     (Fig. 7b).
+ *     (Fig. 7b);
+ *   - what a layer does between two such boundaries: attention over a packed
+ *     batch, and the tokens sorted to their experts and back.
  *
  * The in-switch reduction of the paper has no counterpart on this hardware:
  * the P peer partials are P buffers in local HBM and the reading compute unit
@@ -19,7 +21,8 @@
  *
  * Conventions for every entry point
  *   - All data pointers are DEVICE pointers unless a parameter says "host".
- *     bf16 tensors are row-major, contiguous, 16-byte aligned.
+ *     bf16 tensors are row-major, contiguous (unless a call takes strides),
+ *     16-byte aligned.
  *   - The caller owns all memory and all streams. libtw keeps no pointer after
  *     a call returns. Pointer arrays and argument structs are read on the host
  *     during the call and may live on the caller's stack.
@@ -30,7 +33,8 @@
  *     happens on the host before the first HIP call, so an invalid call
  *     launches nothing and works (returns its error) on a machine without a GPU.
  *   - Results are a pure function of each row's inputs: bits do not depend on
- *     cu_budget, on N, on the stream, or on whether and where rows were split.
+ *     cu_budget, on N, on the stream, or on whether and where rows were split
+ *     (attention: within one form of its launch, see there).
  *   - HIP graphs: every entry point can be recorded into a stream capture
  *     (hipStreamBeginCapture on the caller's stream; the cross-stream entry
  *     points fork their second stream from `parent` and join it back, so a
@@ -575,7 +579,7 @@ tw_status tw_weave_tune(const tw_layer_args *layer, int64_t multiple, const int6
  *   head_dim    a multiple of 8 up to TW_MAX_HEAD_DIM; sizes other than 64 and 128 cost what the next of
  *               the two does
  *   strides     multiples of 8, at least heads * head_dim, at most TW_MAX_ROW_STRIDE
- *   scale       finite, > 0
+ *   scale       > 0, at most 2^127
  *   workspace   device memory of tw_attention_workspace_bytes() for these arguments (0 for many, in which
  *               case it may be NULL), 16-byte aligned, overwritten; calls that may run at the same time
  *               need one each

@@ -979,7 +979,7 @@ static tw_status attention_sizes(const tw_attention_args &a)
 {
     if (a.n_seqs < 0 || a.q_rows < 0 || a.k_rows < 0 || a.q_heads < 1 || a.kv_heads < 1 || a.head_dim < 1) return TW_ERR_SHAPE;
     if (a.q_heads % a.kv_heads != 0) return TW_ERR_SHAPE;
-    if (!(a.scale > 0.0f) || !(a.scale <= 3.402823466e+38f)) return TW_ERR_SHAPE;
+    if (!(a.scale > 0.0f) || !(a.scale <= 0x1p127f)) return TW_ERR_SHAPE;
     if (a.head_dim % 8 != 0 || a.head_dim > TW_MAX_HEAD_DIM) return TW_ERR_UNSUPPORTED;
     if (a.q_heads > TW_MAX_HEADS || a.n_seqs > TW_MAX_SEQS) return TW_ERR_UNSUPPORTED;
     const int64_t wq = static_cast<int64_t>(a.q_heads) * a.head_dim, wk = static_cast<int64_t>(a.kv_heads) * a.head_dim;

@@ -58,6 +58,12 @@ def test_attention_refuses():
     assert attention(q_rows=0, q=None, out=None) == OK
 
 
+def test_attention_refuses_scales():
+    for scale in (0.0, -1.0, 3.0e38, float("inf"), float("nan")):
+        assert attention(scale=scale) == E_SHAPE, scale
+    assert attention(scale=1.7e38, n_seqs=0) == OK
+
+
 def plan(*sizes):
     return tw.attention_plan(*sizes)
 
