@@ -586,8 +586,8 @@ struct WideShape {
     static constexpr int kLoads = kTileBytes / (16 * kThreads);  // of 16 bytes to a lane, for K or V of a tile
     static constexpr int kLoadRows = 64 / kPieces;               // rows of a wave's load
     static constexpr int kStageBytes = 2 * kTileBytes;           // K, V
-    // The rows of q pass through the second stage before its first tile comes, or a place of their own if they are too many;
-    // the results pass through the LDS in the end.
+    // The rows of q pass through the second stage before its first tile comes, or a place of their own if they are too many,
+    // and the results through the same place in the end.
     static constexpr int kQBytes = kRows * kRowBytes, kQAt = kQBytes <= kStageBytes ? kStageBytes : 2 * kStageBytes;
     static constexpr int kLds = kQAt + (kQBytes > kStageBytes ? kQBytes : kStageBytes);
 };
@@ -602,7 +602,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attention_wide_kernel(Attention
     // its registers are left to it (310 us, 313 with fragments ahead).
     constexpr int kAhead = DP == 128 ? 4 : 0;
     extern __shared__ __align__(16) char lds[];
-    __shared__ int flags[Shape::kWaves];  // a wave's pieces of the V tile held Inf or NaN; where rows see a part of the tile
+    __shared__ int flags[2][Shape::kWaves];  // a wave's pieces of the V tile held Inf or NaN; where rows see a part of the tile
     const int lane = threadIdx.x & 63, half = lane >> 5, row_lane = lane & 31;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
 
@@ -691,26 +691,39 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attention_wide_kernel(Attention
     auto compute = [&](int t, auto stage_, auto masked) TW_INLINE {
         constexpr int kStage = decltype(stage_)::value;
         constexpr bool kMasked = decltype(masked)::value;
+        // some row of the wave sees a key of the tile's second half
+        const bool both = !kMasked || __any(last >= keys.begin + t * Shape::kKeys + 32);
         f32x16 sc[2] = {};
         auto key_fragment = [&](int n, int x) TW_INLINE {
             return *reinterpret_cast<const bf16x8 *>(k_frag[x] + kStage * Shape::kStageBytes + n * 32 * Shape::kRowBytes);
         };
-        if constexpr (kAhead > 0) {
-            bf16x8 kf[kAhead];
+        // products [from, to) of the tile's 2 kSteps
+        auto scores = [&](auto from_, auto to_) TW_INLINE {
+            constexpr int kFrom = decltype(from_)::value, kTo = decltype(to_)::value;
+            if constexpr (kAhead > 0) {
+                bf16x8 kf[kAhead];
 #pragma unroll
-            for (int i = 0; i < kAhead; ++i) kf[i] = key_fragment(i / kSteps, i % kSteps);
+                for (int i = kFrom; i < kFrom + kAhead; ++i) kf[i % kAhead] = key_fragment(i / kSteps, i % kSteps);
 #pragma unroll
-            for (int i = 0; i < 2 * kSteps; ++i) {
+                for (int i = kFrom; i < kTo; ++i) {
+                    __builtin_amdgcn_sched_barrier(0);
+                    sc[i / kSteps] = Mfma<32>::run(kf[i % kAhead], qf[i % kSteps], sc[i / kSteps]);
+                    if (i + kAhead < kTo) kf[i % kAhead] = key_fragment((i + kAhead) / kSteps, (i + kAhead) % kSteps);
+                }
                 __builtin_amdgcn_sched_barrier(0);
-                sc[i / kSteps] = Mfma<32>::run(kf[i % kAhead], qf[i % kSteps], sc[i / kSteps]);
-                if (i + kAhead < 2 * kSteps) kf[i % kAhead] = key_fragment((i + kAhead) / kSteps, (i + kAhead) % kSteps);
+            } else {
+#pragma unroll
+                for (int i = kFrom; i < kTo; ++i) sc[i / kSteps] = Mfma<32>::run(key_fragment(i / kSteps, i % kSteps), qf[i % kSteps], sc[i / kSteps]);
             }
-            __builtin_amdgcn_sched_barrier(0);
+        };
+        using First = std::integral_constant<int, 0>;
+        using Half = std::integral_constant<int, kSteps>;
+        using All = std::integral_constant<int, 2 * kSteps>;
+        if constexpr (kMasked) {
+            scores(First{}, Half{});
+            if (both) scores(Half{}, All{});
         } else {
-#pragma unroll
-            for (int n = 0; n < 2; ++n)
-#pragma unroll
-                for (int x = 0; x < kSteps; ++x) sc[n] = Mfma<32>::run(key_fragment(n, x), qf[x], sc[n]);
+            scores(First{}, All{});
         }
         if constexpr (kMasked) {
             const int seen = last - (keys.begin + t * Shape::kKeys) - 4 * half;
@@ -727,8 +740,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attention_wide_kernel(Attention
 #pragma unroll
                 for (int i = 0; i < 16; ++i) o[b][i] *= alpha;
         }
-#pragma unroll
-        for (int t4 = 0; t4 < 4; ++t4) {
+        auto values = [&](int t4) TW_INLINE {
             u32x4 pf;
 #pragma unroll
             for (int i = 0; i < 4; ++i) pf[i] = pack_bf16x2(sc[t4 / 2][(t4 & 1) * 8 + 2 * i], sc[t4 / 2][(t4 & 1) * 8 + 2 * i + 1]);
@@ -745,11 +757,18 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attention_wide_kernel(Attention
                 }
                 o[b] = Mfma<32>::run(__builtin_bit_cast(bf16x8, vf), __builtin_bit_cast(bf16x8, pf), o[b]);
             }
+        };
+        values(0);
+        values(1);
+        if (both) {
+            values(2);
+            values(3);
         }
     };
 
     // Inf and NaN of hidden keys must not meet a p of zero: a tile that is not whole has zeros put in their place, and the rows
-    // that see them get them added behind its step (p > 0 times one of them is the same).
+    // that see them get them added behind its step (p > 0 times one of them is the same). A wave does so to the pieces that it
+    // has loaded itself, before the barrier that makes them everybody's.
     auto clean_values = [&](int t) TW_INLINE {
         char *const mine = lds + (t & 1) * Shape::kStageBytes + Shape::kTileBytes + threadIdx.x * 16;
         uint32_t bad = 0;
@@ -767,13 +786,12 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attention_wide_kernel(Attention
             bad |= here;
         }
         const bool any = __any(bad != 0);
-        if (lane == 0) flags[wave] = any;
-        __syncthreads();
+        if (lane == 0) flags[t & 1][wave] = any;
     };
     auto add_cleaned = [&](int t) TW_INLINE {
         bool infinite = false;
 #pragma unroll
-        for (int w = 0; w < Shape::kWaves; ++w) infinite |= flags[w] != 0;
+        for (int w = 0; w < Shape::kWaves; ++w) infinite |= flags[t & 1][w] != 0;
         if (__builtin_expect(__builtin_amdgcn_readfirstlane(infinite), 0)) {
 #pragma unroll 1
             for (int j = t * Shape::kKeys; j < min((t + 1) * Shape::kKeys, visible); ++j)
@@ -785,10 +803,10 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attention_wide_kernel(Attention
     // Between two barriers the next tile comes in, into the other half of the LDS.
     auto turn = [&](int t, auto stage, auto masked) TW_INLINE {
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        if constexpr (decltype(masked)::value) clean_values(t);
         __syncthreads();
         if (t + 1 < tiles) load_tile(t + 1);
         if constexpr (decltype(masked)::value) {
-            clean_values(t);
             if (!__any(last >= keys.begin + t * Shape::kKeys)) return;
         } else if (!has_rows) {
             return;
@@ -826,9 +844,10 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attention_wide_kernel(Attention
         }
         return;
     }
-    // Results leave by whole rows: a wave's go through its own part of the LDS.
-    __syncthreads();
-    char *const mine = lds + wave * (32 * Shape::kRowBytes);
+    // Results leave by whole rows: a wave's go through the part of the LDS that its rows of q came through, where nobody else
+    // has been if that is no part of a stage.
+    if constexpr (Shape::kQAt < 2 * Shape::kStageBytes) __syncthreads();
+    char *const mine = lds + Shape::kQAt + wave * (32 * Shape::kRowBytes);
     // a row that sees no key has a sum of 0
     const float inv = l == 0.0f ? 0.0f : 1.0f / l;
 #pragma unroll
