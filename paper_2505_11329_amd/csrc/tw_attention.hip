@@ -934,8 +934,8 @@ static AttentionPlan attention_plan(const tw_attention_args &a)
 {
     AttentionPlan plan;
     const int64_t group = a.q_heads / a.kv_heads, list = a.q_rows * group;
-    // Sequences of so few rows on average that tiles of 16 or 32 hold most of them; longer ones among them have more tiles, no more
-    // than there are sequences in all. (4 rows each on average, 64 / 8 heads, keys of up to 1000, 4000, 8000: 4 sequences 17, 17, 26
+    // Sequences of so few rows on average that tiles of 16 or 32 hold most of them; longer ones among them have more tiles, and all
+    // together no more than twice as many as there are sequences. (4 rows each on average, 64 / 8 heads, keys of up to 1000, 4000, 8000: 4 sequences 17, 17, 26
     // us, 23, 27, 30 in the other form; 32 of them 22, -, 99, 29, -, 109.)
     plan.few = list <= 16 * a.n_seqs ? 1 : list <= 32 * a.n_seqs ? 2 : 0;
     // Four waves, two workgroups to a compute unit, where sequences seldom fill tiles of 256 rows or are short, so that a workgroup's
@@ -951,9 +951,9 @@ static AttentionPlan attention_plan(const tw_attention_args &a)
     // unit had one before the cut, and parts cost a second kernel and their sums' way through memory. (One prompt of 1500 tokens,
     // 32 / 8 heads: 43 us whole, 63 in two parts; 512 rows over 8192 keys, 64 / 8 heads: 165 us whole, 141 in two parts, 166 in four;
     // one token over 2500 keys, 32 / 8 heads: 31 us whole, 11 in parts; 16 chunks of 32 rows over up to 8000 keys, 64 / 8 heads:
-    // 140 whole, 107 in two parts.) Of prompts under a causal mask most tiles are short: parts for each compute unit are enough.
+    // 140 whole, 107 in two parts.) Most tiles of causal prompts are short: parts for each compute unit are enough.
     const int64_t tiles = (plan.few ? a.n_seqs : std::max(list / plan.tile_rows + 1, a.n_seqs)) * a.kv_heads, keys = a.k_rows / a.n_seqs;
-    const bool pairs = plan.waves == 4 && !(a.causal && 2 * a.q_rows >= a.k_rows);
+    const bool pairs = plan.waves == 4 && 2 * a.q_rows < a.k_rows;
     const int64_t enough = plan.few || pairs ? 512 : 256, wanted = plan.few ? 2048 : enough;
     plan.min_chunk = plan.few ? 256 : 512;  // (parts of 256, 512 keys of one token over 1500: 10.6, 14.1 us)
     plan.chunks = 1;

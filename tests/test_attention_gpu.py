@@ -245,3 +245,31 @@ def test_streams_workspaces_and_graphs(tw):
         assert torch.equal(out, want[0][0]) and torch.equal(lse, want[0][1]) and torch.equal(other[0], want[1][0])
         q.copy_(cases[1][0] if n % 2 == 0 else inputs([1, 1, 1], [3000, 40, 1800], 8, 2, 128, seed=1)[0])
         want[0] = tw.attention(*cases[0])
+
+
+@pytest.mark.parametrize("rows,batches", [
+    (8, [([1] * 8, [40] * 7 + [2900]), ([1] * 5 + [0] * 3, [9, 3000, 1, 33, 64, 0, 0, 0]), ([0, 4, 0, 1, 3, 0, 0, 0], [5, 900, 0, 1, 700, 0, 2, 0])]),
+    (400, [([100] * 4, [100] * 4), ([0, 1, 0, 380], [60, 77, 0, 400]), ([400, 0, 0, 0], [450, 0, 0, 1])]),
+])
+def test_a_captured_call_replayed_with_other_offsets(tw, rows, batches):
+    """The launch depends on the tensors' sizes alone: a graph serves every batch that fits them."""
+    n, keys = len(batches[0][0]), max(sum(k) for _, k in batches)
+    q, k, v, qo, ko = inputs([rows] + [0] * (n - 1), [keys] + [0] * (n - 1), 8, 2, 64, seed=6)
+    out, lse = torch.zeros_like(q), torch.zeros(q.shape[:2], device="cuda")
+    space = torch.empty(tw.attention_workspace_bytes(n, rows, keys, 8, 2, 64), dtype=torch.uint8, device="cuda")
+    tw.attention(q, k, v, qo, ko, out=out, lse=lse, workspace=space)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        tw.attention(q, k, v, qo, ko, out=out, lse=lse, workspace=space)
+    for q_lens, k_lens in batches + batches[:1]:
+        qo.copy_(R.offsets(q_lens))
+        ko.copy_(R.offsets(k_lens))
+        out.fill_(3.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        got, got_lse = out.clone(), lse.clone()
+        want, want_lse = check(tw, q, k, v, qo, ko, what=str(q_lens))
+        end = sum(q_lens)
+        assert torch.equal(got[:end], want[:end]) and torch.equal(got_lse[:end], want_lse[:end])
+        assert bool((got[end:] == 3).all())
