@@ -373,8 +373,9 @@ __global__ __launch_bounds__(256, 2) void attention_few_kernel(AttentionParams p
     const int rest = blockIdx.x / p.kv_heads;
     const int chunk = rest % p.chunks, i = rest / p.chunks;
     Place at = {};
+    const Sequence own = sequence(p, min(i, p.n_seqs - 1));
     if (p.group > Shape::kRows || !single_tokens(p)) at = find_place<Shape::kRows>(p, i);
-    else if (i < p.n_seqs) at.s = sequence(p, i);
+    else if (i < p.n_seqs) at.s = own;
     const Sequence &s = at.s;
     const int list = s.q_len * p.group, r0 = at.tile * Shape::kRows;
     if (r0 >= list) return;  // (no tile is left for this workgroup)
@@ -871,40 +872,45 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attention_wide_kernel(Attention
 // The chunks of one row and head joined: a wave each, lane c of it with chunk c's maximum and sum.
 __global__ __launch_bounds__(256) void attention_join_kernel(AttentionParams p)
 {
-    const int lane = threadIdx.x & 63;
+    const int lane = threadIdx.x & 63, c0 = lane * 2;
     const int64_t at = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6);
     const int64_t row = at / p.q_heads;
-    // rows of no sequence stay as they are
-    if (row >= p.q_rows || row < p.q_offsets[0] || row >= p.q_offsets[p.n_seqs]) return;
+    if (row >= p.q_rows) return;
+    // Everything is asked for at once: whether the row is one of a sequence, and which chunks have columns, comes with them.
+    const int first = p.q_offsets[0], end = p.q_offsets[p.n_seqs];
     const int64_t step = p.q_rows * p.q_heads;
     float m = kMinusInf, l = 0.0f;
     if (lane < p.chunks) {
         m = p.part_ml[(lane * step + at) * 2];
         l = p.part_ml[(lane * step + at) * 2 + 1];
     }
+    float2 x[8];
+    auto load_columns = [&](int c) TW_INLINE {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            x[i] = {0.0f, 0.0f};
+            if (c0 < p.dim && c + i < p.chunks) x[i] = *reinterpret_cast<const float2 *>(p.part + ((c + i) * step + at) * p.dim + c0);
+        }
+    };
+    load_columns(0);
     const bool empty = m == kMinusInf;
     float top = m;
     for (int d = 32; d; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
     const float f = empty ? 0.0f : __builtin_amdgcn_exp2f(m - top);
     const float sum = group_sum(empty && l == 0.0f ? 0.0f : f * l, 6);
-    const int c0 = lane * 2;
     float a = 0.0f, b = 0.0f;
     const uint64_t live = __ballot(!(empty && l == 0.0f));  // (the others' columns were not put)
-    for (int c = 0; c < p.chunks; c += 8) {  // eight loads under way
-        float2 x[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            x[i] = {0.0f, 0.0f};
-            if (c0 < p.dim && c + i < p.chunks && (live >> (c + i)) & 1)
-                x[i] = *reinterpret_cast<const float2 *>(p.part + ((c + i) * step + at) * p.dim + c0);
-        }
+    for (int c = 0; c < p.chunks; c += 8) {
+        if (c > 0) load_columns(c);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             const float w = __shfl(f, (c + i) & 63);
-            a = fmaf(w, x[i].x, a);
-            b = fmaf(w, x[i].y, b);
+            const bool put = (live >> (c + i)) & 1;
+            a = fmaf(w, put ? x[i].x : 0.0f, a);
+            b = fmaf(w, put ? x[i].y : 0.0f, b);
         }
     }
+    if (row < first || row >= end) return;  // rows of no sequence stay as they are
     const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
     if (p.lse && lane == 0) p.lse[at] = sum == 0.0f ? kMinusInf : (top + __builtin_amdgcn_logf(sum)) * kLn2;
     if (c0 < p.dim)
