@@ -150,8 +150,9 @@ __global__ __launch_bounds__(64 * WAVES) void expert_place_kernel(SortParams p)
 
 // ---- rows ----
 //
-// All of these are bound by memory: 16 bytes of a row to a thread, 2^row_log2 threads to a row of up to 2048 elements and
-// 256 to a longer one.
+// All of these are bound by memory: 16 bytes of a row to a thread, 2^row_log2 threads to a row of up to 2048 elements. Longer rows
+// are cut into parts of 2048 for workgroups of their own (16 tokens of 8 rows of 7168 summed: 4.9 us, 10.2 by one workgroup each, 6.3
+// by two; 16384 of 2 rows of 8192: 139, 145), but for the backward pass, whose dot products need whole rows.
 
 struct RowsParams {
     const char *in;       // x | y | dout
@@ -198,7 +199,11 @@ __device__ __forceinline__ void places(const RowsParams &p, int64_t token, int k
     }
 }
 
-// The token that this thread's row is of.
+// This thread's piece of its row, and the token that the row is of.
+__device__ __forceinline__ int row_part(const RowsParams &p)
+{
+    return (blockIdx.y << p.row_log2) + (threadIdx.x & ((1 << p.row_log2) - 1));
+}
 __device__ __forceinline__ int64_t row_token(const RowsParams &p)
 {
     return p.first + static_cast<int64_t>(blockIdx.x) * (256 >> p.row_log2) + (threadIdx.x >> p.row_log2);
@@ -207,52 +212,48 @@ __device__ __forceinline__ int64_t row_token(const RowsParams &p)
 template <bool STREAMED>
 __global__ __launch_bounds__(256) void expert_dispatch_kernel(RowsParams p)
 {
-    const int threads = 1 << p.row_log2;
+    const int c = row_part(p);
     const int64_t token = row_token(p);
-    if (token >= p.tokens) return;
+    if (token >= p.tokens || c >= p.pieces) return;
+    const u32x4 x = row_piece<false>(p.in, token, p.pieces, c);
     for (int k0 = 0; k0 < p.top_k; k0 += kMost) {
         int32_t at[kMost];
         places(p, token, k0, at);
-        for (int c = threadIdx.x & (threads - 1); c < p.pieces; c += threads) {
-            const u32x4 x = row_piece<false>(p.in, token, p.pieces, c);
 #pragma unroll
-            for (int k = 0; k < kMost; ++k)
-                if (at[k] >= 0) put_piece<STREAMED>(p.out, at[k], p.pieces, c, x);
-        }
+        for (int k = 0; k < kMost; ++k)
+            if (at[k] >= 0) put_piece<STREAMED>(p.out, at[k], p.pieces, c, x);
     }
 }
 
 template <bool WEIGHTED, bool STREAMED>
 __global__ __launch_bounds__(256) void expert_combine_kernel(RowsParams p)
 {
-    const int threads = 1 << p.row_log2;
+    const int c = row_part(p);
     const int64_t token = row_token(p);
-    if (token >= p.tokens) return;
-    for (int c = threadIdx.x & (threads - 1); c < p.pieces; c += threads) {
-        float sum[8] = {};
-        for (int k0 = 0; k0 < p.top_k; k0 += kMost) {
-            int32_t at[kMost];
-            places(p, token, k0, at);
-            u32x4 v[kMost] = {};
+    if (token >= p.tokens || c >= p.pieces) return;
+    float sum[8] = {};
+    for (int k0 = 0; k0 < p.top_k; k0 += kMost) {
+        int32_t at[kMost];
+        places(p, token, k0, at);
+        u32x4 v[kMost] = {};
 #pragma unroll
-            for (int k = 0; k < kMost; ++k)
-                if (at[k] >= 0) v[k] = row_piece<true>(p.in, at[k], p.pieces, c);
+        for (int k = 0; k < kMost; ++k)
+            if (at[k] >= 0) v[k] = row_piece<true>(p.in, at[k], p.pieces, c);
 #pragma unroll
-            for (int k = 0; k < kMost; ++k) {
-                if (at[k] < 0) continue;
-                if constexpr (WEIGHTED) {
-                    const float w = p.weights[token * p.top_k + k0 + k];
-                    float f[8];
-                    unpack8(v[k], f);
+        for (int k = 0; k < kMost; ++k) {
+            if (at[k] < 0) continue;
+            if constexpr (WEIGHTED) {
+                const float w = p.weights[token * p.top_k + k0 + k];
+                float f[8];
+                unpack8(v[k], f);
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) sum[i] = fmaf(w, f[i], sum[i]);
-                } else {
-                    add8(v[k], sum);
-                }
+                for (int i = 0; i < 8; ++i) sum[i] = fmaf(w, f[i], sum[i]);
+            } else {
+                add8(v[k], sum);
             }
         }
-        put_piece<STREAMED>(p.out, token, p.pieces, c, pack8(sum));
     }
+    put_piece<STREAMED>(p.out, token, p.pieces, c, pack8(sum));
 }
 
 template <bool STREAMED>
@@ -352,13 +353,15 @@ static void row_layout(int64_t H, RowsParams *p)
     p->row_log2 = std::max(p->row_log2, 3);  // eight threads at least: one to each pair's gradient
 }
 
-static tw_status launch_rows(void (*kernel)(RowsParams), const RowsParams &p, void *stream)
+// `cut`: workgroups for parts of a row.
+static tw_status launch_rows(void (*kernel)(RowsParams), const RowsParams &p, bool cut, void *stream)
 {
     // a launch has fewer than 2^32 threads
-    const int64_t per_group = 256 >> p.row_log2, most = int64_t(1) << 23;
+    const int64_t per_group = 256 >> p.row_log2, parts = cut ? (p.pieces + 255) / 256 : 1, most = (int64_t(1) << 23) / parts;
     RowsParams part = p;
     for (int64_t groups = (p.tokens + per_group - 1) / per_group; groups > 0; groups -= most) {
-        TW_HIP(launch_kernel(kernel, dim3(static_cast<uint32_t>(std::min(groups, most))), dim3(256), 0, static_cast<hipStream_t>(stream), part));
+        const dim3 grid(static_cast<uint32_t>(std::min(groups, most)), static_cast<uint32_t>(parts));
+        TW_HIP(launch_kernel(kernel, grid, dim3(256), 0, static_cast<hipStream_t>(stream), part));
         part.first += most * per_group;
     }
     return TW_OK;
@@ -445,7 +448,7 @@ tw_status tw_expert_dispatch(const void *x, const int32_t *position, int64_t N, 
     p.rows = rows;
     p.top_k = top_k;
     row_layout(H, &p);
-    return launch_rows(streamed(rows_b) ? expert_dispatch_kernel<true> : expert_dispatch_kernel<false>, p, stream);
+    return launch_rows(streamed(rows_b) ? expert_dispatch_kernel<true> : expert_dispatch_kernel<false>, p, true, stream);
 }
 
 tw_status tw_expert_combine(const void *y, int64_t rows, const int32_t *position, const float *weights, int64_t N,
@@ -470,8 +473,8 @@ tw_status tw_expert_combine(const void *y, int64_t rows, const int32_t *position
     p.top_k = top_k;
     row_layout(H, &p);
     if (streamed(tokens_b))
-        return launch_rows(weights ? expert_combine_kernel<true, true> : expert_combine_kernel<false, true>, p, stream);
-    return launch_rows(weights ? expert_combine_kernel<true, false> : expert_combine_kernel<false, false>, p, stream);
+        return launch_rows(weights ? expert_combine_kernel<true, true> : expert_combine_kernel<false, true>, p, true, stream);
+    return launch_rows(weights ? expert_combine_kernel<true, false> : expert_combine_kernel<false, false>, p, true, stream);
 }
 
 tw_status tw_expert_combine_backward(const void *dout, const void *y, int64_t rows, const int32_t *position,
@@ -505,7 +508,7 @@ tw_status tw_expert_combine_backward(const void *dout, const void *y, int64_t ro
     p.rows = rows;
     p.top_k = top_k;
     row_layout(H, &p);
-    return launch_rows(streamed(rows_b) ? expert_combine_backward_kernel<true> : expert_combine_backward_kernel<false>, p, stream);
+    return launch_rows(streamed(rows_b) ? expert_combine_backward_kernel<true> : expert_combine_backward_kernel<false>, p, false, stream);
 }
 
 }  // extern "C"
