@@ -199,6 +199,13 @@ __device__ __forceinline__ void places(const RowsParams &p, int64_t token, int k
     }
 }
 
+// Their weights, those of pairs without a place among them, so that nothing waits for the places.
+__device__ __forceinline__ void weights(const RowsParams &p, int64_t token, int k0, float (&w)[kMost])
+{
+#pragma unroll
+    for (int k = 0; k < kMost; ++k) w[k] = k0 + k < p.top_k ? p.weights[token * p.top_k + k0 + k] : 0.0f;
+}
+
 // This thread's piece of its row, and the token that the row is of.
 __device__ __forceinline__ int row_part(const RowsParams &p)
 {
@@ -234,6 +241,8 @@ __global__ __launch_bounds__(256) void expert_combine_kernel(RowsParams p)
     float sum[8] = {};
     for (int k0 = 0; k0 < p.top_k; k0 += kMost) {
         int32_t at[kMost];
+        float w[kMost];
+        if constexpr (WEIGHTED) weights(p, token, k0, w);
         places(p, token, k0, at);
         u32x4 v[kMost] = {};
 #pragma unroll
@@ -243,11 +252,10 @@ __global__ __launch_bounds__(256) void expert_combine_kernel(RowsParams p)
         for (int k = 0; k < kMost; ++k) {
             if (at[k] < 0) continue;
             if constexpr (WEIGHTED) {
-                const float w = p.weights[token * p.top_k + k0 + k];
                 float f[8];
                 unpack8(v[k], f);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) sum[i] = fmaf(w, f[i], sum[i]);
+                for (int i = 0; i < 8; ++i) sum[i] = fmaf(w[k], f[i], sum[i]);
             } else {
                 add8(v[k], sum);
             }
@@ -265,12 +273,13 @@ __global__ __launch_bounds__(256) void expert_combine_backward_kernel(RowsParams
     const bool has = token < p.tokens;
     for (int k0 = 0; k0 < p.top_k; k0 += kMost) {
         int32_t at[kMost];
-        float w[kMost], dot[kMost] = {};
+        float w[kMost] = {}, dot[kMost] = {};
 #pragma unroll
         for (int k = 0; k < kMost; ++k) at[k] = -1;
-        if (has) places(p, token, k0, at);
-#pragma unroll
-        for (int k = 0; k < kMost; ++k) w[k] = at[k] >= 0 ? p.weights[token * p.top_k + k0 + k] : 0.0f;
+        if (has) {
+            weights(p, token, k0, w);
+            places(p, token, k0, at);
+        }
         if (has)
             for (int c = in_row; c < p.pieces; c += threads) {
                 float d[8];
