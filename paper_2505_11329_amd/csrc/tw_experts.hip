@@ -167,7 +167,7 @@ struct RowsParams {
     int row_log2;
 };
 
-static constexpr int kMost = 8;  // pairs of a token that are worked on at a time
+static constexpr int kMost = 8;  // most pairs of a token that are worked on at a time
 
 // Experts' rows are read once and not kept in the caches (the gradient of a dispatch, 2531 tokens of 8 rows of 5120: 50 us with
 // ordinary loads, 46 so). Results of more than half of what the last-level cache holds are not kept either (STREAMED; 8101 tokens
@@ -186,11 +186,12 @@ __device__ __forceinline__ void put_piece(char *base, int64_t row, int pieces, i
     else *to = v;
 }
 
-// The places of pairs [k0, k0 + kMost) of a token, -1 for none.
-__device__ __forceinline__ void places(const RowsParams &p, int64_t token, int k0, int32_t (&at)[kMost])
+// The places of pairs [k0, k0 + N) of a token, -1 for none.
+template <int N>
+__device__ __forceinline__ void places(const RowsParams &p, int64_t token, int k0, int32_t (&at)[N])
 {
 #pragma unroll
-    for (int k = 0; k < kMost; ++k) {
+    for (int k = 0; k < N; ++k) {
         at[k] = -1;
         if (k0 + k < p.top_k) {
             const int32_t s = p.position[token * p.top_k + k0 + k];
@@ -200,10 +201,11 @@ __device__ __forceinline__ void places(const RowsParams &p, int64_t token, int k
 }
 
 // Their weights, those of pairs without a place among them, so that nothing waits for the places.
-__device__ __forceinline__ void weights(const RowsParams &p, int64_t token, int k0, float (&w)[kMost])
+template <int N>
+__device__ __forceinline__ void weights(const RowsParams &p, int64_t token, int k0, float (&w)[N])
 {
 #pragma unroll
-    for (int k = 0; k < kMost; ++k) w[k] = k0 + k < p.top_k ? p.weights[token * p.top_k + k0 + k] : 0.0f;
+    for (int k = 0; k < N; ++k) w[k] = k0 + k < p.top_k ? p.weights[token * p.top_k + k0 + k] : 0.0f;
 }
 
 // This thread's piece of its row, and the token that the row is of.
@@ -264,32 +266,30 @@ __global__ __launch_bounds__(256) void expert_combine_kernel(RowsParams p)
     put_piece<STREAMED>(p.out, token, p.pieces, c, pack8(sum));
 }
 
-template <bool STREAMED>
+template <bool STREAMED, int PAIRS>
 __global__ __launch_bounds__(256) void expert_combine_backward_kernel(RowsParams p)
 {
-    __shared__ float wave_dot[4][kMost];
+    __shared__ float wave_dot[4][PAIRS];
     const int threads = 1 << p.row_log2, in_row = threadIdx.x & (threads - 1);
     const int64_t token = row_token(p);
     const bool has = token < p.tokens;
-    for (int k0 = 0; k0 < p.top_k; k0 += kMost) {
-        int32_t at[kMost];
-        float w[kMost] = {}, dot[kMost] = {};
+    for (int k0 = blockIdx.y * PAIRS; k0 < p.top_k; k0 += gridDim.y * PAIRS) {
+        int32_t at[PAIRS];
+        float w[PAIRS] = {}, dot[PAIRS] = {};
 #pragma unroll
-        for (int k = 0; k < kMost; ++k) at[k] = -1;
+        for (int k = 0; k < PAIRS; ++k) at[k] = -1;
         if (has) {
             weights(p, token, k0, w);
             places(p, token, k0, at);
-        }
-        if (has)
             for (int c = in_row; c < p.pieces; c += threads) {
                 float d[8];
                 unpack8(row_piece<false>(p.in, token, p.pieces, c), d);
-                u32x4 v[kMost] = {};
+                u32x4 v[PAIRS] = {};
 #pragma unroll
-                for (int k = 0; k < kMost; ++k)
+                for (int k = 0; k < PAIRS; ++k)
                     if (at[k] >= 0) v[k] = row_piece<true>(p.y, at[k], p.pieces, c);
 #pragma unroll
-                for (int k = 0; k < kMost; ++k) {
+                for (int k = 0; k < PAIRS; ++k) {
                     if (at[k] < 0) continue;
                     float f[8];
                     unpack8(v[k], f);
@@ -301,17 +301,18 @@ __global__ __launch_bounds__(256) void expert_combine_backward_kernel(RowsParams
                     put_piece<STREAMED>(p.out, at[k], p.pieces, c, pack8(f));
                 }
             }
+        }
         // a row's dot products: over its lanes, then over its waves in order
 #pragma unroll
-        for (int k = 0; k < kMost; ++k) dot[k] = group_sum(dot[k], min(p.row_log2, 6));
+        for (int k = 0; k < PAIRS; ++k) dot[k] = group_sum(dot[k], min(p.row_log2, 6));
         if (p.row_log2 > 6) {
             if ((threadIdx.x & 63) == 0)
 #pragma unroll
-                for (int k = 0; k < kMost; ++k) wave_dot[threadIdx.x >> 6][k] = dot[k];
+                for (int k = 0; k < PAIRS; ++k) wave_dot[threadIdx.x >> 6][k] = dot[k];
             __syncthreads();
             const int first = (threadIdx.x >> p.row_log2) << (p.row_log2 - 6);
 #pragma unroll
-            for (int k = 0; k < kMost; ++k) {
+            for (int k = 0; k < PAIRS; ++k) {
                 dot[k] = wave_dot[first][k];
                 for (int w2 = 1; w2 < threads / 64; ++w2) dot[k] += wave_dot[first + w2][k];
             }
@@ -319,7 +320,7 @@ __global__ __launch_bounds__(256) void expert_combine_backward_kernel(RowsParams
         }
         if (has)
 #pragma unroll
-            for (int k = 0; k < kMost; ++k)
+            for (int k = 0; k < PAIRS; ++k)
                 if (in_row == k && k0 + k < p.top_k) p.dweights[token * p.top_k + k0 + k] = dot[k];
     }
 }
@@ -362,19 +363,24 @@ static void row_layout(int64_t H, RowsParams *p)
     p->row_log2 = std::max(p->row_log2, 3);  // eight threads at least: one to each pair's gradient
 }
 
-// `cut`: workgroups for parts of a row.
-static tw_status launch_rows(void (*kernel)(RowsParams), const RowsParams &p, bool cut, void *stream)
+// Workgroups of a launch: for groups of rows, and `parts` for the parts of each.
+static int64_t row_groups(const RowsParams &p) { return (p.tokens + (256 >> p.row_log2) - 1) / (256 >> p.row_log2); }
+
+static tw_status launch_rows(void (*kernel)(RowsParams), const RowsParams &p, int parts, void *stream)
 {
     // a launch has fewer than 2^32 threads
-    const int64_t per_group = 256 >> p.row_log2, parts = cut ? (p.pieces + 255) / 256 : 1, most = (int64_t(1) << 23) / parts;
+    const int64_t most = (int64_t(1) << 23) / parts;
     RowsParams part = p;
-    for (int64_t groups = (p.tokens + per_group - 1) / per_group; groups > 0; groups -= most) {
+    for (int64_t groups = row_groups(p); groups > 0; groups -= most) {
         const dim3 grid(static_cast<uint32_t>(std::min(groups, most)), static_cast<uint32_t>(parts));
         TW_HIP(launch_kernel(kernel, grid, dim3(256), 0, static_cast<hipStream_t>(stream), part));
-        part.first += most * per_group;
+        part.first += most * (256 >> p.row_log2);
     }
     return TW_OK;
 }
+
+// Parts of a row of up to 256 pieces.
+static int row_parts(const RowsParams &p) { return (p.pieces + 255) / 256; }
 
 template <typename Id>
 static tw_status launch_sort(const SortParams &p, int64_t runs, hipStream_t stream)
@@ -457,7 +463,7 @@ tw_status tw_expert_dispatch(const void *x, const int32_t *position, int64_t N, 
     p.rows = rows;
     p.top_k = top_k;
     row_layout(H, &p);
-    return launch_rows(streamed(rows_b) ? expert_dispatch_kernel<true> : expert_dispatch_kernel<false>, p, true, stream);
+    return launch_rows(streamed(rows_b) ? expert_dispatch_kernel<true> : expert_dispatch_kernel<false>, p, row_parts(p), stream);
 }
 
 tw_status tw_expert_combine(const void *y, int64_t rows, const int32_t *position, const float *weights, int64_t N,
@@ -482,8 +488,8 @@ tw_status tw_expert_combine(const void *y, int64_t rows, const int32_t *position
     p.top_k = top_k;
     row_layout(H, &p);
     if (streamed(tokens_b))
-        return launch_rows(weights ? expert_combine_kernel<true, true> : expert_combine_kernel<false, true>, p, true, stream);
-    return launch_rows(weights ? expert_combine_kernel<true, false> : expert_combine_kernel<false, false>, p, true, stream);
+        return launch_rows(weights ? expert_combine_kernel<true, true> : expert_combine_kernel<false, true>, p, row_parts(p), stream);
+    return launch_rows(weights ? expert_combine_kernel<true, false> : expert_combine_kernel<false, false>, p, row_parts(p), stream);
 }
 
 tw_status tw_expert_combine_backward(const void *dout, const void *y, int64_t rows, const int32_t *position,
@@ -517,7 +523,11 @@ tw_status tw_expert_combine_backward(const void *dout, const void *y, int64_t ro
     p.rows = rows;
     p.top_k = top_k;
     row_layout(H, &p);
-    return launch_rows(streamed(rows_b) ? expert_combine_backward_kernel<true> : expert_combine_backward_kernel<false>, p, false, stream);
+    // Results that stay in the caches: workgroups for one or two of a token's pairs, which all find dout there (64 tokens of 8 rows of
+    // 4096: 4.7 us with one, 5.3 with two, 8.3 with eight; 1500 tokens 47, 45, 47; 8192, whose results do not stay, 251, 234, 211).
+    if (streamed(rows_b)) return launch_rows(expert_combine_backward_kernel<true, kMost>, p, 1, stream);
+    if (row_groups(p) * top_k <= 4096) return launch_rows(expert_combine_backward_kernel<false, 1>, p, top_k, stream);
+    return launch_rows(expert_combine_backward_kernel<false, 2>, p, (top_k + 1) / 2, stream);
 }
 
 }  // extern "C"
