@@ -96,6 +96,22 @@ def test_combine_backward(tw, N, K, E, H):
     assert torch.equal(in_place[has], dy[has])
 
 
+@pytest.mark.parametrize("N,K,E,H", [(1400, 3, 16, 2056),      # two pairs to a workgroup, the last of them alone
+                                     (2100, 4, 8, 8192)])      # more than the caches keep
+def test_many_rows_out_and_back(tw, N, K, E, H):
+    position, x, y, w = routed(N, K, E, H)
+    dy = torch.full_like(y, math.nan)
+    _, dw = tw.expert_combine_backward(x, y, position, w, dy=dy)
+    want, tol, want_w, tol_w = R.combine_backward(x, y, position, w)
+    R.assert_close(dy, want, tol, "dy")
+    R.assert_close(dw, want_w, tol_w, "dweights")
+    out = torch.zeros_like(y)
+    tw.expert_dispatch(x, position, out=out)
+    has = position >= 0
+    assert torch.equal(out[position[has].long()], x[:, None].expand(N, K, H)[has])
+    assert int((out != 0).any(dim=1).sum()) == int(has.sum())
+
+
 def test_gradients_against_differences(tw):
     """Both are gradients of sums that are linear in each argument: central differences in 64 bits are exact but for
     rounding (values below 2^6 and steps of 1: 2^-40 at most)."""
