@@ -961,7 +961,9 @@ static AttentionPlan attention_plan(const tw_attention_args &a)
     const int64_t tiles = (plan.few ? a.n_seqs : std::max(list / plan.tile_rows + 1, a.n_seqs)) * a.kv_heads, keys = a.k_rows / a.n_seqs;
     const bool pairs = plan.waves == 4 && 2 * a.q_rows < a.k_rows;
     const int64_t enough = plan.few || pairs ? 512 : 256, wanted = plan.few ? 2048 : enough;
-    plan.min_chunk = plan.few ? 256 : 512;  // (parts of 256, 512 keys of one token over 1500: 10.6, 14.1 us)
+    // (Parts of at least 128, 256, 512 keys: one token over 1500, 32 / 8 heads, 10.6, 10.6, 14.1 us, 8 over up to 800 15.4, 13.5, 17.6; 16
+    // rows over 2000, 32 / 8 heads of 128, 14.7, 15.6, 18.9, 16 rows of 4 sequences each 17, 21, 27.)
+    plan.min_chunk = plan.few ? 256 : 128;
     plan.chunks = 1;
     if (tiles < enough) {
         const int64_t most = std::min<int64_t>({kMostChunks, (wanted + tiles - 1) / tiles, (keys + plan.min_chunk - 1) / plan.min_chunk});
