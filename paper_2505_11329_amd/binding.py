@@ -473,7 +473,8 @@ def weave_layer_auto(X1, W1, partials, residual, weight, eps, W2, stream_compute
 def attention(q, k, v, q_offsets, k_offsets, causal=True, scale=None, out=None, lse=None, workspace=None, stream=None):
     """tw_attention: q [rows, q_heads, head_dim], k and v [k_rows, kv_heads, head_dim], whose rows may be strided (columns of
     one projection's output), offsets int32 [n_seqs + 1]. scale None: 1 / sqrt(head_dim). Returns (out, lse); rows of no
-    sequence are not written in either. workspace None: from torch's allocator, for this call's stream."""
+    sequence are not written in either. workspace None: from torch's allocator, for this call's stream; out and lse that the
+    call makes are torch's current stream's, as with the other calls."""
     return (_native or native()).attention(q, k, v, q_offsets, k_offsets, causal, scale, out, lse, workspace, stream)
 
 

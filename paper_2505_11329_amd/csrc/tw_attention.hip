@@ -10,7 +10,7 @@
 // free, and V's fragments are read in the order that S^T leaves them in (four keys of one column to a lane by the
 // transposing LDS read).
 //   p = 2^(s c - m), c = scale / ln 2, m the row's maximum of s c; l = sum p; out = (sum p v) / l; lse = (m + log2 l) ln 2
-// p is rounded to bf16 for the product with v, as an operand of the matrix cores has to be (relative 2^-9 each, the
+// p is rounded to bf16 for the product with v, as an operand of the matrix cores has to be (relative 2^-8 each, the
 // sum over keys is in fp32); l sums the unrounded p in fp32.
 #include <algorithm>
 
@@ -343,7 +343,7 @@ __device__ __forceinline__ bool single_tokens(const AttentionParams &p)
 // by what comes from memory. Each wave has keys of its own, 32 at a time, and a place in the LDS for them: the next ones are
 // asked for as soon as a product has read the ones before, and nothing but the result ties the waves to each other. Two
 // workgroups to a compute unit keep up to 128 KB on their way. Where a tile has all of its sequence's rows its keys are not kept in
-// the caches: 48 tokens over 6000 keys, 64 / 8 heads, 115 us, 131 if kept; 4 tokens over 8192 keys 19.3, 21.1.
+// the caches: 48 tokens over 6000 keys, 64 / 8 heads, 107 us, 122 if kept; 4 tokens over 8192 keys 20.9, 22.0.
 template <int DP, int RB>
 struct FewShape {
     static constexpr int kWaves = 4, kThreads = 64 * kWaves, kRows = 16 * RB, kKeys = 32;
@@ -714,7 +714,8 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attention_wide_kernel(Attention
                 __builtin_amdgcn_sched_barrier(0);
             } else {
 #pragma unroll
-                for (int i = kFrom; i < kTo; ++i) sc[i / kSteps] = Mfma<32>::run(key_fragment(i / kSteps, i % kSteps), qf[i % kSteps], sc[i / kSteps]);
+                for (int i = kFrom; i < kTo; ++i)
+                    sc[i / kSteps] = Mfma<32>::run(key_fragment(i / kSteps, i % kSteps), qf[i % kSteps], sc[i / kSteps]);
             }
         };
         using First = std::integral_constant<int, 0>;
@@ -941,8 +942,8 @@ static AttentionPlan attention_plan(const tw_attention_args &a)
     AttentionPlan plan;
     const int64_t group = a.q_heads / a.kv_heads, list = a.q_rows * group;
     // Sequences of so few rows on average that tiles of 16 or 32 hold most of them; longer ones among them have more tiles, and all
-    // together no more than twice as many as there are sequences. (4 rows each on average, 64 / 8 heads, keys of up to 1000, 4000, 8000: 4 sequences 17, 17, 26
-    // us, 23, 27, 30 in the other form; 32 of them 22, -, 99, 29, -, 109.)
+    // together no more than twice as many as there are sequences. (4 rows each on average, 64 / 8 heads: 4 sequences with up to 1000,
+    // 2000, 8000 keys 17, 17, 26 us, 23, 27, 30 in the other form; 32 of them with up to 1000, 8000 keys 22, 99, 29, 109.)
     plan.few = list <= 16 * a.n_seqs ? 1 : list <= 32 * a.n_seqs ? 2 : 0;
     // Four waves, two workgroups to a compute unit, where sequences seldom fill tiles of 256 rows or are short, so that a workgroup's
     // start, search and results are much of its time, beside which the second one works (16 heads of 128, prompts of up to 128 tokens
