@@ -329,11 +329,12 @@ __device__ __forceinline__ Place find_place(const AttentionParams &p, int i)
     return at;
 }
 
-// Whether every sequence has one query row, but for empty ones behind all others: the i-th tile is then the i-th sequence's.
+// Whether the rows are single tokens of the first sequences, one each, and the sequences behind have none: the i-th tile is then
+// the i-th sequence's. (Every start is looked at; that the rows are no more than the sequences bounds the last one's.)
 __device__ __forceinline__ bool single_tokens(const AttentionParams &p)
 {
     const int lane = threadIdx.x & 63, first = p.q_offsets[0], rows = p.q_offsets[p.n_seqs] - first;
-    bool single = true;
+    bool single = rows <= p.n_seqs;
 #pragma unroll 8
     for (int b = lane; b < p.n_seqs; b += 64) single &= p.q_offsets[b] - first == min(b, rows);
     return __all(single);

@@ -273,3 +273,49 @@ def test_a_captured_call_replayed_with_other_offsets(tw, rows, batches):
         end = sum(q_lens)
         assert torch.equal(got[:end], want[:end]) and torch.equal(got_lse[:end], want_lse[:end])
         assert bool((got[end:] == 3).all())
+
+
+@pytest.mark.parametrize("q_lens,heads,kv_heads,dim,past", [
+    ([1, 5], 32, 8, 128, (0, 40)), ([1, 3], 64, 8, 64, (5, 0)), ([1, 1, 3], 64, 8, 128, (900, 12)), ([1, 7], 24, 8, 80, (30, 3000)),
+    ([1] * 61 + [5], 8, 1, 64, (7, 90)), ([1] * 40 + [20], 16, 4, 72, (300, 0)), ([1] * 47 + [41], 16, 2, 128, (60, 2000)),
+    ([1] * 99 + [60], 16, 2, 64, (33, 500)), ([1] * 256 + [1024], 8, 2, 128, (100, 0)), ([1] * 7 + [2], 23, 1, 128, (2500, 2500)),
+])
+@pytest.mark.parametrize("spare", [0, 1])
+def test_single_tokens_and_a_longer_sequence_behind_them(tw, q_lens, heads, kv_heads, dim, past, spare):
+    """The form for few rows, whose tiles are the sequences one by one only where every one of them has a single row."""
+    k_lens = [n + past[i == len(q_lens) - 1] for i, n in enumerate(q_lens)]
+    q, k, v, qo, ko = inputs(q_lens, k_lens, heads, kv_heads, dim, seed=12, tail=spare)
+    sizes = len(q_lens), q.shape[0], k.shape[0], heads, kv_heads, dim
+    assert tw.attention_plan(*sizes).key_waves == 4
+    for causal in (True, False):
+        print(q_lens[:3], len(q_lens), causal, flush=True)
+        out, lse = torch.full_like(q, math.nan), torch.full(q.shape[:2], math.nan, device="cuda")
+        space = torch.full((tw.attention_workspace_bytes(*sizes),), 255, dtype=torch.uint8, device="cuda")   # NaN, too
+        check(tw, q, k, v, qo, ko, causal=causal, out=out, lse=lse, workspace=space, what="%s %s" % (q_lens[-1], causal))
+
+
+@pytest.mark.parametrize("group,most", [(4, 70), (8, 700)])
+def test_a_captured_call_of_single_tokens_replayed_with_a_longer_sequence_behind_them(tw, group, most):
+    n, rows, keys = 40, 78, 40 * most + 100
+    q, k, v, qo, ko = inputs([rows] + [0] * (n - 1), [keys] + [0] * (n - 1), group, 1, 64, seed=8)
+    out, lse = torch.zeros_like(q), torch.zeros(q.shape[:2], device="cuda")
+    space = torch.full((tw.attention_workspace_bytes(n, rows, keys, group, 1, 64),), 255, dtype=torch.uint8, device="cuda")
+    assert tw.attention_plan(n, rows, keys, group, 1, 64).key_waves == 4
+    tw.attention(q, k, v, qo, ko, out=out, lse=lse, workspace=space)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        tw.attention(q, k, v, qo, ko, out=out, lse=lse, workspace=space)
+    for q_lens in ([1] * n, [1] * (n - 1) + [39], [1] * 20 + [0] * 20, [1] * (n - 1) + [2], [0] + [1] * (n - 1), [1] * n):
+        k_lens = [x + most - 60 + i for i, x in enumerate(q_lens)]
+        qo.copy_(R.offsets(q_lens))
+        ko.copy_(R.offsets(k_lens))
+        out.fill_(math.nan)
+        lse.fill_(math.nan)
+        graph.replay()
+        torch.cuda.synchronize()
+        end = sum(q_lens)
+        want, want_lse, tol, tol_lse = R.attention(q, k, v, qo, ko, True, 0.125)
+        R.assert_close(out[:end], want[:end], tol[:end], "out %s" % q_lens)
+        R.assert_close(lse[:end], want_lse[:end], tol_lse[:end], "lse %s" % q_lens)
+        assert bool(torch.isnan(out[end:]).all()) and bool(torch.isnan(lse[end:]).all())
