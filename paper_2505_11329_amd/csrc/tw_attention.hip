@@ -333,10 +333,11 @@ __device__ __forceinline__ Place find_place(const AttentionParams &p, int i)
 // the i-th sequence's. (Every start is looked at; that the rows are no more than the sequences bounds the last one's.)
 __device__ __forceinline__ bool single_tokens(const AttentionParams &p)
 {
-    const int lane = threadIdx.x & 63, first = p.q_offsets[0], rows = p.q_offsets[p.n_seqs] - first;
+    const int lane = threadIdx.x & 63, first = clamp_row(p.q_offsets[0], 0, p.q_rows);
+    const int rows = clamp_row(p.q_offsets[p.n_seqs], first, p.q_rows) - first;
     bool single = rows <= p.n_seqs;
 #pragma unroll 8
-    for (int b = lane; b < p.n_seqs; b += 64) single &= p.q_offsets[b] - first == min(b, rows);
+    for (int b = lane; b < p.n_seqs; b += 64) single &= clamp_row(p.q_offsets[b], 0, p.q_rows) - first == min(b, rows);
     return __all(single);
 }
 

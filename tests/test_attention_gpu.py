@@ -319,3 +319,17 @@ def test_a_captured_call_of_single_tokens_replayed_with_a_longer_sequence_behind
         R.assert_close(out[:end], want[:end], tol[:end], "out %s" % q_lens)
         R.assert_close(lse[:end], want_lse[:end], tol_lse[:end], "lse %s" % q_lens)
         assert bool(torch.isnan(out[end:]).all()) and bool(torch.isnan(lse[end:]).all())
+
+
+def test_offsets_outside_the_tensors_in_the_form_for_few_rows(tw):
+    """Taken as their nearest rows, these are single tokens and empty sequences around them."""
+    for rows, wild, tame in ((2, [-1, 0, 1, 2, 2], [0, 0, 1, 2, 2]), (3, [-9, -4, 1, 2, 3, 1 << 30], [0, 0, 1, 2, 3, 3]),
+                             (3, [0, 1, 2, 5, 9], [0, 1, 2, 3, 3])):
+        k_lens = [50, 3, 700, 33, 5][:len(wild) - 1]
+        q, k, v, _, ko = inputs([rows] + [0] * (len(wild) - 2), k_lens, 8, 2, 64, seed=rows)
+        assert tw.attention_plan(len(k_lens), rows, k.shape[0], 8, 2, 64).key_waves == 4
+        wild, tame = (torch.tensor(x, dtype=torch.int32, device="cuda") for x in (wild, tame))
+        want = check(tw, q, k, v, tame, ko, what=str(tame.tolist()))
+        got = tw.attention(q, k, v, wild, ko, out=torch.full_like(q, math.nan), lse=torch.full(q.shape[:2], math.nan, device="cuda"))
+        for x, y in zip(got, want):
+            assert torch.equal(x, y)
