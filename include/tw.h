@@ -560,8 +560,9 @@ tw_status tw_weave_tune(const tw_layer_args *layer, int64_t multiple, const int6
  *   lse    = m + log( sum_j exp(s[j] - m) )
  *
  * A row that sees no key (Lk < Lq, or Lk == 0) gets out = 0 and lse = -inf. Keys that a row does not see
- * have no part in its result, whatever their values: Inf and NaN there stay there. Scores, maxima and
- * sums are fp32; exp(s[j] - m) is rounded to bf16 where it multiplies v and not where it is summed.
+ * have no part in its result, whatever their values: Inf and NaN there stay there. Inf in v of a key that
+ * it sees gives Inf, or NaN where exp(s[j] - m) is 0 in fp32. Scores, maxima and sums are fp32;
+ * exp(s[j] - m) is rounded to bf16 where it multiplies v and not where it is summed.
  *
  *   q           device bf16, row t, head h, at q + t * q_stride + h * head_dim (strides count elements)
  *   k, v        device bf16, row t, key head h, at k + t * k_stride + h * head_dim; may be columns of one

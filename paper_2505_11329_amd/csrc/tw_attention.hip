@@ -181,11 +181,33 @@ __device__ __forceinline__ float softmax_step(typename Mfma<M>::acc (&sc)[N], fl
     return alpha;
 }
 
-// Adds a key's values that are Inf or NaN, read from memory, to the sums of a lane whose row sees it.
+// Inf and NaN among the values of keys that a row does not see must not meet its p of zero. So in a tile that some row sees only a
+// part of, zeros take their place, and what their products would have been is added to the rows that see them: Inf itself,
+// as any p > 0 times Inf, and NaN where p has underflowed to 0. So a row gets the same from such a tile as from one that all rows see.
+
+// A bit for each of a lane's p, those that have underflowed.
 template <int M, int N>
-__device__ __forceinline__ void add_infinite(typename Mfma<M>::acc (&o)[N], const char *values, int dim, int part, bool sees)
+__device__ __forceinline__ uint32_t underflowed(const typename Mfma<M>::acc (&p)[N])
+{
+    constexpr int kAcc = M * M / 64;
+    uint32_t bits = 0;
+#pragma unroll
+    for (int i = N * kAcc - 1; i >= 0; --i) {
+        bits = bits + bits + (p[i / kAcc][i % kAcc] < 0x1p-126f);
+        __builtin_amdgcn_sched_barrier(0);  // (one after the other: registers are scarce here, and time is not)
+    }
+    return bits;
+}
+
+// Adds a key's values that are Inf or NaN, read from memory, to the sums of a lane whose row sees it. The key is the j-th of the
+// tile, and lost its row's underflowed().
+template <int M, int N>
+__device__ __forceinline__ void add_infinite(typename Mfma<M>::acc (&o)[N], const char *values, int dim, int part, bool sees, int j, uint32_t lost)
 {
     constexpr int kUnit = 256 / M, kQuads = M * M / 256;
+    // the lane that has the key's p, and its number there
+    const int lane = threadIdx.x & 63, holder = (lane & (M - 1)) | ((j / 4) % (64 / M) * M);
+    const bool none = (__shfl(lost, holder) >> (j / M * (M * M / 64) + j % M / kUnit * 4 + j % 4)) & 1;
 #pragma unroll
     for (int b = 0; b < N; ++b)
 #pragma unroll
@@ -196,7 +218,7 @@ __device__ __forceinline__ void add_infinite(typename Mfma<M>::acc (&o)[N], cons
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const uint32_t bits = i & 1 ? x[i >> 1] & 0xffff0000u : x[i >> 1] << 16;
-                o[b][g * 4 + i] += sees && (bits & 0x7f800000u) == 0x7f800000u ? __uint_as_float(bits) : 0.0f;
+                o[b][g * 4 + i] += sees && (bits & 0x7f800000u) == 0x7f800000u ? __uint_as_float(none ? bits | 0x7fc00000u : bits) : 0.0f;
             }
             __builtin_amdgcn_sched_barrier(0);  // (one load at a time: registers are scarce here, and time is not)
         }
@@ -483,8 +505,6 @@ __global__ __launch_bounds__(256, 2) void attention_few_kernel(AttentionParams p
         }
         all_but_landed<Shape::kLoads>();
         if (masked) {
-            // Inf and NaN of hidden keys must not meet a p of zero: zeros in their place, and the rows that see them get
-            // them added (p > 0 times one of them is the same)
             uint32_t bad = 0;
 #pragma unroll
             for (int i = 0; i < Shape::kLoads; ++i) {
@@ -501,10 +521,14 @@ __global__ __launch_bounds__(256, 2) void attention_few_kernel(AttentionParams p
             }
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
             if (__builtin_expect(__any(bad != 0), 0)) {
+                uint32_t lost[RB];
+#pragma unroll
+                for (int rb = 0; rb < RB; ++rb) lost[rb] = underflowed<16>(sc[rb]);
 #pragma unroll 1
                 for (int j = key0; j < min(key0 + Shape::kKeys, end); ++j)
 #pragma unroll
-                    for (int rb = 0; rb < RB; ++rb) add_infinite<16, kBlocks>(o[rb], v_head + j * p.v_stride, p.dim, part, j <= last[rb]);
+                    for (int rb = 0; rb < RB; ++rb)
+                        add_infinite<16>(o[rb], v_head + j * p.v_stride, p.dim, part, j <= last[rb], j - key0, lost[rb]);
             }
         }
 #pragma unroll
@@ -691,7 +715,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attention_wide_kernel(Attention
 #pragma unroll
     for (int x = 0; x < kSteps; ++x) qf[x] = *reinterpret_cast<const bf16x8 *>(k_frag[x] + Shape::kQAt + wave * 32 * Shape::kRowBytes);
 
-    auto compute = [&](int t, auto stage_, auto masked) TW_INLINE {
+    auto compute = [&](int t, auto stage_, auto masked, bool infinite) TW_INLINE {
         constexpr int kStage = decltype(stage_)::value;
         constexpr bool kMasked = decltype(masked)::value;
         // some row of the wave sees a key of the tile's second half
@@ -744,6 +768,14 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attention_wide_kernel(Attention
 #pragma unroll
                 for (int i = 0; i < 16; ++i) o[b][i] *= alpha;
         }
+        if constexpr (kMasked) {
+            if (__builtin_expect(infinite, 0)) {
+                const uint32_t lost = underflowed<32>(sc);
+#pragma unroll 1
+                for (int j = t * Shape::kKeys; j < min((t + 1) * Shape::kKeys, visible); ++j)
+                    add_infinite<32>(o, v_head + j * p.v_stride, p.dim, half, keys.begin + j <= last, j & (Shape::kKeys - 1), lost);
+            }
+        }
         auto values = [&](int t4) TW_INLINE {
             u32x4 pf;
 #pragma unroll
@@ -770,9 +802,8 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attention_wide_kernel(Attention
         }
     };
 
-    // Inf and NaN of hidden keys must not meet a p of zero: a tile that is not whole has zeros put in their place, and the rows
-    // that see them get them added behind its step (p > 0 times one of them is the same). A wave does so to the pieces that it
-    // has loaded itself, before the barrier that makes them everybody's.
+    // A wave puts zeros in the place of Inf and NaN in the pieces that it has loaded itself, before the barrier that makes them
+    // everybody's.
     auto clean_values = [&](int t) TW_INLINE {
         char *const mine = lds + (t & 1) * Shape::kStageBytes + Shape::kTileBytes + threadIdx.x * 16;
         uint32_t bad = 0;
@@ -792,15 +823,11 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attention_wide_kernel(Attention
         const bool any = __any(bad != 0);
         if (lane == 0) flags[t & 1][wave] = any;
     };
-    auto add_cleaned = [&](int t) TW_INLINE {
+    auto cleaned = [&](int t) TW_INLINE {
         bool infinite = false;
 #pragma unroll
         for (int w = 0; w < Shape::kWaves; ++w) infinite |= flags[t & 1][w] != 0;
-        if (__builtin_expect(__builtin_amdgcn_readfirstlane(infinite), 0)) {
-#pragma unroll 1
-            for (int j = t * Shape::kKeys; j < min((t + 1) * Shape::kKeys, visible); ++j)
-                add_infinite<32, kBlocks>(o, v_head + j * p.v_stride, p.dim, half, keys.begin + j <= last);
-        }
+        return __builtin_amdgcn_readfirstlane(infinite) != 0;
     };
 
     const bool has_rows = r0 + wave * 32 < list;
@@ -815,8 +842,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attention_wide_kernel(Attention
         } else if (!has_rows) {
             return;
         }
-        compute(t, stage, masked);
-        if constexpr (decltype(masked)::value) add_cleaned(t);
+        compute(t, stage, masked, decltype(masked)::value && cleaned(t));
     };
     using Stage0 = std::integral_constant<int, 0>;
     using Stage1 = std::integral_constant<int, 1>;

@@ -333,3 +333,44 @@ def test_offsets_outside_the_tensors_in_the_form_for_few_rows(tw):
         got = tw.attention(q, k, v, wild, ko, out=torch.full_like(q, math.nan), lse=torch.full(q.shape[:2], math.nan, device="cuda"))
         for x, y in zip(got, want):
             assert torch.equal(x, y)
+
+
+# one of each way to read the keys: four and eight waves of 32 rows, whole keys and parts; few rows, whole keys and parts
+FORMS = [(200, 320, 2, 1, 64), (200, 320, 4, 4, 128), (2048, 2112, 32, 32, 128), (100, 4096, 16, 2, 128), (100, 4160, 16, 2, 128),
+         (100, 4096, 16, 2, 64), (4, 256, 4, 2, 64),
+         (4, 256, 8, 1, 128), (3, 2048, 16, 2, 128), (2, 2048, 8, 1, 64)]
+
+
+@pytest.mark.parametrize("rows,keys,heads,kv_heads,dim", FORMS)
+def test_inf_in_values_of_any_weight_whatever_the_rows_around(tw, rows, keys, heads, kv_heads, dim):
+    """A key that a row sees, with Inf, -Inf and NaN among its values: Inf where its weight is one in fp32, NaN where it is
+    too small for that, and the same whether the rows of the tile see all of the tile's keys (no mask; the number of keys is a
+    multiple of every tile) or a part of them (a mask, which hides none from the last row)."""
+    assert keys % 64 == 0
+    g = torch.Generator().manual_seed(keys)
+    q = torch.zeros(rows, heads, dim, dtype=torch.bfloat16, device="cuda")
+    q[:, :, 0] = 1
+    v = torch.randn(keys, kv_heads, dim, generator=g).bfloat16().cuda()
+    at = keys - 6
+    v[at, :, 0], v[at, :, 1], v[at, :, 2], v[at, :, 3] = math.inf, -math.inf, math.nan, math.inf
+    v[at + 1, :, 3] = -math.inf
+    o = [R.offsets([n]).cuda() for n in (rows, keys)]
+    for best in (0, at - 9, keys - 1):       # the key with all of the weight
+        for gap in (0, 20, 64, 80, 86, 87, 88, 90, 92, 96, 100, 104, 120, 200, 1000):
+            k = torch.zeros(keys, kv_heads, dim, dtype=torch.bfloat16, device="cuda")
+            k[:, :, 0] = -gap
+            k[best, :, 0] = 0
+            got = [tw.attention(q, k, v, *o, causal=causal, scale=1.0) for causal in (True, False)]
+            last = [(out[-1], lse[-1]) for out, lse in got]
+            print(rows, keys, best, gap, last[0][0][0, :4].tolist(), last[1][0][0, :4].tolist(), flush=True)
+            for a, b in zip(*last):
+                assert torch.equal(torch.nan_to_num(a, 3e38, 2e38, -2e38), torch.nan_to_num(b, 3e38, 2e38, -2e38))
+            out, lse = last[0]
+            assert bool(torch.isfinite(out[:, 4:]).all()) and bool(torch.isfinite(lse).all())
+            assert bool(torch.isnan(out[:, 2:4]).all())
+            if gap <= 80:            # e^-80 is a number of fp32, e^-120 is none
+                assert bool((out[:, 0] == math.inf).all()) and bool((out[:, 1] == -math.inf).all())
+            elif gap >= 120:
+                assert bool(torch.isnan(out[:, :2]).all())
+            # rows that the mask hides those keys from
+            assert bool(torch.isfinite(got[0][0][:max(rows - 6, 0)]).all())
