@@ -562,7 +562,9 @@ tw_status tw_weave_tune(const tw_layer_args *layer, int64_t multiple, const int6
  * A row that sees no key (Lk < Lq, or Lk == 0) gets out = 0 and lse = -inf. Keys that a row does not see
  * have no part in its result, whatever their values: Inf and NaN there stay there. Inf in v of a key that
  * it sees gives Inf, or NaN where exp(s[j] - m) is 0 in fp32. Scores, maxima and sums are fp32;
- * exp(s[j] - m) is rounded to bf16 where it multiplies v and not where it is summed.
+ * exp(s[j] - m) is rounded to bf16 where it multiplies v and not where it is summed. Scores of any size
+ * are taken; where scale * q . k overflows the row is NaN, and a row all of whose scores are -Inf counts as one
+ * that sees no key. The sums are kept up to 2^8 times what the formula has: sum_j |v[j]| must stay below 2^119.
  *
  *   q           device bf16, row t, head h, at q + t * q_stride + h * head_dim (strides count elements)
  *   k, v        device bf16, row t, key head h, at k + t * k_stride + h * head_dim; may be columns of one

@@ -36,7 +36,7 @@ struct AttentionParams {
     int group_shift;
     int n_seqs, q_heads, kv_heads, group, dim, causal;
     int chunks, min_chunk;
-    float c;
+    float c, inv_c;
 };
 
 // The kernels' parts are lambdas: all of them belong into the loop they are called from.
@@ -146,12 +146,12 @@ __device__ __forceinline__ uint32_t finite_bf16x2(uint32_t x)
     return x & ~((bad - (bad >> 15)) | bad);
 }
 
-// One tile's step of the softmax: sc holds a lane's scores and gets p; m and l are the row's. Returns the factor of what was
-// summed before, 1 for most tiles: the maximum that is taken off follows the row's true one only when that is more than 2^8
-// ahead, so that p stays below 2^8, which changes no relative error, and the sums seldom have to be rescaled. Each row
-// decides for itself. (Four chains of maxima and sums: a chain's next instruction waits for eight clocks.)
+// One tile's step of the softmax: sc holds a lane's scores, softmax_exp makes them p; m and l are the row's. softmax_max returns the
+// factor of what was summed before, 1 for most tiles: the maximum that is taken off follows the row's true one only when that is
+// more than 2^8 ahead, so that p stays below 2^8, which changes no relative error, and the sums seldom have to be rescaled. Each
+// row decides for itself. (Four chains of maxima and sums: a chain's next instruction waits for eight clocks.)
 template <int M, int N>
-__device__ __forceinline__ float softmax_step(typename Mfma<M>::acc (&sc)[N], float c, float *m, float *l)
+__device__ __forceinline__ float softmax_max(const typename Mfma<M>::acc (&sc)[N], float c, float *m)
 {
     constexpr int kAcc = M * M / 64;
     float tops[4];
@@ -166,19 +166,44 @@ __device__ __forceinline__ float softmax_step(typename Mfma<M>::acc (&sc)[N], fl
     if (top > *m + kLag) {
         alpha = __builtin_amdgcn_exp2f(*m - top);
         *m = top;
-        *l *= alpha;
     }
-    const float m_use = *m == kMinusInf ? 0.0f : *m;
+    return alpha;
+}
+
+// The maximum that is taken off; 0 while a row has seen no key.
+__device__ __forceinline__ float taken_off(float m) { return m == kMinusInf ? 0.0f : m; }
+
+template <int M, int N>
+__device__ __forceinline__ void softmax_exp(typename Mfma<M>::acc (&sc)[N], float c, float m, float *l)
+{
+    constexpr int kAcc = M * M / 64;
     float sums[4] = {*l, 0.0f, 0.0f, 0.0f};
 #pragma unroll
     for (int n = 0; n < N; ++n)
 #pragma unroll
         for (int i = 0; i < kAcc; ++i) {
-            sc[n][i] = __builtin_amdgcn_exp2f(fmaf(sc[n][i], c, -m_use));
+            sc[n][i] = __builtin_amdgcn_exp2f(fmaf(sc[n][i], c, -m));
             sums[i % 4] += sc[n][i];
         }
     *l = (sums[0] + sums[1]) + (sums[2] + sums[3]);
-    return alpha;
+}
+
+// m is a rounded product, and p takes it off the exact one: their difference, half a step of m, must stay small against the range of
+// p. Below 2^24 it is 1/2 at most. Above, each score is rounded as m was, and leaves softmax_exp no m to take off. (It is divided by
+// c because softmax_exp multiplies; c is no less than 2^-104 there, and the quotient a number.) Rare, and tested where sums are
+// rescaled: with a branch of its own 8192 tokens of 32 heads of 64 took 313 us, 311 so, 310 without.
+__device__ __forceinline__ bool large_max(float m) { return fabsf(m) >= 0x1p24f; }
+
+template <int M, int N>
+__device__ __forceinline__ void take_off_large(typename Mfma<M>::acc (&sc)[N], float c, float inv_c, float *m)
+{
+#pragma clang fp contract(off)
+    const bool large = large_max(*m);
+#pragma unroll
+    for (int n = 0; n < N; ++n)
+#pragma unroll
+        for (int i = 0; i < M * M / 64; ++i) sc[n][i] = large ? (sc[n][i] * c - *m) * inv_c : sc[n][i];
+    *m = large ? 0.0f : *m;
 }
 
 // Inf and NaN among the values of keys that a row does not see must not meet its p of zero. So in a tile that some row sees only a
@@ -495,11 +520,15 @@ __global__ __launch_bounds__(256, 2) void attention_few_kernel(AttentionParams p
         u32x4 pf[RB];
 #pragma unroll
         for (int rb = 0; rb < RB; ++rb) {
-            const float alpha = softmax_step<16>(sc[rb], p.c, &m[rb], &l[rb]);
-            if (__any(alpha != 1.0f)) {
+            const float alpha = softmax_max<16>(sc[rb], p.c, &m[rb]);
+            float off = taken_off(m[rb]);
+            if (__any(alpha != 1.0f || large_max(off))) {
+                l[rb] *= alpha;
 #pragma unroll
                 for (int b = 0; b < kBlocks; ++b) o[rb][b] *= alpha;
+                if (__builtin_expect(__any(large_max(off)), 0)) take_off_large<16>(sc[rb], p.c, p.inv_c, &off);
             }
+            softmax_exp<16>(sc[rb], p.c, off, &l[rb]);
             pf[rb] = {pack_bf16x2(sc[rb][0][0], sc[rb][0][1]), pack_bf16x2(sc[rb][0][2], sc[rb][0][3]),
                       pack_bf16x2(sc[rb][1][0], sc[rb][1][1]), pack_bf16x2(sc[rb][1][2], sc[rb][1][3])};
         }
@@ -761,13 +790,17 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attention_wide_kernel(Attention
                 for (int i = 0; i < 16; ++i)
                     if (n * 32 + 8 * (i / 4) + i % 4 > seen) sc[n][i] = kMinusInf;
         }
-        const float alpha = softmax_step<32>(sc, p.c, &m, &l);
-        if (__any(alpha != 1.0f)) {
+        const float alpha = softmax_max<32>(sc, p.c, &m);
+        float off = taken_off(m);
+        if (__any(alpha != 1.0f || large_max(off))) {
+            l *= alpha;
 #pragma unroll
             for (int b = 0; b < kBlocks; ++b)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) o[b][i] *= alpha;
+            if (__builtin_expect(__any(large_max(off)), 0)) take_off_large<32>(sc, p.c, p.inv_c, &off);
         }
+        softmax_exp<32>(sc, p.c, off, &l);
         if constexpr (kMasked) {
             if (__builtin_expect(infinite, 0)) {
                 const uint32_t lost = underflowed<32>(sc);
@@ -1182,6 +1215,7 @@ tw_status tw_attention(const tw_attention_args *args, void *workspace, int64_t w
     p.chunks = plan.chunks;
     p.min_chunk = plan.min_chunk;
     p.c = static_cast<float>(a.scale * 1.4426950408889634);
+    p.inv_c = 1.0f / p.c;
     const hipStream_t s = static_cast<hipStream_t>(stream);
     TW_TRY(a.head_dim > 64 ? launch_attention_for<128>(p, plan, grid, s) : launch_attention_for<64>(p, plan, grid, s));
     if (plan.chunks > 1) {

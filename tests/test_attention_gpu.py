@@ -374,3 +374,43 @@ def test_inf_in_values_of_any_weight_whatever_the_rows_around(tw, rows, keys, he
                 assert bool(torch.isnan(out[:, :2]).all())
             # rows that the mask hides those keys from
             assert bool(torch.isfinite(got[0][0][:max(rows - 6, 0)]).all())
+
+
+@pytest.mark.parametrize("rows,keys,heads,kv_heads,dim", FORMS + [(1, 1, 2, 2, 64), (70, 1, 2, 1, 128)])
+def test_scores_whose_steps_are_large(tw, rows, keys, heads, kv_heads, dim):
+    """Scores whose neighbouring numbers in fp32 are far apart: the key with the largest one has all of the weight. Its p is
+    rounded to bf16 and so is the result; lse is the score, rounded three times, and a sum of 1."""
+    g = torch.Generator().manual_seed(rows)
+    q, k = (torch.zeros(n, h, dim, dtype=torch.bfloat16, device="cuda") for n, h in ((rows, heads), (keys, kv_heads)))
+    v = torch.randn(keys, kv_heads, dim, generator=g).bfloat16().cuda()
+    o = [R.offsets([n]).cuda() for n in (rows, keys)]
+    for power in (20, 25, 28, 31, 34, 40, 60, 100, 122):
+        for sign, best, others in ((1.3, 1.7, 1.0), (-1.3, 1.0, 1.7)):
+            for at in (0, keys - 1):
+                print(rows, keys, power, sign, at, flush=True)
+                q[:, :, 0], k[:, :, 0] = sign * 2.0 ** (power // 2), others * 2.0 ** (power - power // 2)
+                k[at, :, 0] = best * 2.0 ** (power - power // 2)
+                out, lse = tw.attention(q, k, v, *o, causal=False, scale=0.3)
+                want = v[at].double().repeat_interleave(heads // kv_heads, dim=0).expand(rows, heads, dim)
+                R.assert_close(out, want, (2 * R.BF16 + 2.0 ** -15) * want.abs(), "out")
+                score = float(torch.tensor(0.3)) * float(q[0, 0, 0].double() * k[at, 0, 0].double())
+                want_lse = torch.full((rows, heads), score, dtype=torch.float64, device="cuda")
+                R.assert_close(lse, want_lse, 4 * R.F32 * want_lse.abs() + 2.0 ** -20, "lse")
+
+
+@pytest.mark.parametrize("rows,keys,heads,kv_heads,dim", FORMS)
+def test_scores_beyond_fp32(tw, rows, keys, heads, kv_heads, dim):
+    """Scores that overflow give NaN, as Inf - Inf does; a row all of whose scores are -Inf counts as one that sees no key."""
+    q, k = (torch.zeros(n, h, dim, dtype=torch.bfloat16, device="cuda") for n, h in ((rows, heads), (keys, kv_heads)))
+    v = torch.ones_like(k)
+    o = [R.offsets([n]).cuda() for n in (rows, keys)]
+    q[:, :, 0] = 2.0 ** 63
+    k[0, :, 0] = 2.0 ** 63      # 2^126 is a number of fp32, four times that is none
+    minus_inf = torch.full_like(k, -math.inf)
+    for causal in (True, False):
+        out, lse = tw.attention(q, k, v, *o, causal=causal, scale=1.0)
+        assert bool((out == 1).all()) and bool(torch.isfinite(lse).all())
+        out, lse = tw.attention(q, k, v, *o, causal=causal, scale=4.0)
+        assert bool(torch.isnan(out).all()) and bool(torch.isnan(lse).all())
+        out, lse = tw.attention(torch.ones_like(q), minus_inf, v, *o, causal=causal)
+        assert not bool(out.any()) and bool((lse == -math.inf).all())
