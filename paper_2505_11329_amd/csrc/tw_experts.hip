@@ -355,6 +355,9 @@ static bool aligned4(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 3
 
 static bool streamed(uint64_t result_bytes) { return result_bytes > static_cast<uint64_t>(kLastLevelCacheBytes / 2); }
 
+// What the pairs' rows come to, however many more rows there are.
+static uint64_t placed_bytes(const RowsParams &p) { return static_cast<uint64_t>(std::min(p.rows, p.tokens * p.top_k)) * p.pieces * 16u; }
+
 static void row_layout(int64_t H, RowsParams *p)
 {
     p->pieces = static_cast<int>(H / 8);
@@ -463,7 +466,7 @@ tw_status tw_expert_dispatch(const void *x, const int32_t *position, int64_t N, 
     p.rows = rows;
     p.top_k = top_k;
     row_layout(H, &p);
-    return launch_rows(streamed(rows_b) ? expert_dispatch_kernel<true> : expert_dispatch_kernel<false>, p, row_parts(p), stream);
+    return launch_rows(streamed(placed_bytes(p)) ? expert_dispatch_kernel<true> : expert_dispatch_kernel<false>, p, row_parts(p), stream);
 }
 
 tw_status tw_expert_combine(const void *y, int64_t rows, const int32_t *position, const float *weights, int64_t N,
@@ -525,7 +528,7 @@ tw_status tw_expert_combine_backward(const void *dout, const void *y, int64_t ro
     row_layout(H, &p);
     // Results that stay in the caches: workgroups for one or two of a token's pairs, which all find dout there (64 tokens of 8 rows of
     // 4096: 4.7 us with one, 5.3 with two, 8.3 with eight; 1500 tokens 47, 45, 47; 8192, whose results do not stay, 251, 234, 211).
-    if (streamed(rows_b)) return launch_rows(expert_combine_backward_kernel<true, kMost>, p, 1, stream);
+    if (streamed(placed_bytes(p))) return launch_rows(expert_combine_backward_kernel<true, kMost>, p, 1, stream);
     if (row_groups(p) * top_k <= 4096) return launch_rows(expert_combine_backward_kernel<false, 1>, p, top_k, stream);
     return launch_rows(expert_combine_backward_kernel<false, 2>, p, (top_k + 1) / 2, stream);
 }

@@ -5,6 +5,7 @@ import pytest
 import torch
 
 import operator_reference as R
+from helpers import captured_kernels
 
 pytestmark = pytest.mark.gpu
 
@@ -220,3 +221,26 @@ def test_streams_and_graphs(tw):
             assert torch.equal(a, b)
         for a, b in zip(eager, want[(n + 1) % 2]):
             assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("N,K,H", [(64, 8, 4096), (1000, 2, 2048)])
+def test_room_to_spare_changes_nothing(tw, N, K, H):
+    """A buffer with more rows than there are pairs: the launch is that of one that fits, since it writes as much."""
+    position, x, y, w = routed(N, K, 16, H)
+    many = (160 << 20) // (H * 2)
+    results = []
+    for rows in (N * K, many):
+        out, y2 = torch.zeros(rows, H, dtype=torch.bfloat16, device="cuda"), torch.zeros(rows, H, dtype=torch.bfloat16, device="cuda")
+        y2[:N * K] = y
+        dy, dw, s = torch.zeros_like(y2), torch.zeros_like(w), torch.cuda.Stream()
+        torch.cuda.synchronize()
+        kernels = captured_kernels(s, lambda: (tw.expert_dispatch(x, position, out=out, stream=s),
+                                               tw.expert_combine_backward(x, y2, position, w, dy=dy, dweights=dw, stream=s)))
+        assert len(kernels) == 2
+        tw.expert_dispatch(x, position, out=out)
+        tw.expert_combine_backward(x, y2, position, w, dy=dy, dweights=dw)
+        assert not bool(out[N * K:].any()) and not bool(dy[N * K:].any())
+        results.append((kernels, out[:N * K], dy[:N * K], dw))
+    assert results[0][0] == results[1][0]
+    for a, b in zip(results[0][1:], results[1][1:]):
+        assert torch.equal(a, b)
