@@ -588,7 +588,9 @@ tw_status tw_weave_tune(const tw_layer_args *layer, int64_t multiple, const int6
  *               need one each
  *
  * Where rows and heads alone are too few for the device, each sequence's keys are cut into parts that work
- * side by side, and a second kernel joins them. The result bits of a row depend
+ * side by side, and a second kernel joins them. This goes by the sizes alone, k_rows / n_seqs keys to a
+ * sequence, so that a captured call serves whatever offsets fit; the price is that tensors with many more
+ * rows than their sequences are launched as if these had them all (slower, not wrong). The result bits of a row depend
  * on its own q, its sequence's k and v, and on the form of the launch, which follows from the sizes of
  * the call (tw_attention_plan): calls of the same form, e.g. one batch and the same batch split in two
  * large halves, give the same bits.

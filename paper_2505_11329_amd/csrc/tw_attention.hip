@@ -1004,7 +1004,8 @@ static AttentionPlan attention_plan(const tw_attention_args &a)
     const int64_t group = a.q_heads / a.kv_heads, list = a.q_rows * group;
     // Sequences of so few rows on average that tiles of 16 or 32 hold most of them; longer ones among them have more tiles, and all
     // together no more than twice as many as there are sequences. (4 rows each on average, 64 / 8 heads: 4 sequences with up to 1000,
-    // 2000, 8000 keys 17, 17, 26 us, 23, 27, 30 in the other form; 32 of them with up to 1000, 8000 keys 22, 99, 29, 109.)
+    // 2000, 8000 keys 16.5, 17, 25 us, 14.5, 16.5, 26.5 in the other form; 32 of them with up to 1000, 6000, 8000 keys 22, 90, 99; 29, 96,
+    // 127.)
     plan.few = list <= 16 * a.n_seqs ? 1 : list <= 32 * a.n_seqs ? 2 : 0;
     // Four waves, two workgroups to a compute unit, where sequences seldom fill tiles of 256 rows or are short, so that a workgroup's
     // start, search and results are much of its time, beside which the second one works (16 heads of 128, prompts of up to 128 tokens

@@ -151,8 +151,8 @@ __global__ __launch_bounds__(64 * WAVES) void expert_place_kernel(SortParams p)
 // ---- rows ----
 //
 // All of these are bound by memory: 16 bytes of a row to a thread, 2^row_log2 threads to a row of up to 2048 elements. Longer rows
-// are cut into parts of 2048 for workgroups of their own (16 tokens of 8 rows of 7168 summed: 4.9 us, 10.2 by one workgroup each, 6.3
-// by two; 16384 of 2 rows of 8192: 139, 145), but for the backward pass, whose dot products need whole rows.
+// are cut into parts of 2048 for workgroups of their own (16 tokens of 8 rows of 7168 summed: 4.1 us, 8.6 by one workgroup each, 5.4
+// by two; 16384 of 2 rows of 8192: 133, 143), but for the backward pass, whose dot products need whole rows.
 
 struct RowsParams {
     const char *in;       // x | y | dout
@@ -527,7 +527,7 @@ tw_status tw_expert_combine_backward(const void *dout, const void *y, int64_t ro
     p.top_k = top_k;
     row_layout(H, &p);
     // Results that stay in the caches: workgroups for one or two of a token's pairs, which all find dout there (64 tokens of 8 rows of
-    // 4096: 4.7 us with one, 5.3 with two, 8.3 with eight; 1500 tokens 47, 45, 47; 8192, whose results do not stay, 251, 234, 211).
+    // 4096: 4.7 us with one, 5.4 with two, 8.3 with eight; 1500 tokens 47, 45, 48; 8192, whose results do not stay, 223, 211, 211).
     if (streamed(placed_bytes(p))) return launch_rows(expert_combine_backward_kernel<true, kMost>, p, 1, stream);
     if (row_groups(p) * top_k <= 4096) return launch_rows(expert_combine_backward_kernel<false, 1>, p, top_k, stream);
     return launch_rows(expert_combine_backward_kernel<false, 2>, p, (top_k + 1) / 2, stream);
