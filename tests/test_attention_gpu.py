@@ -1,4 +1,5 @@
 """tw_attention against the plain 64-bit form: lengths, heads, head sizes, masks, strides, and what it leaves alone."""
+import ctypes
 import math
 
 import pytest
@@ -414,3 +415,23 @@ def test_scores_beyond_fp32(tw, rows, keys, heads, kv_heads, dim):
         assert bool(torch.isnan(out).all()) and bool(torch.isnan(lse).all())
         out, lse = tw.attention(torch.ones_like(q), minus_inf, v, *o, causal=causal)
         assert not bool(out.any()) and bool((lse == -math.inf).all())
+
+
+@pytest.mark.parametrize("rows,keys,heads,kv_heads,dim", FORMS)
+def test_no_lse_and_results_between_other_columns(tw, rows, keys, heads, kv_heads, dim):
+    """The C call without lse, results in rows that are longer than theirs, in every form."""
+    q, k, v, qo, ko = inputs([rows], [keys], heads, kv_heads, dim, seed=keys, tail=1)
+    wide = torch.full((rows + 2, heads + 2, dim), 7.0, dtype=torch.bfloat16, device="cuda")
+    out = wide[:, 1:heads + 1]
+    want, _ = tw.attention(q, k, v, qo, ko)
+    a = tw.AttentionArgs(q=q.data_ptr(), k=k.data_ptr(), v=v.data_ptr(), out=out.data_ptr(), lse=None, q_offsets=qo.data_ptr(),
+                         k_offsets=ko.data_ptr(), n_seqs=1, q_rows=rows + 2, k_rows=keys + 2, q_stride=heads * dim, k_stride=kv_heads * dim,
+                         v_stride=kv_heads * dim, out_stride=(heads + 2) * dim, q_heads=heads, kv_heads=kv_heads, head_dim=dim,
+                         scale=1.0 / math.sqrt(dim), causal=1)
+    need = tw.lib().tw_attention_workspace_bytes(ctypes.byref(a))
+    space = torch.empty(max(need, 16), dtype=torch.uint8, device="cuda")
+    stream = ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)
+    assert tw.lib().tw_attention(ctypes.byref(a), ctypes.c_void_p(space.data_ptr()), need, stream) == 0
+    assert torch.equal(out[1:-1], want[1:-1])
+    out[1:-1] = 7.0
+    assert bool((wide == 7).all())
