@@ -12,8 +12,10 @@
  *   - a bf16 GEMM standing in for the other split's projection, and the
  *     fused-kernel-next-to-GEMM launch that one step of the weave consists of
  *     (Fig. 7b);
- *   - what a layer does between two such boundaries: attention over a packed
- *     batch, and the tokens sorted to their experts and back.
+ *   - what a layer does between two such boundaries: norms and position
+ *     rotation of queries and keys, attention over a packed batch, the tokens
+ *     sorted to their experts and back, and the experts' products and
+ *     activation in between.
  *
  * The in-switch reduction of the paper has no counterpart on this hardware:
  * the P peer partials are P buffers in local HBM and the reading compute unit
@@ -680,6 +682,133 @@ tw_status tw_expert_combine(const void *y, int64_t rows, const int32_t *position
 tw_status tw_expert_combine_backward(const void *dout, const void *y, int64_t rows, const int32_t *position,
                                      const float *weights, int64_t N, int top_k, int64_t H, void *dy, float *dweights,
                                      void *stream);
+
+/*
+ * The experts' products: row r of C is row r of A times the weights of the expert that r belongs to, in one
+ * launch for all experts. Expert e has the rows [offsets[e], offsets[e+1]), as tw_expert_sort leaves them in
+ * device memory, so nothing waits for the host and a captured call serves whatever offsets it meets.
+ *
+ *   C[r] = bf16( A[r] B[e] ), summed in fp32;  B[e](k, n) at B[(e*N + n)*K + k] (TW_B_NK: [n_experts x N x K],
+ *   each expert's weight as a linear layer keeps it) or at B[(e*K + k)*N + n] (TW_B_KN: [n_experts x K x N]).
+ *   The gradient of A is the same call on the gradient of C with N and K exchanged and the other layout.
+ *
+ * tw_expert_gemm_backward, the gradient of B: dB[e](k, n) = bf16( sum over the rows r of e of A[r,k] dC[r,n] ),
+ *   stored like B; 0 for an expert without rows.
+ *
+ *   A             device bf16 [rows x K];  C, dC  [rows x N];  B, dB  n_experts weights of N x K elements
+ *   offsets       device int32 [n_experts + 1], ascending, 4-byte aligned. Values outside [0, rows] are taken as the
+ *                 nearest of the two, and a value below one before it as that one, so that wrong ones give wrong results
+ *                 and nothing else.
+ *   rows          < 2^31; rows of C outside [offsets[0], offsets[n_experts]) are left as they were, and those of A and dC
+ *                 have no part in any result
+ *   N, K          multiples of 8, at most TW_MAX_EXPERT_WIDTH; K == 0: rows of C that have an expert are 0
+ *   n_experts     1 ... TW_MAX_EXPERTS
+ * What a row, or a weight's gradient, comes to depends on its own inputs and on the form of the launch, which follows from
+ * the sizes of the call alone; no atomics order any sum. Inf and NaN propagate by IEEE rules within their row (their
+ * expert's gradient) and reach no other. Outputs must not overlap inputs.
+ */
+#define TW_MAX_EXPERT_WIDTH (1 << 17)
+
+tw_status tw_expert_gemm(const void *A, const void *B, void *C, const int32_t *offsets, int64_t rows, int64_t N, int64_t K,
+                         int n_experts, int b_layout, void *stream);
+
+tw_status tw_expert_gemm_backward(const void *A, const void *dC, void *dB, const int32_t *offsets, int64_t rows, int64_t N,
+                                  int64_t K, int n_experts, int b_layout, void *stream);
+
+/*
+ * Gated activation, between an expert's (or any MLP's) two products. A row of x holds F gates g and behind them F values u:
+ *   out = bf16( g s u ),  s = 1 / (1 + exp(-g))
+ * tw_gated_silu_backward, dout the gradient of out:
+ *   dx = bf16( dout u s (1 + g (1 - s)) ) beside bf16( dout g s );  dx may be x (same start address)
+ *   x, dx     device bf16 [rows x 2F];  out, dout  device bf16 [rows x F]
+ *   F         a multiple of 8, 8 ... TW_MAX_H;  rows < 2^31
+ *   limit     device int32, 4-byte aligned, or NULL: rows from *limit on are left as they were (for rows sorted by expert:
+ *             offsets + n_experts, so that rows without an expert cost nothing)
+ * All of it is computed in fp32 and rounded once. Outputs must not overlap inputs but as stated.
+ */
+tw_status tw_gated_silu(const void *x, int64_t rows, int64_t F, const int32_t *limit, void *out, void *stream);
+
+tw_status tw_gated_silu_backward(const void *dout, const void *x, int64_t rows, int64_t F, const int32_t *limit, void *dx,
+                                 void *stream);
+
+/*
+ * Norms of queries and keys for each head, and the rotation by their position, in one pass: what a layer does between
+ * its projection and tw_attention. For each token t and each head x of it (head_dim elements, D):
+ *
+ *   z = x * rsqrt(mean(x^2) + eps) * w      w the weight of the queries' or of the keys' norm; z = x without norms
+ *   y = z with the pairs of its first rot_dim columns turned by the angles of position p = positions[t]:
+ *       y[a] = z[a] cos - z[b] sin,  y[b] = z[b] cos + z[a] sin,   cos, sin = rotation[p][i], rotation[p][rot_dim/2 + i]
+ *       pair i is a, b = i, i + rot_dim/2, or, interleaved, a, b = 2i, 2i + 1;  i < rot_dim/2
+ *
+ * in fp32, rounded to bf16 once.
+ *
+ *   q, k            device bf16, token t, head h, at q + t * q_stride + h * head_dim (strides count elements); may be
+ *                   columns of one buffer (the result of one projection)
+ *   q_out, k_out    the same; q_out may be q and k_out may be k (same start address and stride). Any other overlap of an
+ *                   output with an input or the other output is refused; rows with the same stride whose columns are
+ *                   apart do not overlap.
+ *   positions       device, [tokens] of int32 (position_bytes 4) or int64 (8), aligned to it. A token whose position is
+ *                   outside [0, n_positions), e.g. -1, is padding: its rows of the outputs are left as they were
+ *   rotation        device fp32 [n_positions x rot_dim], 16-byte aligned: for each position the rot_dim / 2 cosines, then
+ *                   the sines. Tables of angles that are scaled for long contexts serve as well, and factors on both.
+ *                   NULL together with positions: no rotation, all tokens (n_positions and rot_dim then do not count)
+ *   q_weight, k_weight   device bf16 [head_dim], 16-byte aligned; both NULL: no norms. (rotation or weights must be there.)
+ *   tokens          0 ... 2^31 - 1;  n_positions  0 ... 2^31 - 1
+ *   head_dim        a multiple of 8 up to TW_MAX_HEAD_DIM; rot_dim a multiple of 8, 8 ... head_dim
+ *   q_heads, kv_heads    1 ... TW_MAX_HEADS each
+ *   strides         multiples of 8, at least heads * head_dim, at most TW_MAX_ROW_STRIDE
+ *   eps             finite, >= 0
+ *
+ * tw_qk_norm_rope_backward, dq and dk the gradients of q_out and k_out: with r = rsqrt(mean(x^2) + eps) and dz the pairs of dy
+ * turned back,
+ *   dx = r (dz w - x r^2 mean(dz w x)) to dq_out and dk_out, in bf16;  dx = dz without norms
+ *   dweight[c] = sum over tokens and heads of dz[c] x[c] r, in fp32, to dq_weight and dk_weight; padding has no part
+ *   q, k            the calls' inputs, as they were (not read without norms: may then be NULL)
+ *   dq, dk          laid out like q and k; dq_out may be dq and dk_out dk (same start address and stride), or q and k likewise
+ *   dq_weight, dk_weight  device fp32 [head_dim], 4-byte aligned; not written without norms (may then be NULL)
+ *   workspace       device memory of tw_qk_norm_rope_backward_workspace_bytes(), 16-byte aligned, overwritten; calls that
+ *                   may run at the same time need one each
+ * The sums over tokens are taken in an order that follows from the sizes of the call.
+ */
+typedef struct tw_qk_norm_rope_args {
+    const void *q;
+    const void *k;
+    void *q_out;
+    void *k_out;
+    const void *positions;
+    const float *rotation;
+    const void *q_weight;
+    const void *k_weight;
+    int64_t tokens;
+    int64_t n_positions;
+    int64_t q_stride;
+    int64_t k_stride;
+    int64_t q_out_stride;
+    int64_t k_out_stride;
+    int position_bytes;
+    int q_heads;
+    int kv_heads;
+    int head_dim;
+    int rot_dim;
+    int interleaved;
+    float eps;
+    /* the gradient's: */
+    const void *dq;
+    const void *dk;
+    float *dq_weight;
+    float *dk_weight;
+    int64_t dq_stride;
+    int64_t dk_stride;
+} tw_qk_norm_rope_args;
+
+/* The fields of the gradient are not looked at. */
+tw_status tw_qk_norm_rope(const tw_qk_norm_rope_args *args, void *stream);
+
+/* dq_out and dk_out go to args->q_out and args->k_out. */
+tw_status tw_qk_norm_rope_backward(const tw_qk_norm_rope_args *args, void *workspace, int64_t workspace_bytes, void *stream);
+
+/* Bytes of workspace that the gradient needs for these sizes (of the pointers only whether there are weights counts); -1 for sizes it refuses. Host only. */
+int64_t tw_qk_norm_rope_backward_workspace_bytes(const tw_qk_norm_rope_args *args);
 
 /* Compute units of the current device; -1 when no device can be queried. */
 int tw_device_cu_count(void);

@@ -61,6 +61,16 @@ class AttentionArgs(ctypes.Structure):
                 ("head_dim", ctypes.c_int), ("scale", ctypes.c_float), ("causal", ctypes.c_int)]
 
 
+class QkNormRopeArgs(ctypes.Structure):
+    """struct tw_qk_norm_rope_args"""
+    _fields_ = [("q", _vp), ("k", _vp), ("q_out", _vp), ("k_out", _vp), ("positions", _vp), ("rotation", _vp), ("q_weight", _vp),
+                ("k_weight", _vp), ("tokens", _i64), ("n_positions", _i64), ("q_stride", _i64), ("k_stride", _i64),
+                ("q_out_stride", _i64), ("k_out_stride", _i64), ("position_bytes", ctypes.c_int), ("q_heads", ctypes.c_int),
+                ("kv_heads", ctypes.c_int), ("head_dim", ctypes.c_int), ("rot_dim", ctypes.c_int), ("interleaved", ctypes.c_int),
+                ("eps", ctypes.c_float), ("dq", _vp), ("dk", _vp), ("dq_weight", _vp), ("dk_weight", _vp), ("dq_stride", _i64),
+                ("dk_stride", _i64)]
+
+
 class AttentionLaunch(ctypes.Structure):
     """struct tw_attention_launch"""
     _fields_ = [("tile_rows", ctypes.c_int), ("key_waves", ctypes.c_int), ("chunks", ctypes.c_int), ("min_chunk", ctypes.c_int)]
@@ -186,6 +196,19 @@ def lib():
         L.tw_expert_combine.restype = ctypes.c_int
         L.tw_expert_combine_backward.argtypes = [_vp, _vp, _i64, _vp, _vp, _i64, ctypes.c_int, _i64, _vp, _vp, _vp]
         L.tw_expert_combine_backward.restype = ctypes.c_int
+        for name in ("tw_expert_gemm", "tw_expert_gemm_backward"):
+            getattr(L, name).argtypes = [_vp, _vp, _vp, _vp, _i64, _i64, _i64, ctypes.c_int, ctypes.c_int, _vp]
+            getattr(L, name).restype = ctypes.c_int
+        L.tw_gated_silu.argtypes = [_vp, _i64, _i64, _vp, _vp, _vp]
+        L.tw_gated_silu.restype = ctypes.c_int
+        L.tw_gated_silu_backward.argtypes = [_vp, _vp, _i64, _i64, _vp, _vp, _vp]
+        L.tw_gated_silu_backward.restype = ctypes.c_int
+        L.tw_qk_norm_rope.argtypes = [ctypes.POINTER(QkNormRopeArgs), _vp]
+        L.tw_qk_norm_rope.restype = ctypes.c_int
+        L.tw_qk_norm_rope_backward.argtypes = [ctypes.POINTER(QkNormRopeArgs), _vp, _i64, _vp]
+        L.tw_qk_norm_rope_backward.restype = ctypes.c_int
+        L.tw_qk_norm_rope_backward_workspace_bytes.argtypes = [ctypes.POINTER(QkNormRopeArgs)]
+        L.tw_qk_norm_rope_backward_workspace_bytes.restype = _i64
         L.tw_hbm_probe_mixed.argtypes = [_vp, _vp, _i64, ctypes.c_int, ctypes.c_int, ctypes.c_int, _vp]
         L.tw_hbm_probe_mixed.restype = ctypes.c_int
         L.tw_hbm_probe_shaped.argtypes = [_vp, _vp, _i64, ctypes.c_int, ctypes.c_int, ctypes.c_int, ctypes.c_int, _vp]
@@ -499,6 +522,47 @@ def expert_combine_backward(dout, y, position, weights, dy=None, dweights=None, 
     return (_native or native()).expert_combine_backward(dout, y, position, weights, dy, dweights, stream)
 
 
+def expert_gemm(A, B, offsets, b_layout=B_NK, C=None, stream=None):
+    """tw_expert_gemm: A [rows, K] sorted by expert, B [n_experts, N, K] (B_NK) or [n_experts, K, N] (B_KN), offsets from
+    expert_sort. Returns C [rows, N]; rows without an expert are not written. The gradient of A: the same on that of C, with the
+    other b_layout."""
+    return (_native or native()).expert_gemm(A, B, offsets, b_layout, C, stream)
+
+
+def expert_gemm_backward(A, dC, offsets, b_layout=B_NK, dB=None, stream=None):
+    """tw_expert_gemm_backward: the gradient of B, laid out like it, from A [rows, K] and dC [rows, N]. Returns dB."""
+    return (_native or native()).expert_gemm_backward(A, dC, offsets, b_layout, dB, stream)
+
+
+def gated_silu(x, limit=None, out=None, stream=None):
+    """tw_gated_silu: x [rows, 2F], gates and behind them values. limit: int32 [1] on the GPU (of rows sorted by expert
+    offsets[-1:]), the number of rows, or None for all. Returns out [rows, F]; rows from limit on are not written."""
+    return (_native or native()).gated_silu(x, limit, out, stream)
+
+
+def gated_silu_backward(dout, x, limit=None, dx=None, stream=None):
+    """tw_gated_silu_backward. Returns dx [rows, 2F], which may be x; rows from limit on are not written."""
+    return (_native or native()).gated_silu_backward(dout, x, limit, dx, stream)
+
+
+def qk_norm_rope(q, k, positions, rotation, q_weight=None, k_weight=None, eps=1e-6, interleaved=False, q_out=None, k_out=None,
+                 stream=None):
+    """tw_qk_norm_rope: q [tokens, q_heads, head_dim] and k [tokens, kv_heads, head_dim], whose rows may be strided (columns of
+    one projection); positions int32 or int64 [tokens], negative for padding; rotation float32 [n_positions, rot_dim], cosines and
+    sines, both None for norms alone; weights None for the rotation alone. Returns (q_out, k_out), which may be q and k; rows of
+    padding are not written."""
+    return (_native or native()).qk_norm_rope(q, k, positions, rotation, q_weight, k_weight, eps, interleaved, q_out, k_out, stream)
+
+
+def qk_norm_rope_backward(dq, dk, positions, rotation, q=None, k=None, q_weight=None, k_weight=None, eps=1e-6, interleaved=False,
+                          dq_out=None, dk_out=None, dq_weight=None, dk_weight=None, workspace=None, stream=None):
+    """tw_qk_norm_rope_backward: dq and dk the gradients of q_out and k_out; q, k and the weights as given to qk_norm_rope (None
+    without norms). Returns (dq_out, dk_out, dq_weight, dk_weight); dq_out may be dq or q, dk_out dk or k; the weights' gradients are
+    float32 (None without norms). workspace: as for attention."""
+    return (_native or native()).qk_norm_rope_backward(dq, dk, positions, rotation, q, k, q_weight, k_weight, eps, interleaved,
+                                                       dq_out, dk_out, dq_weight, dk_weight, workspace, stream)
+
+
 def _attention_sizes(n_seqs, q_rows, k_rows, q_heads, kv_heads, head_dim):
     w, kw = q_heads * head_dim, kv_heads * head_dim
     return AttentionArgs(n_seqs=n_seqs, q_rows=q_rows, k_rows=k_rows, q_stride=w, k_stride=kw, v_stride=kw, out_stride=w,
@@ -516,6 +580,13 @@ def attention_plan(n_seqs, q_rows, k_rows, q_heads, kv_heads, head_dim):
     a, launch = _attention_sizes(n_seqs, q_rows, k_rows, q_heads, kv_heads, head_dim), AttentionLaunch()
     _check(lib().tw_attention_plan(ctypes.byref(a), ctypes.byref(launch)), "tw_attention_plan")
     return launch
+
+
+def qk_norm_rope_backward_workspace_bytes(tokens, q_heads, kv_heads, head_dim, rot_dim=0, interleaved=False):
+    """tw_qk_norm_rope_backward_workspace_bytes with norms; rot_dim 0: no rotation."""
+    a = QkNormRopeArgs(tokens=tokens, q_heads=q_heads, kv_heads=kv_heads, head_dim=head_dim, q_weight=16, rot_dim=rot_dim,
+                       rotation=16 if rot_dim else None, position_bytes=4, interleaved=int(interleaved))
+    return int(lib().tw_qk_norm_rope_backward_workspace_bytes(ctypes.byref(a)))
 
 
 def expert_sort_workspace_bytes(N, top_k, n_experts):

@@ -1,0 +1,65 @@
+// Rows in groups, one for each expert: where the tiles of a grouped product lie. The offsets stay on the device, so every
+// wave finds its tile by itself.
+#pragma once
+
+#include "tw_device.h"
+
+namespace tw {
+
+// The groups' first rows, n_groups + 1 of them. They are taken as they should be, whatever they are: inside the tensor
+// and ascending, so that no two groups share a row and the tiles are no more than the launch has counted on.
+struct Groups {
+    const int32_t *offsets;
+    int n_groups;
+    int rows;
+};
+
+// 64 groups, one to a lane: their first rows and those behind them. `carry` is where the first of them begins, and then where
+// the last of them ends.
+struct GroupRows {
+    int begin, end;
+};
+__device__ __forceinline__ GroupRows group_rows(const Groups &g, int first, int lane, int *carry)
+{
+    const int e = first + lane;
+    const int mine = e < g.n_groups ? min(max(g.offsets[e + 1], 0), g.rows) : 0;
+    const int end = max(max_upto(mine), *carry);
+    int begin = __builtin_amdgcn_update_dpp(0, end, 0x138, 0xf, 0xf, false);  // wave_shr 1: the lane before
+    if (lane == 0) begin = *carry;
+    *carry = __builtin_amdgcn_readlane(end, 63);
+    return {begin, end};
+}
+__device__ __forceinline__ int first_group_row(const Groups &g)
+{
+    return min(max(__builtin_amdgcn_readfirstlane(g.offsets[0]), 0), g.rows);
+}
+
+// Tile `index` of a list of all groups' tiles, group after group: rows of `tile_rows` times `tiles_n` columns of them. All of it
+// is the same in every lane.
+struct GroupTile {
+    int group;        // -1: there is no such tile
+    int tile;         // within the group's tiles
+    int begin, rows;  // the group's
+    int total;        // tiles of all groups up to this one's, of all where there is no such tile
+};
+__device__ __forceinline__ GroupTile find_group_tile(const Groups &g, int tile_rows_log2, int tiles_n, int index)
+{
+    const int lane = threadIdx.x & 63;
+    int carry = first_group_row(g), before = 0;
+    for (int first = 0; first < g.n_groups; first += 64) {
+        const GroupRows r = group_rows(g, first, lane, &carry);
+        const int tiles = static_cast<int>((static_cast<uint32_t>(r.end - r.begin) + (1u << tile_rows_log2) - 1) >> tile_rows_log2) * tiles_n;
+        const int upto = before + sum_upto(tiles);
+        const uint64_t past = __ballot(upto > index);
+        if (past) {
+            const int l = __builtin_ctzll(past);
+            const int begin = __builtin_amdgcn_readlane(r.begin, l), last = __builtin_amdgcn_readlane(upto, l);
+            return {first + l, index - (last - __builtin_amdgcn_readlane(tiles, l)), begin, __builtin_amdgcn_readlane(r.end, l) - begin,
+                    last};
+        }
+        before = __builtin_amdgcn_readlane(upto, 63);
+    }
+    return {-1, 0, 0, 0, before};
+}
+
+}  // namespace tw

@@ -827,6 +827,198 @@ PyObject *py_expert_combine_backward(PyObject *, PyObject *const *v, Py_ssize_t 
     });
 }
 
+// offsets of the experts of weights [experts, ...]
+const int32_t *expert_offsets(PyObject *o, int64_t experts)
+{
+    if (experts < 1 || experts >= INT32_MAX) fail(PyExc_ValueError, "there must be experts, and not too many");
+    return int32_array(o, {"offsets"}, {experts + 1});
+}
+
+// A, B, offsets, b_layout, C, stream
+PyObject *py_expert_gemm(PyObject *, PyObject *const *v, Py_ssize_t n)
+{
+    return entry("expert_gemm", n, 6, [&] {
+        const at::Tensor &A = sized(v[0], {"A"}, 2, "A must be [rows, K]");
+        const at::Tensor &B = sized(v[1], {"B"}, 3, "B must be [n_experts, N, K], or [n_experts, K, N]");
+        const int64_t rows = A.size(0), K = A.size(1), experts = B.size(0), layout = b_layout(v[3]);
+        const int64_t N = B.size(layout == TW_B_NK ? 1 : 2);
+        const void *a = bf16_array(v[0], {"A"}, {rows, K});
+        const void *b = layout == TW_B_NK ? bf16_array(v[1], {"B"}, {experts, N, K}) : bf16_array(v[1], {"B"}, {experts, K, N});
+        const int32_t *at = expert_offsets(v[2], experts);
+        Ref C = given_or_empty(v[4], A, {rows, N}, at::kBFloat16);
+        void *c = bf16_array(C.o, {"C"}, {rows, N}), *s = stream_here(v[5]);
+        call("tw_expert_gemm", [&] {
+            return tw_expert_gemm(a, b, c, at, rows, N, K, static_cast<int>(experts), static_cast<int>(layout), s);
+        });
+        return C.release();
+    });
+}
+
+// A, dC, offsets, b_layout, dB, stream
+PyObject *py_expert_gemm_backward(PyObject *, PyObject *const *v, Py_ssize_t n)
+{
+    return entry("expert_gemm_backward", n, 6, [&] {
+        const at::Tensor &A = sized(v[0], {"A"}, 2, "A must be [rows, K]");
+        const at::Tensor &D = sized(v[1], {"dC"}, 2, "dC must be [rows, N]");
+        const at::Tensor &at_e = sized(v[2], {"offsets"}, 1, "offsets must be [n_experts + 1]");
+        const int64_t rows = A.size(0), K = A.size(1), N = D.size(1), experts = at_e.size(0) - 1, layout = b_layout(v[3]);
+        const void *a = bf16_array(v[0], {"A"}, {rows, K}), *d = bf16_array(v[1], {"dC"}, {rows, N});
+        const int32_t *at = expert_offsets(v[2], experts);
+        const int64_t nk[] = {experts, N, K}, kn[] = {experts, K, N};
+        const at::IntArrayRef shape = layout == TW_B_NK ? at::IntArrayRef(nk) : at::IntArrayRef(kn);
+        Ref dB = given_or_empty(v[4], A, shape, at::kBFloat16);
+        void *b = bf16_array(dB.o, {"dB"}, shape), *s = stream_here(v[5]);
+        call("tw_expert_gemm_backward", [&] {
+            return tw_expert_gemm_backward(a, d, b, at, rows, N, K, static_cast<int>(experts), static_cast<int>(layout), s);
+        });
+        return dB.release();
+    });
+}
+
+// The gated activation's sizes: x [rows, 2F]
+struct Gate {
+    int64_t rows, F;
+    const int32_t *limit = nullptr;
+    Gate(PyObject *x, PyObject *o)
+    {
+        const at::Tensor &t = sized(x, {"x"}, 2, "x must be [rows, 2F]");
+        if (t.size(1) % 2) fail(PyExc_ValueError, "x must be [rows, 2F]");
+        rows = t.size(0);
+        F = t.size(1) / 2;
+        if (o != Py_None) limit = int32_array(o, {"limit"}, {1});
+    }
+};
+
+// x, limit, out, stream
+PyObject *py_gated_silu(PyObject *, PyObject *const *v, Py_ssize_t n)
+{
+    return entry("gated_silu", n, 4, [&] {
+        const at::Tensor &x = gpu_tensor(v[0], {"x"});
+        const Gate g(v[0], v[1]);
+        Ref out = given_or_empty(v[2], x, {g.rows, g.F}, at::kBFloat16);
+        const void *from = bf16_array(v[0], {"x"}, {g.rows, 2 * g.F});
+        void *to = bf16_array(out.o, {"out"}, {g.rows, g.F}), *s = stream_here(v[3]);
+        call("tw_gated_silu", [&] { return tw_gated_silu(from, g.rows, g.F, g.limit, to, s); });
+        return out.release();
+    });
+}
+
+// dout, x, limit, dx, stream
+PyObject *py_gated_silu_backward(PyObject *, PyObject *const *v, Py_ssize_t n)
+{
+    return entry("gated_silu_backward", n, 5, [&] {
+        const at::Tensor &x = gpu_tensor(v[1], {"x"});
+        const Gate g(v[1], v[2]);
+        Ref dx = given_or_empty(v[3], x, {g.rows, 2 * g.F}, at::kBFloat16);
+        const void *d = bf16_array(v[0], {"dout"}, {g.rows, g.F}), *from = bf16_array(v[1], {"x"}, {g.rows, 2 * g.F});
+        void *to = bf16_array(dx.o, {"dx"}, {g.rows, 2 * g.F}), *s = stream_here(v[4]);
+        call("tw_gated_silu_backward", [&] { return tw_gated_silu_backward(d, from, g.rows, g.F, g.limit, to, s); });
+        return dx.release();
+    });
+}
+
+// Rows of heads of the shape that others have: pointer and row stride.
+void *heads_ptr(PyObject *o, const Name &n, at::IntArrayRef shape, int64_t *stride)
+{
+    const at::Tensor &t = typed(o, n, at::kBFloat16, "bfloat16");
+    check_shape(o, t, n, shape);
+    *stride = heads_stride(t, n);
+    return t.data_ptr();
+}
+
+struct Rope {
+    tw_qk_norm_rope_args a = {};
+    Ref q_out, k_out, q_weight, k_weight;
+    int64_t q_shape[3], k_shape[3];
+    // q and k: tensors of the queries' and the keys' shapes (what comes in, or the gradients)
+    void fill(PyObject *Q, const char *q_name, PyObject *K, const char *k_name, PyObject *positions, PyObject *rotation, PyObject *wq,
+              PyObject *wk, PyObject *eps, PyObject *interleaved, PyObject *to_q, const char *to_q_name, PyObject *to_k, const char *to_k_name)
+    {
+        const at::Tensor &q = gpu_tensor(Q, {q_name}), &k = gpu_tensor(K, {k_name});
+        if (q.dim() != 3 || k.dim() != 3) fail(PyExc_ValueError, "%s and %s must be [tokens, heads, head_dim]", q_name, k_name);
+        const int64_t tokens = q.size(0), dim = q.size(2);
+        if (q.size(1) > INT32_MAX || k.size(1) > INT32_MAX || dim > INT32_MAX) fail(PyExc_ValueError, "too many heads");
+        for (int i = 0; i < 3; ++i) {
+            q_shape[i] = q.size(i);
+            k_shape[i] = i == 1 ? k.size(1) : q.size(i);
+        }
+        a.tokens = tokens;
+        a.q_heads = static_cast<int>(q.size(1));
+        a.kv_heads = static_cast<int>(k.size(1));
+        a.head_dim = static_cast<int>(dim);
+        a.eps = as_float(eps);
+        a.interleaved = as_bool(interleaved);
+        if ((positions == Py_None) != (rotation == Py_None)) fail(PyExc_ValueError, "positions and rotation belong together");
+        if ((wq == Py_None) != (wk == Py_None)) fail(PyExc_ValueError, "q_weight and k_weight belong together");
+        if (positions != Py_None) {
+            const at::Tensor &at = here(sized(positions, {"positions"}, 1, "positions must be [tokens]"), {"positions"});
+            if (at.scalar_type() != at::kInt && at.scalar_type() != at::kLong) {
+                Ref dt = attr_str(positions, "dtype");
+                bad_tensor(PyExc_TypeError, "%U must be int32 or int64, got %S", {"positions"}, dt.o);
+            }
+            if (!at.is_contiguous()) bad_tensor(PyExc_ValueError, "%U must be contiguous", {"positions"});
+            check_shape(positions, at, {"positions"}, {tokens});
+            a.positions = at.data_ptr();
+            a.position_bytes = at.scalar_type() == at::kInt ? 4 : 8;
+            const at::Tensor &r = sized(rotation, {"rotation"}, 2, "rotation must be [n_positions, rot_dim]");
+            a.rotation = float_array(rotation, {"rotation"}, r.sizes());
+            a.n_positions = r.size(0);
+            if (r.size(1) > dim) fail(PyExc_ValueError, "rotation has more columns than a head");
+            a.rot_dim = static_cast<int>(r.size(1));
+            if (r.numel() == 0) fail(PyExc_ValueError, "rotation must be [n_positions, rot_dim]");
+        }
+        if (wq != Py_None) {
+            a.q_weight = bf16_array(wq, {"q_weight"}, {dim});
+            a.k_weight = bf16_array(wk, {"k_weight"}, {dim});
+        }
+        q_out = given_or_empty(to_q, q, q_shape, at::kBFloat16);
+        k_out = given_or_empty(to_k, q, k_shape, at::kBFloat16);
+        a.q_out = heads_ptr(q_out.o, {to_q_name}, q_shape, &a.q_out_stride);
+        a.k_out = heads_ptr(k_out.o, {to_k_name}, k_shape, &a.k_out_stride);
+    }
+};
+
+// q, k, positions, rotation, q_weight, k_weight, eps, interleaved, q_out, k_out, stream
+PyObject *py_qk_norm_rope(PyObject *, PyObject *const *v, Py_ssize_t n)
+{
+    return entry("qk_norm_rope", n, 11, [&] {
+        Rope t;
+        t.fill(v[0], "q", v[1], "k", v[2], v[3], v[4], v[5], v[6], v[7], v[8], "q_out", v[9], "k_out");
+        t.a.q = heads_ptr(v[0], {"q"}, t.q_shape, &t.a.q_stride);
+        t.a.k = heads_ptr(v[1], {"k"}, t.k_shape, &t.a.k_stride);
+        void *s = stream_here(v[10]);
+        call("tw_qk_norm_rope", [&] { return tw_qk_norm_rope(&t.a, s); });
+        return pair(t.q_out, t.k_out);
+    });
+}
+
+// dq, dk, positions, rotation, q, k, q_weight, k_weight, eps, interleaved, dq_out, dk_out, dq_weight, dk_weight, workspace, stream
+PyObject *py_qk_norm_rope_backward(PyObject *, PyObject *const *v, Py_ssize_t n)
+{
+    return entry("qk_norm_rope_backward", n, 16, [&]() -> PyObject * {
+        Rope t;
+        t.fill(v[0], "dq", v[1], "dk", v[2], v[3], v[6], v[7], v[8], v[9], v[10], "dq_out", v[11], "dk_out");
+        t.a.dq = heads_ptr(v[0], {"dq"}, t.q_shape, &t.a.dq_stride);
+        t.a.dk = heads_ptr(v[1], {"dk"}, t.k_shape, &t.a.dk_stride);
+        const bool norm = v[6] != Py_None;
+        Ref wq, wk;
+        const at::Tensor &like = THPVariable_Unpack(v[0]);
+        if (norm) {
+            t.a.q = heads_ptr(v[4], {"q"}, t.q_shape, &t.a.q_stride);
+            t.a.k = heads_ptr(v[5], {"k"}, t.k_shape, &t.a.k_stride);
+            wq = given_or_empty(v[12], like, {t.q_shape[2]}, at::kFloat);
+            wk = given_or_empty(v[13], like, {t.q_shape[2]}, at::kFloat);
+            t.a.dq_weight = float_array(wq.o, {"dq_weight"}, {t.q_shape[2]});
+            t.a.dk_weight = float_array(wk.o, {"dk_weight"}, {t.q_shape[2]});
+        }
+        void *s = stream_here(v[15]);
+        Workspace w;
+        w.fill(v[14], tw_qk_norm_rope_backward_workspace_bytes(&t.a), like, s);
+        call("tw_qk_norm_rope_backward", [&] { return tw_qk_norm_rope_backward(&t.a, w.p, w.bytes, s); });
+        return PyTuple_Pack(4, t.q_out.o, t.k_out.o, norm ? wq.o : Py_None, norm ? wk.o : Py_None);
+    });
+}
+
 // ---- for the entry points that binding.py calls through ctypes ----
 
 struct Buffer {
@@ -906,6 +1098,9 @@ PyMethodDef g_methods[] = {TW_METHOD(reduce_add_rmsnorm), TW_METHOD(split_launch
                            TW_METHOD(fill_layer),         TW_METHOD(bf16_ptr),         TW_METHOD(stream_handle),
                            TW_METHOD(set_error),          TW_METHOD(attention),        TW_METHOD(expert_sort),
                            TW_METHOD(expert_dispatch),    TW_METHOD(expert_combine),   TW_METHOD(expert_combine_backward),
+                           TW_METHOD(expert_gemm),        TW_METHOD(expert_gemm_backward),
+                           TW_METHOD(gated_silu),         TW_METHOD(gated_silu_backward),
+                           TW_METHOD(qk_norm_rope),       TW_METHOD(qk_norm_rope_backward),
                            {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_twpy", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};
 

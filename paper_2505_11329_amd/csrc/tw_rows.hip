@@ -1,0 +1,648 @@
+// What a layer does row by row beside its products: the gated activation and its gradient; norms and position rotation of
+// queries and keys, and their gradient.
+#include <algorithm>
+#include <cmath>
+
+#include "tw_device.h"
+#include "tw_internal.h"
+
+namespace tw {
+
+typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
+typedef float f32x4_t __attribute__((ext_vector_type(4)));
+
+static constexpr float kLog2e = 1.44269504088896340736f;
+
+// ---- gated activation ----
+//
+// Bound by memory: three (backward five) pieces of 16 bytes to a thread.
+
+struct GateParams {
+    const char *x, *dout;
+    char *out;             // out | dx
+    const int32_t *limit;
+    int64_t first, end;    // rows of the launch
+    uint32_t pieces;       // 16-byte pieces of F columns
+};
+
+// 1 / (1 + exp(-g)) without overflow: by exp(-|g|), which is at most 1.
+__device__ __forceinline__ float sigmoid(float g)
+{
+    const float e = __builtin_amdgcn_exp2f(-fabsf(g) * kLog2e);
+    return (g >= 0.0f ? 1.0f : e) * __builtin_amdgcn_rcpf(1.0f + e);
+}
+
+template <bool STREAMED>
+__device__ __forceinline__ void put(char *to, int64_t piece, u32x4 v)
+{
+    u32x4 *const at = reinterpret_cast<u32x4 *>(to) + piece;
+    if constexpr (STREAMED) __builtin_nontemporal_store(v, at);
+    else *at = v;
+}
+
+template <bool BACKWARD, bool STREAMED>
+__global__ __launch_bounds__(256) void gated_silu_kernel(GateParams p)
+{
+    const uint32_t i = blockIdx.x * 256u + threadIdx.x, in_launch = i / p.pieces, c = i - in_launch * p.pieces;
+    const int64_t row = p.first + in_launch;
+    if (row >= (p.limit ? min(static_cast<int64_t>(*p.limit), p.end) : p.end)) return;
+    const u32x4 *const x = reinterpret_cast<const u32x4 *>(p.x) + row * 2 * p.pieces + c;
+    float g[8], u[8];
+    const u32x4 vg = __builtin_nontemporal_load(x), vu = __builtin_nontemporal_load(x + p.pieces);
+    unpack8(vg, g);
+    unpack8(vu, u);
+    if constexpr (!BACKWARD) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) u[k] *= g[k] * sigmoid(g[k]);
+        put<STREAMED>(p.out, row * p.pieces + c, pack8(u));
+    } else {
+        float d[8];
+        unpack8(__builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(p.dout) + row * p.pieces + c), d);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const float s = sigmoid(g[k]), gs = g[k] * s;
+            g[k] = d[k] * u[k] * fmaf(gs, 1.0f - s, s);
+            u[k] = d[k] * gs;
+        }
+        put<STREAMED>(p.out, row * 2 * p.pieces + c, pack8(g));
+        put<STREAMED>(p.out, row * 2 * p.pieces + p.pieces + c, pack8(u));
+    }
+}
+
+// ---- norms and rotation ----
+//
+// A head belongs to a group of up to 16 lanes, each of which has two chunks of V columns of it: of rotated halves the two whose
+// columns are pairs, so that nothing but the norm's sum goes from lane to lane. A group works on every slots-th head of one
+// token: the angles are read once for them. Bound by memory.
+
+struct RopeParams {
+    const char *in[2], *dy[2];   // queries, keys
+    char *out[2];
+    int64_t in_stride[2], dy_stride[2], out_stride[2];  // bytes
+    const char *weight[2];
+    const void *positions;
+    const float *rotation;
+    float *part;                 // gradient: each workgroup's sums, [2 x dim]
+    int64_t tokens, n_positions;
+    int position_bytes, q_heads, heads, dim, rot, interleaved;
+    int lanes_log2, slots;
+    float eps, inv_dim;
+};
+
+template <int V>
+struct Chunk {
+    float f[V];
+};
+template <int V>
+__device__ __forceinline__ void load_chunk(const char *from, float (&f)[V])
+{
+    if constexpr (V == 8) {
+        unpack8(*reinterpret_cast<const u32x4 *>(from), f);
+    } else {
+        const u32x2_t v = *reinterpret_cast<const u32x2_t *>(from);
+        f[0] = bf16_lo(v.x);
+        f[1] = bf16_hi(v.x);
+        f[2] = bf16_lo(v.y);
+        f[3] = bf16_hi(v.y);
+    }
+}
+template <int V>
+__device__ __forceinline__ void store_chunk(char *to, const float (&f)[V])
+{
+    if constexpr (V == 8) *reinterpret_cast<u32x4 *>(to) = pack8(f);
+    else *reinterpret_cast<u32x2_t *>(to) = u32x2_t{pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3])};
+}
+
+// A lane's two chunks of a head, and whether their columns are rotated.
+struct Columns {
+    int c[2];       // first column
+    bool has[2], turned[2];
+};
+template <int V>
+__device__ __forceinline__ Columns lane_columns(const RopeParams &p, int j)
+{
+    const int n = p.dim / V;
+    Columns l;
+    if (p.interleaved) {
+        const int half = (n + 1) / 2;
+        l.c[0] = j * V;
+        l.c[1] = (j + half) * V;
+        l.has[0] = j < half;
+        l.has[1] = l.has[0] && j + half < n;
+        l.turned[0] = l.c[0] < p.rot;
+        l.turned[1] = l.c[1] < p.rot;
+    } else {
+        const int pairs = p.rot / 2 / V, rest = pairs + 2 * (j - pairs) + pairs;
+        const bool paired = j < pairs;
+        l.c[0] = (paired ? j : rest) * V;
+        l.c[1] = (paired ? j + pairs : rest + 1) * V;
+        l.has[0] = l.c[0] < p.dim;
+        l.has[1] = l.c[1] < p.dim;
+        l.turned[0] = l.turned[1] = paired;
+    }
+    return l;
+}
+
+// cos and sin of a lane's pairs: V of them where its chunks are halves, V / 2 to each chunk where pairs are neighbours.
+template <int V>
+__device__ __forceinline__ void load_angles(const RopeParams &p, const Columns &l, int64_t position, float (&cs)[V], float (&sn)[V])
+{
+    const float *const row = p.rotation + position * p.rot;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const int at = p.interleaved ? l.c[h] / 2 : l.c[0] + h * (V / 2);
+#pragma unroll
+        for (int i = 0; i < V / 2; ++i) {
+            cs[h * (V / 2) + i] = 1.0f;
+            sn[h * (V / 2) + i] = 0.0f;
+        }
+        if (l.turned[h])
+#pragma unroll
+            for (int i = 0; i < V / 2; ++i) {
+                cs[h * (V / 2) + i] = row[at + i];
+                sn[h * (V / 2) + i] = row[p.rot / 2 + at + i];
+            }
+    }
+}
+
+template <int V, bool BACK>
+__device__ __forceinline__ void turn(const RopeParams &p, const Columns &l, const float (&cs)[V], const float (&sn)[V], float (&x0)[V],
+                                     float (&x1)[V])
+{
+    if (!p.interleaved) {
+        if (!l.turned[0]) return;
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            const float s = BACK ? -sn[i] : sn[i], a = x0[i], b = x1[i];
+            x0[i] = a * cs[i] - b * s;
+            x1[i] = b * cs[i] + a * s;
+        }
+    } else {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            if (!l.turned[h]) continue;
+            float(&x)[V] = h ? x1 : x0;
+#pragma unroll
+            for (int i = 0; i < V / 2; ++i) {
+                const float c = cs[h * (V / 2) + i], s = BACK ? -sn[h * (V / 2) + i] : sn[h * (V / 2) + i], a = x[2 * i], b = x[2 * i + 1];
+                x[2 * i] = a * c - b * s;
+                x[2 * i + 1] = b * c + a * s;
+            }
+        }
+    }
+}
+
+// The token's position, -1 for padding.
+__device__ __forceinline__ int64_t position_of(const RopeParams &p, int64_t token)
+{
+    if (!p.positions) return 0;
+    const int64_t at = p.position_bytes == 8 ? static_cast<const int64_t *>(p.positions)[token] : static_cast<const int32_t *>(p.positions)[token];
+    return at >= 0 && at < p.n_positions ? at : -1;
+}
+
+__device__ __forceinline__ int64_t head_at(const RopeParams &p, const int64_t (&stride)[2], int64_t token, int which, int head)
+{
+    return token * stride[which] + static_cast<int64_t>(which ? head - p.q_heads : head) * p.dim * 2;
+}
+
+template <int V, bool NORM>
+__global__ __launch_bounds__(256) void qk_norm_rope_kernel(RopeParams p)
+{
+    const int lanes = 1 << p.lanes_log2, j = threadIdx.x & (lanes - 1);
+    const int64_t item = (static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x) >> p.lanes_log2;
+    const int64_t token = item / p.slots;
+    const int slot = static_cast<int>(item - token * p.slots);
+    if (token >= p.tokens) return;
+    const int64_t position = position_of(p, token);
+    if (position < 0) return;
+    const Columns l = lane_columns<V>(p, j);
+    float cs[V], sn[V], w[2][2][V];
+    if (p.rotation) load_angles<V>(p, l, position, cs, sn);
+    if constexpr (NORM)
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+                if (l.has[h]) load_chunk<V>(p.weight[t] + l.c[h] * 2, w[t][h]);
+    for (int head = slot; head < p.heads; head += p.slots) {
+        const int t = head >= p.q_heads;
+        const char *const from = p.in[t] + head_at(p, p.in_stride, token, t, head);
+        float x[2][V] = {};
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+            if (l.has[h]) load_chunk<V>(from + l.c[h] * 2, x[h]);
+        if constexpr (NORM) {
+            float sum = 0.0f;
+#pragma unroll
+            for (int i = 0; i < V; ++i) sum = fmaf(x[0][i], x[0][i], fmaf(x[1][i], x[1][i], sum));
+            const float r = 1.0f / sqrtf(group_sum(sum, p.lanes_log2) * p.inv_dim + p.eps);
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int i = 0; i < V; ++i) x[h][i] = x[h][i] * r * (t ? w[1][h][i] : w[0][h][i]);
+        }
+        if (p.rotation) turn<V, false>(p, l, cs, sn, x[0], x[1]);
+        char *const to = p.out[t] + head_at(p, p.out_stride, token, t, head);
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+            if (l.has[h]) store_chunk<V>(to + l.c[h] * 2, x[h]);
+    }
+}
+
+// The gradient. The sums over tokens of the weights' gradient stay in registers; the workgroup's groups are added in their order.
+template <int V, bool NORM>
+__global__ __launch_bounds__(256) void qk_norm_rope_backward_kernel(RopeParams p)
+{
+    extern __shared__ float sums[];  // [groups x 2 x dim]
+    const int lanes = 1 << p.lanes_log2, j = threadIdx.x & (lanes - 1), groups = 256 >> p.lanes_log2;
+    const Columns l = lane_columns<V>(p, j);
+    float cs[V], sn[V], w[2][2][V], dw[2][2][V] = {};
+    if constexpr (NORM)
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+                if (l.has[h]) load_chunk<V>(p.weight[t] + l.c[h] * 2, w[t][h]);
+    const int64_t items = p.tokens * p.slots, step = static_cast<int64_t>(gridDim.x) * groups;
+    for (int64_t item = static_cast<int64_t>(blockIdx.x) * groups + (threadIdx.x >> p.lanes_log2); item < items; item += step) {
+        const int64_t token = item / p.slots;
+        const int slot = static_cast<int>(item - token * p.slots);
+        const int64_t position = position_of(p, token);
+        if (position < 0) continue;
+        if (p.rotation) load_angles<V>(p, l, position, cs, sn);
+        for (int head = slot; head < p.heads; head += p.slots) {
+            const int t = head >= p.q_heads;
+            const char *const from = p.dy[t] + head_at(p, p.dy_stride, token, t, head);
+            float d[2][V] = {}, x[2][V] = {};
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+                if (l.has[h]) load_chunk<V>(from + l.c[h] * 2, d[h]);
+            if constexpr (NORM) {
+                const char *const was = p.in[t] + head_at(p, p.in_stride, token, t, head);
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+                    if (l.has[h]) load_chunk<V>(was + l.c[h] * 2, x[h]);
+            }
+            if (p.rotation) turn<V, true>(p, l, cs, sn, d[0], d[1]);
+            if constexpr (NORM) {
+                float square = 0.0f, along = 0.0f;
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int i = 0; i < V; ++i) {
+                        square = fmaf(x[h][i], x[h][i], square);
+                        if (l.has[h]) along = fmaf(d[h][i] * (t ? w[1][h][i] : w[0][h][i]), x[h][i], along);
+                    }
+                const float r = 1.0f / sqrtf(group_sum(square, p.lanes_log2) * p.inv_dim + p.eps);
+                const float back = group_sum(along, p.lanes_log2) * p.inv_dim * r * r;
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int i = 0; i < V; ++i) {
+                        const float n = d[h][i] * x[h][i] * r;
+                        dw[0][h][i] += t ? 0.0f : n;
+                        dw[1][h][i] += t ? n : 0.0f;
+                        d[h][i] = r * (d[h][i] * (t ? w[1][h][i] : w[0][h][i]) - x[h][i] * back);
+                    }
+            }
+            char *const to = p.out[t] + head_at(p, p.out_stride, token, t, head);
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+                if (l.has[h]) store_chunk<V>(to + l.c[h] * 2, d[h]);
+        }
+    }
+    if constexpr (NORM) {
+        float *const mine = sums + (threadIdx.x >> p.lanes_log2) * 2 * p.dim;
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+                if (l.has[h])
+#pragma unroll
+                    for (int i = 0; i < V; ++i) mine[t * p.dim + l.c[h] + i] = dw[t][h][i];
+        __syncthreads();
+        for (int c = threadIdx.x; c < 2 * p.dim; c += 256) {
+            float sum = 0.0f;
+            for (int g = 0; g < groups; ++g) sum += sums[g * 2 * p.dim + c];
+            p.part[static_cast<int64_t>(blockIdx.x) * 2 * p.dim + c] = sum;
+        }
+    }
+}
+
+// The workgroups' sums of 16 columns: 16 of each column's at a time, then those in order.
+__global__ __launch_bounds__(256) void qk_norm_rope_join_kernel(const float *part, int parts, int dim, float *dq_weight, float *dk_weight)
+{
+    __shared__ float sums[16][16];
+    const int in = threadIdx.x & 15, row = threadIdx.x >> 4, c = blockIdx.x * 16 + in;
+    float sum = 0.0f;
+    if (c < 2 * dim)
+        for (int g = row; g < parts; g += 16) sum += part[static_cast<int64_t>(g) * 2 * dim + c];
+    sums[row][in] = sum;
+    __syncthreads();
+    if (row != 0 || c >= 2 * dim) return;
+    for (int g = 1; g < 16; ++g) sum += sums[g][in];
+    (c < dim ? dq_weight[c] : dk_weight[c - dim]) = sum;
+}
+
+// ---- host ----
+
+static bool aligned_to(const void *p, unsigned bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0; }
+
+static tw_status gate_sizes(int64_t rows, int64_t F)
+{
+    if (rows < 0 || F < 1) return TW_ERR_SHAPE;
+    return F % 8 != 0 || F > TW_MAX_H || rows > INT32_MAX ? TW_ERR_UNSUPPORTED : TW_OK;
+}
+
+static tw_status launch_gate(GateParams p, int64_t rows, int64_t F, bool backward, void *stream)
+{
+    p.pieces = static_cast<uint32_t>(F / 8);
+    const bool streamed = rows * F * (backward ? 4 : 2) > kLastLevelCacheBytes / 2;
+    auto *const kernel = backward ? (streamed ? gated_silu_kernel<true, true> : gated_silu_kernel<true, false>)
+                                  : (streamed ? gated_silu_kernel<false, true> : gated_silu_kernel<false, false>);
+    // a launch has fewer than 2^31 pieces
+    const int64_t most = (int64_t(1) << 30) / p.pieces;
+    for (; p.first < rows; p.first = p.end) {
+        p.end = std::min(p.first + most, rows);
+        const int64_t pieces = (p.end - p.first) * p.pieces;
+        TW_HIP(launch_kernel(kernel, dim3(static_cast<uint32_t>((pieces + 255) / 256)), dim3(256), 0, static_cast<hipStream_t>(stream), p));
+    }
+    return TW_OK;
+}
+
+// Rows of `width` bytes every `stride`: whether any byte belongs to both. Of rows with one stride, columns that are apart are apart.
+struct RowSet {
+    const void *p;
+    int64_t stride, width;
+};
+static bool rows_overlap(const RowSet &a, const RowSet &b, int64_t rows)
+{
+    const uint64_t a_bytes = static_cast<uint64_t>((rows - 1) * a.stride + a.width), b_bytes = static_cast<uint64_t>((rows - 1) * b.stride + b.width);
+    if (!ranges_overlap(a.p, a_bytes, b.p, b_bytes)) return false;
+    if (a.stride != b.stride) return true;
+    int64_t ahead = static_cast<int64_t>(reinterpret_cast<uintptr_t>(b.p) - reinterpret_cast<uintptr_t>(a.p)) % a.stride;
+    if (ahead < 0) ahead += a.stride;
+    return ahead < a.width || ahead + b.width > a.stride;
+}
+
+static tw_status rope_sizes(const tw_qk_norm_rope_args &a)
+{
+    if (a.tokens < 0 || a.q_heads < 1 || a.kv_heads < 1 || a.head_dim < 1 || !(a.eps >= 0.0f) || std::isinf(a.eps)) return TW_ERR_SHAPE;
+    if (a.tokens > INT32_MAX || a.q_heads > TW_MAX_HEADS || a.kv_heads > TW_MAX_HEADS || a.head_dim % 8 != 0 || a.head_dim > TW_MAX_HEAD_DIM)
+        return TW_ERR_UNSUPPORTED;
+    if (a.rotation) {
+        if (a.n_positions < 0 || a.rot_dim < 1 || a.rot_dim > a.head_dim) return TW_ERR_SHAPE;
+        if (a.n_positions > INT32_MAX || a.rot_dim % 8 != 0 || (a.position_bytes != 4 && a.position_bytes != 8)) return TW_ERR_UNSUPPORTED;
+    }
+    return TW_OK;
+}
+
+static tw_status rope_stride(int64_t stride, int64_t width)
+{
+    if (stride < width) return TW_ERR_SHAPE;
+    return stride % 8 != 0 || stride > TW_MAX_ROW_STRIDE ? TW_ERR_UNSUPPORTED : TW_OK;
+}
+
+struct RopeLayout {
+    int v, lanes_log2, slots;
+    int64_t grid;
+};
+static RopeLayout rope_layout(const tw_qk_norm_rope_args &a, bool backward)
+{
+    RopeLayout l;
+    const int rot = a.rotation ? a.rot_dim : 0;
+    l.v = !a.interleaved && rot % 16 != 0 ? 4 : 8;
+    const int chunks = a.head_dim / l.v, pairs = a.interleaved ? 0 : rot / 2 / l.v;
+    const int lanes = pairs + (chunks - 2 * pairs + 1) / 2;
+    l.lanes_log2 = 0;
+    while ((1 << l.lanes_log2) < lanes) ++l.lanes_log2;
+    const int heads = a.q_heads + a.kv_heads, groups = 256 >> l.lanes_log2;
+    // a head to a group until there are enough groups for the device, then up to eight
+    int each = 1;
+    while (each < 8 && a.tokens * heads / (each * 2) >= int64_t(groups) * 1024) each *= 2;
+    l.slots = (heads + each - 1) / each;
+    l.grid = (a.tokens * l.slots + groups - 1) / groups;
+    if (backward) l.grid = std::min<int64_t>(l.grid, 1024);
+    return l;
+}
+
+static RopeParams rope_params(const tw_qk_norm_rope_args &a, const RopeLayout &l)
+{
+    RopeParams p = {};
+    p.in[0] = static_cast<const char *>(a.q);
+    p.in[1] = static_cast<const char *>(a.k);
+    p.out[0] = static_cast<char *>(a.q_out);
+    p.out[1] = static_cast<char *>(a.k_out);
+    p.in_stride[0] = a.q_stride * 2;
+    p.in_stride[1] = a.k_stride * 2;
+    p.out_stride[0] = a.q_out_stride * 2;
+    p.out_stride[1] = a.k_out_stride * 2;
+    p.weight[0] = static_cast<const char *>(a.q_weight);
+    p.weight[1] = static_cast<const char *>(a.k_weight);
+    p.positions = a.positions;
+    p.rotation = a.rotation;
+    p.tokens = a.tokens;
+    p.n_positions = a.n_positions;
+    p.position_bytes = a.position_bytes;
+    p.q_heads = a.q_heads;
+    p.heads = a.q_heads + a.kv_heads;
+    p.dim = a.head_dim;
+    p.rot = a.rotation ? a.rot_dim : 0;
+    p.interleaved = a.interleaved != 0;
+    p.lanes_log2 = l.lanes_log2;
+    p.slots = l.slots;
+    p.eps = a.eps;
+    p.inv_dim = 1.0f / static_cast<float>(a.head_dim);
+    return p;
+}
+
+// What both directions ask of the arguments; `read` are the gradients' inputs besides.
+static tw_status rope_tensors(const tw_qk_norm_rope_args &a, bool backward)
+{
+    const bool norm = a.q_weight != nullptr;
+    if (norm != (a.k_weight != nullptr) || (a.rotation != nullptr) != (a.positions != nullptr) || (!norm && !a.rotation)) return TW_ERR_NULL;
+    const bool reads_x = !backward || norm;
+    if (!a.q_out || !a.k_out || (reads_x && (!a.q || !a.k)) || (backward && (!a.dq || !a.dk)) ||
+        (backward && norm && (!a.dq_weight || !a.dk_weight)))
+        return TW_ERR_NULL;
+    const int64_t q_width = int64_t(a.q_heads) * a.head_dim, k_width = int64_t(a.kv_heads) * a.head_dim;
+    TW_TRY(rope_stride(a.q_out_stride, q_width));
+    TW_TRY(rope_stride(a.k_out_stride, k_width));
+    if (reads_x) {
+        TW_TRY(rope_stride(a.q_stride, q_width));
+        TW_TRY(rope_stride(a.k_stride, k_width));
+    }
+    if (backward) {
+        TW_TRY(rope_stride(a.dq_stride, q_width));
+        TW_TRY(rope_stride(a.dk_stride, k_width));
+    }
+    if (!aligned16(a.q_out) || !aligned16(a.k_out) || (reads_x && (!aligned16(a.q) || !aligned16(a.k))) ||
+        (backward && (!aligned16(a.dq) || !aligned16(a.dk))) || !aligned16(a.rotation) || !aligned16(a.q_weight) || !aligned16(a.k_weight) ||
+        (a.positions && !aligned_to(a.positions, a.position_bytes)) ||
+        (backward && norm && (!aligned_to(a.dq_weight, 4) || !aligned_to(a.dk_weight, 4))))
+        return TW_ERR_ALIGN;
+    const RowSet out[2] = {{a.q_out, a.q_out_stride * 2, q_width * 2}, {a.k_out, a.k_out_stride * 2, k_width * 2}};
+    RowSet read[4];
+    int n_read = 0, of[4];
+    const auto reads = [&](const void *p, int64_t stride, int which) {
+        read[n_read] = {p, stride * 2, out[which].width};
+        of[n_read++] = which;
+    };
+    if (reads_x) {
+        reads(a.q, a.q_stride, 0);
+        reads(a.k, a.k_stride, 1);
+    }
+    if (backward) {
+        reads(a.dq, a.dq_stride, 0);
+        reads(a.dk, a.dk_stride, 1);
+    }
+    if (rows_overlap(out[0], out[1], a.tokens)) return TW_ERR_ALIAS;
+    const struct {
+        const void *p;
+        uint64_t bytes;
+    } flat[] = {{a.positions, static_cast<uint64_t>(a.positions ? a.tokens * a.position_bytes : 0)},
+                {a.rotation, static_cast<uint64_t>(a.rotation ? a.n_positions * a.rot_dim * 4 : 0)},
+                {a.q_weight, norm ? a.head_dim * 2u : 0u},
+                {a.k_weight, norm ? a.head_dim * 2u : 0u},
+                {a.dq_weight, backward && norm ? a.head_dim * 4u : 0u},
+                {a.dk_weight, backward && norm ? a.head_dim * 4u : 0u}};
+    for (int o = 0; o < 2; ++o) {
+        for (int i = 0; i < n_read; ++i) {
+            const bool in_place = of[i] == o && read[i].p == out[o].p && read[i].stride == out[o].stride;
+            if (!in_place && rows_overlap(out[o], read[i], a.tokens)) return TW_ERR_ALIAS;
+        }
+        for (const auto &f : flat)
+            if (ranges_overlap(out[o].p, static_cast<uint64_t>((a.tokens - 1) * out[o].stride + out[o].width), f.p, f.bytes)) return TW_ERR_ALIAS;
+    }
+    for (int w = 4; w < 6; ++w) {
+        for (int i = 0; i < w; ++i)
+            if (ranges_overlap(flat[w].p, flat[w].bytes, flat[i].p, flat[i].bytes)) return TW_ERR_ALIAS;
+        for (int i = 0; i < n_read; ++i)
+            if (ranges_overlap(flat[w].p, flat[w].bytes, read[i].p, static_cast<uint64_t>((a.tokens - 1) * read[i].stride + read[i].width)))
+                return TW_ERR_ALIAS;
+    }
+    return TW_OK;
+}
+
+// The workspace shares nothing with the call's tensors.
+static tw_status rope_workspace(const tw_qk_norm_rope_args &a, const void *workspace, uint64_t need)
+{
+    const int64_t q = int64_t(a.q_heads) * a.head_dim, k = int64_t(a.kv_heads) * a.head_dim;
+    const struct {
+        const void *p;
+        int64_t stride, width;
+    } rows[] = {{a.q, a.q_stride, q},       {a.k, a.k_stride, k},   {a.q_out, a.q_out_stride, q}, {a.k_out, a.k_out_stride, k},
+                {a.dq, a.dq_stride, q},     {a.dk, a.dk_stride, k}, {a.q_weight, 0, a.head_dim},  {a.k_weight, 0, a.head_dim},
+                {a.dq_weight, 0, 2 * a.head_dim}, {a.dk_weight, 0, 2 * a.head_dim}};
+    for (const auto &r : rows)
+        if (ranges_overlap(workspace, need, r.p, static_cast<uint64_t>((a.tokens - 1) * r.stride + r.width) * 2)) return TW_ERR_ALIAS;
+    if (ranges_overlap(workspace, need, a.positions, a.positions ? static_cast<uint64_t>(a.tokens) * a.position_bytes : 0) ||
+        ranges_overlap(workspace, need, a.rotation, a.rotation ? static_cast<uint64_t>(a.n_positions) * a.rot_dim * 4 : 0))
+        return TW_ERR_ALIAS;
+    return TW_OK;
+}
+
+static tw_status launch_join(const tw_qk_norm_rope_args &a, const float *part, int parts, hipStream_t stream)
+{
+    TW_HIP(launch_kernel(qk_norm_rope_join_kernel, dim3(static_cast<uint32_t>((2 * a.head_dim + 15) / 16)), dim3(256), 0, stream, part, parts,
+                         a.head_dim, a.dq_weight, a.dk_weight));
+    return TW_OK;
+}
+
+}  // namespace tw
+
+using namespace tw;
+
+extern "C" {
+
+tw_status tw_gated_silu(const void *x, int64_t rows, int64_t F, const int32_t *limit, void *out, void *stream)
+{
+    TW_TRY(gate_sizes(rows, F));
+    if (rows == 0) return TW_OK;
+    if (!x || !out) return TW_ERR_NULL;
+    if (!aligned16(x) || !aligned16(out) || !aligned_to(limit, 4)) return TW_ERR_ALIGN;
+    const uint64_t half = static_cast<uint64_t>(rows) * F * 2u;
+    if (ranges_overlap(out, half, x, 2 * half) || ranges_overlap(out, half, limit, limit ? 4 : 0)) return TW_ERR_ALIAS;
+    GateParams p = {};
+    p.x = static_cast<const char *>(x);
+    p.out = static_cast<char *>(out);
+    p.limit = limit;
+    return launch_gate(p, rows, F, false, stream);
+}
+
+tw_status tw_gated_silu_backward(const void *dout, const void *x, int64_t rows, int64_t F, const int32_t *limit, void *dx, void *stream)
+{
+    TW_TRY(gate_sizes(rows, F));
+    if (rows == 0) return TW_OK;
+    if (!dout || !x || !dx) return TW_ERR_NULL;
+    if (!aligned16(dout) || !aligned16(x) || !aligned16(dx) || !aligned_to(limit, 4)) return TW_ERR_ALIGN;
+    const uint64_t half = static_cast<uint64_t>(rows) * F * 2u;
+    if (ranges_overlap(dx, 2 * half, dout, half) || (dx != x && ranges_overlap(dx, 2 * half, x, 2 * half)) ||
+        ranges_overlap(dx, 2 * half, limit, limit ? 4 : 0))
+        return TW_ERR_ALIAS;
+    GateParams p = {};
+    p.x = static_cast<const char *>(x);
+    p.dout = static_cast<const char *>(dout);
+    p.out = static_cast<char *>(dx);
+    p.limit = limit;
+    return launch_gate(p, rows, F, true, stream);
+}
+
+tw_status tw_qk_norm_rope(const tw_qk_norm_rope_args *args, void *stream)
+{
+    if (!args) return TW_ERR_NULL;
+    const tw_qk_norm_rope_args &a = *args;
+    TW_TRY(rope_sizes(a));
+    if (a.tokens == 0) return TW_OK;
+    TW_TRY(rope_tensors(a, false));
+    const RopeLayout l = rope_layout(a, false);
+    const RopeParams p = rope_params(a, l);
+    if (l.grid > (1 << 23)) return TW_ERR_UNSUPPORTED;
+    auto *const kernel = a.q_weight ? (l.v == 8 ? qk_norm_rope_kernel<8, true> : qk_norm_rope_kernel<4, true>)
+                                    : (l.v == 8 ? qk_norm_rope_kernel<8, false> : qk_norm_rope_kernel<4, false>);
+    TW_HIP(launch_kernel(kernel, dim3(static_cast<uint32_t>(l.grid)), dim3(256), 0, static_cast<hipStream_t>(stream), p));
+    return TW_OK;
+}
+
+int64_t tw_qk_norm_rope_backward_workspace_bytes(const tw_qk_norm_rope_args *args)
+{
+    if (!args || rope_sizes(*args) != TW_OK) return -1;
+    if (args->tokens == 0 || !args->q_weight) return 0;
+    return rope_layout(*args, true).grid * 2 * args->head_dim * 4;
+}
+
+tw_status tw_qk_norm_rope_backward(const tw_qk_norm_rope_args *args, void *workspace, int64_t workspace_bytes, void *stream)
+{
+    if (!args) return TW_ERR_NULL;
+    const tw_qk_norm_rope_args &a = *args;
+    TW_TRY(rope_sizes(a));
+    const bool norm = a.q_weight != nullptr;
+    const hipStream_t s = static_cast<hipStream_t>(stream);
+    if (a.tokens == 0) {
+        if (!norm) return TW_OK;
+        if (!a.dq_weight || !a.dk_weight) return TW_ERR_NULL;
+        if (!aligned_to(a.dq_weight, 4) || !aligned_to(a.dk_weight, 4)) return TW_ERR_ALIGN;
+        if (ranges_overlap(a.dq_weight, a.head_dim * 4u, a.dk_weight, a.head_dim * 4u)) return TW_ERR_ALIAS;
+        return launch_join(a, nullptr, 0, s);
+    }
+    TW_TRY(rope_tensors(a, true));
+    const int64_t need = tw_qk_norm_rope_backward_workspace_bytes(args);
+    if (need > 0 && !workspace) return TW_ERR_NULL;
+    if (workspace_bytes < need) return TW_ERR_SHAPE;
+    if (need > 0 && !aligned16(workspace)) return TW_ERR_ALIGN;
+    TW_TRY(rope_workspace(a, workspace, static_cast<uint64_t>(need)));
+    const RopeLayout l = rope_layout(a, true);
+    RopeParams p = rope_params(a, l);
+    p.dy[0] = static_cast<const char *>(a.dq);
+    p.dy[1] = static_cast<const char *>(a.dk);
+    p.dy_stride[0] = a.dq_stride * 2;
+    p.dy_stride[1] = a.dk_stride * 2;
+    p.part = static_cast<float *>(workspace);
+    auto *const kernel = norm ? (l.v == 8 ? qk_norm_rope_backward_kernel<8, true> : qk_norm_rope_backward_kernel<4, true>)
+                              : (l.v == 8 ? qk_norm_rope_backward_kernel<8, false> : qk_norm_rope_backward_kernel<4, false>);
+    const unsigned lds = norm ? (256u >> l.lanes_log2) * 2 * a.head_dim * 4 : 0;
+    TW_HIP(launch_kernel(kernel, dim3(static_cast<uint32_t>(l.grid)), dim3(256), lds, s, p));
+    return norm ? launch_join(a, p.part, static_cast<int>(l.grid), s) : TW_OK;
+}
+
+}  // extern "C"
