@@ -72,58 +72,65 @@ __global__ __launch_bounds__(256) void gated_silu_kernel(GateParams p)
 // ---- norms and rotation ----
 //
 // A head belongs to a group of up to 16 lanes, each of which has two chunks of V columns of it: of rotated halves the two whose
-// columns are pairs, so that nothing but the norm's sum goes from lane to lane. A group works on every slots-th head of one
-// token: the angles are read once for them. Bound by memory.
+// columns are pairs, so that nothing but the norm's sums goes from lane to lane. Bound by memory: 16384 tokens, 32 / 8 heads of 128
+// take 59 us, 5.6 TB/s of what is read and written, as a copy does, 8101 of 28 / 4 heads 27 us. (The angles come from the caches
+// for each head: two, four and eight heads of a token to a group, with their loads under way together, are 3 to 15 % slower.)
+
+// Queries or keys.
+struct RopeSide {
+    const char *in, *dy;
+    char *out;
+    int64_t in_stride, dy_stride, out_stride;  // bytes
+    const char *weight;
+    int heads;
+    int first, grid;  // workgroups of the launch
+};
 
 struct RopeParams {
-    const char *in[2], *dy[2];   // queries, keys
-    char *out[2];
-    int64_t in_stride[2], dy_stride[2], out_stride[2];  // bytes
-    const char *weight[2];
+    RopeSide side[2];
     const void *positions;
     const float *rotation;
-    float *part;                 // gradient: each workgroup's sums, [2 x dim]
-    int64_t tokens, n_positions;
-    int position_bytes, q_heads, heads, dim, rot, interleaved;
-    int lanes_log2, slots;
+    float *part;                 // gradient: each workgroup's sums, [grid x dim]
+    int tokens;
+    int64_t n_positions;
+    int position_bytes, dim, rot;
+    int lanes_log2;
     float eps, inv_dim;
 };
 
 template <int V>
-struct Chunk {
-    float f[V];
+struct Piece;
+template <>
+struct Piece<8> {
+    using T = u32x4;
 };
-template <int V>
-__device__ __forceinline__ void load_chunk(const char *from, float (&f)[V])
+template <>
+struct Piece<4> {
+    using T = u32x2_t;
+};
+
+__device__ __forceinline__ void unpack(const u32x4 &v, float (&f)[8]) { unpack8(v, f); }
+__device__ __forceinline__ void unpack(const u32x2_t &v, float (&f)[4])
 {
-    if constexpr (V == 8) {
-        unpack8(*reinterpret_cast<const u32x4 *>(from), f);
-    } else {
-        const u32x2_t v = *reinterpret_cast<const u32x2_t *>(from);
-        f[0] = bf16_lo(v.x);
-        f[1] = bf16_hi(v.x);
-        f[2] = bf16_lo(v.y);
-        f[3] = bf16_hi(v.y);
-    }
+    f[0] = bf16_lo(v.x);
+    f[1] = bf16_hi(v.x);
+    f[2] = bf16_lo(v.y);
+    f[3] = bf16_hi(v.y);
 }
-template <int V>
-__device__ __forceinline__ void store_chunk(char *to, const float (&f)[V])
-{
-    if constexpr (V == 8) *reinterpret_cast<u32x4 *>(to) = pack8(f);
-    else *reinterpret_cast<u32x2_t *>(to) = u32x2_t{pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3])};
-}
+__device__ __forceinline__ u32x4 pack(const float (&f)[8]) { return pack8(f); }
+__device__ __forceinline__ u32x2_t pack(const float (&f)[4]) { return u32x2_t{pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3])}; }
 
 // A lane's two chunks of a head, and whether their columns are rotated.
 struct Columns {
     int c[2];       // first column
     bool has[2], turned[2];
 };
-template <int V>
+template <int V, bool NEXT>
 __device__ __forceinline__ Columns lane_columns(const RopeParams &p, int j)
 {
     const int n = p.dim / V;
     Columns l;
-    if (p.interleaved) {
+    if constexpr (NEXT) {
         const int half = (n + 1) / 2;
         l.c[0] = j * V;
         l.c[1] = (j + half) * V;
@@ -132,7 +139,7 @@ __device__ __forceinline__ Columns lane_columns(const RopeParams &p, int j)
         l.turned[0] = l.c[0] < p.rot;
         l.turned[1] = l.c[1] < p.rot;
     } else {
-        const int pairs = p.rot / 2 / V, rest = pairs + 2 * (j - pairs) + pairs;
+        const int pairs = p.rot / 2 / V, rest = 2 * pairs + 2 * (j - pairs);
         const bool paired = j < pairs;
         l.c[0] = (paired ? j : rest) * V;
         l.c[1] = (paired ? j + pairs : rest + 1) * V;
@@ -144,13 +151,13 @@ __device__ __forceinline__ Columns lane_columns(const RopeParams &p, int j)
 }
 
 // cos and sin of a lane's pairs: V of them where its chunks are halves, V / 2 to each chunk where pairs are neighbours.
-template <int V>
+template <int V, bool NEXT>
 __device__ __forceinline__ void load_angles(const RopeParams &p, const Columns &l, int64_t position, float (&cs)[V], float (&sn)[V])
 {
     const float *const row = p.rotation + position * p.rot;
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-        const int at = p.interleaved ? l.c[h] / 2 : l.c[0] + h * (V / 2);
+        const int at = NEXT ? l.c[h] / 2 : l.c[0] + h * (V / 2);
 #pragma unroll
         for (int i = 0; i < V / 2; ++i) {
             cs[h * (V / 2) + i] = 1.0f;
@@ -165,183 +172,202 @@ __device__ __forceinline__ void load_angles(const RopeParams &p, const Columns &
     }
 }
 
-template <int V, bool BACK>
-__device__ __forceinline__ void turn(const RopeParams &p, const Columns &l, const float (&cs)[V], const float (&sn)[V], float (&x0)[V],
-                                     float (&x1)[V])
+template <int V, bool NEXT, bool BACK>
+__device__ __forceinline__ void turn(const Columns &l, const float (&cs)[V], const float (&sn)[V], float (&x)[2][V])
 {
-    if (!p.interleaved) {
+    if constexpr (!NEXT) {
         if (!l.turned[0]) return;
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-            const float s = BACK ? -sn[i] : sn[i], a = x0[i], b = x1[i];
-            x0[i] = a * cs[i] - b * s;
-            x1[i] = b * cs[i] + a * s;
+            const float s = BACK ? -sn[i] : sn[i], a = x[0][i], b = x[1][i];
+            x[0][i] = a * cs[i] - b * s;
+            x[1][i] = b * cs[i] + a * s;
         }
     } else {
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             if (!l.turned[h]) continue;
-            float(&x)[V] = h ? x1 : x0;
 #pragma unroll
             for (int i = 0; i < V / 2; ++i) {
-                const float c = cs[h * (V / 2) + i], s = BACK ? -sn[h * (V / 2) + i] : sn[h * (V / 2) + i], a = x[2 * i], b = x[2 * i + 1];
-                x[2 * i] = a * c - b * s;
-                x[2 * i + 1] = b * c + a * s;
+                const float c = cs[h * (V / 2) + i], s = BACK ? -sn[h * (V / 2) + i] : sn[h * (V / 2) + i], a = x[h][2 * i], b = x[h][2 * i + 1];
+                x[h][2 * i] = a * c - b * s;
+                x[h][2 * i + 1] = b * c + a * s;
             }
         }
     }
 }
 
 // The token's position, -1 for padding.
-__device__ __forceinline__ int64_t position_of(const RopeParams &p, int64_t token)
+__device__ __forceinline__ int64_t position_of(const RopeParams &p, int token)
 {
     if (!p.positions) return 0;
     const int64_t at = p.position_bytes == 8 ? static_cast<const int64_t *>(p.positions)[token] : static_cast<const int32_t *>(p.positions)[token];
     return at >= 0 && at < p.n_positions ? at : -1;
 }
 
-__device__ __forceinline__ int64_t head_at(const RopeParams &p, const int64_t (&stride)[2], int64_t token, int which, int head)
+// 1 / sqrt(x), also of numbers so small that the instruction takes them for 0.
+__device__ __forceinline__ float inverse_root(float x)
 {
-    return token * stride[which] + static_cast<int64_t>(which ? head - p.q_heads : head) * p.dim * 2;
+    const bool small = x < 0x1p-100f;
+    return __builtin_amdgcn_rsqf(small ? x * 0x1p60f : x) * (small ? 0x1p30f : 1.0f);
 }
 
-template <int V, bool NORM>
+// NEXT: pairs are neighbours (interleaved), not halves. STREAMED: results of more than half of what the last-level cache holds are
+// written past it.
+template <int V, bool NEXT, bool NORM, bool STREAMED>
 __global__ __launch_bounds__(256) void qk_norm_rope_kernel(RopeParams p)
 {
-    const int lanes = 1 << p.lanes_log2, j = threadIdx.x & (lanes - 1);
-    const int64_t item = (static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x) >> p.lanes_log2;
-    const int64_t token = item / p.slots;
-    const int slot = static_cast<int>(item - token * p.slots);
+    using P = typename Piece<V>::T;
+    const RopeSide &s = p.side[static_cast<int>(blockIdx.x) >= p.side[1].first];
+    const int j = threadIdx.x & ((1 << p.lanes_log2) - 1);
+    const uint32_t item = ((blockIdx.x - s.first) * 256u + threadIdx.x) >> p.lanes_log2, heads = s.heads;
+    const int token = static_cast<int>(item / heads), head = static_cast<int>(item - token * heads);
     if (token >= p.tokens) return;
+    const Columns l = lane_columns<V, NEXT>(p, j);
+    const char *const in = s.in + token * s.in_stride + head * p.dim * 2;
+    char *const out = s.out + token * s.out_stride + head * p.dim * 2;
+    P x[2] = {}, w[2] = {};
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+        if (l.has[h]) x[h] = __builtin_nontemporal_load(reinterpret_cast<const P *>(in + l.c[h] * 2));
     const int64_t position = position_of(p, token);
-    if (position < 0) return;
-    const Columns l = lane_columns<V>(p, j);
-    float cs[V], sn[V], w[2][2][V];
-    if (p.rotation) load_angles<V>(p, l, position, cs, sn);
     if constexpr (NORM)
 #pragma unroll
-        for (int t = 0; t < 2; ++t)
+        for (int h = 0; h < 2; ++h)
+            if (l.has[h]) w[h] = *reinterpret_cast<const P *>(s.weight + l.c[h] * 2);
+    if (position < 0) return;
+    float cs[V], sn[V], f[2][V];
+    if (p.rotation) load_angles<V, NEXT>(p, l, position, cs, sn);
 #pragma unroll
-            for (int h = 0; h < 2; ++h)
-                if (l.has[h]) load_chunk<V>(p.weight[t] + l.c[h] * 2, w[t][h]);
-    for (int head = slot; head < p.heads; head += p.slots) {
-        const int t = head >= p.q_heads;
-        const char *const from = p.in[t] + head_at(p, p.in_stride, token, t, head);
-        float x[2][V] = {};
+    for (int h = 0; h < 2; ++h) unpack(x[h], f[h]);
+    if constexpr (NORM) {
+        float sum = 0.0f;
 #pragma unroll
         for (int h = 0; h < 2; ++h)
-            if (l.has[h]) load_chunk<V>(from + l.c[h] * 2, x[h]);
-        if constexpr (NORM) {
-            float sum = 0.0f;
 #pragma unroll
-            for (int i = 0; i < V; ++i) sum = fmaf(x[0][i], x[0][i], fmaf(x[1][i], x[1][i], sum));
-            const float r = 1.0f / sqrtf(group_sum(sum, p.lanes_log2) * p.inv_dim + p.eps);
+            for (int i = 0; i < V; ++i) sum = fmaf(f[h][i], f[h][i], sum);
+        const float r = inverse_root(group_sum(sum, p.lanes_log2) * p.inv_dim + p.eps);
 #pragma unroll
-            for (int h = 0; h < 2; ++h)
+        for (int h = 0; h < 2; ++h) {
+            float wf[V];
+            unpack(w[h], wf);
 #pragma unroll
-                for (int i = 0; i < V; ++i) x[h][i] = x[h][i] * r * (t ? w[1][h][i] : w[0][h][i]);
+            for (int i = 0; i < V; ++i) f[h][i] = f[h][i] * r * wf[i];
         }
-        if (p.rotation) turn<V, false>(p, l, cs, sn, x[0], x[1]);
-        char *const to = p.out[t] + head_at(p, p.out_stride, token, t, head);
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
-            if (l.has[h]) store_chunk<V>(to + l.c[h] * 2, x[h]);
     }
+    if (p.rotation) turn<V, NEXT, false>(l, cs, sn, f);
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+        if (l.has[h]) {
+            P *const to = reinterpret_cast<P *>(out + l.c[h] * 2);
+            if constexpr (STREAMED) __builtin_nontemporal_store(pack(f[h]), to);
+            else *to = pack(f[h]);
+        }
 }
 
 // The gradient. The sums over tokens of the weights' gradient stay in registers; the workgroup's groups are added in their order.
-template <int V, bool NORM>
+// 16384 tokens, 32 / 8 heads of 128: 98 us, 5.1 TB/s (the next head's loads ahead of this one's work: 101).
+template <int V, bool NEXT, bool NORM, bool STREAMED>
 __global__ __launch_bounds__(256) void qk_norm_rope_backward_kernel(RopeParams p)
 {
-    extern __shared__ float sums[];  // [groups x 2 x dim]
-    const int lanes = 1 << p.lanes_log2, j = threadIdx.x & (lanes - 1), groups = 256 >> p.lanes_log2;
-    const Columns l = lane_columns<V>(p, j);
-    float cs[V], sn[V], w[2][2][V], dw[2][2][V] = {};
+    using P = typename Piece<V>::T;
+    extern __shared__ float sums[];  // [groups x dim]
+    const RopeSide &s = p.side[static_cast<int>(blockIdx.x) >= p.side[1].first];
+    const int j = threadIdx.x & ((1 << p.lanes_log2) - 1), groups = 256 >> p.lanes_log2, group = threadIdx.x >> p.lanes_log2;
+    const Columns l = lane_columns<V, NEXT>(p, j);
+    P w[2] = {};
+    float dw[2][V] = {};
     if constexpr (NORM)
 #pragma unroll
-        for (int t = 0; t < 2; ++t)
+        for (int h = 0; h < 2; ++h)
+            if (l.has[h]) w[h] = *reinterpret_cast<const P *>(s.weight + l.c[h] * 2);
+    const uint32_t heads = s.heads;
+    const int64_t items = static_cast<int64_t>(p.tokens) * s.heads, step = static_cast<int64_t>(s.grid) * groups;
+    for (int64_t item = static_cast<int64_t>(blockIdx.x - s.first) * groups + group; item < items; item += step) {
+        const int token = static_cast<int>(items >> 32 ? item / heads : static_cast<uint32_t>(item) / heads);
+        const int head = static_cast<int>(item - static_cast<int64_t>(token) * heads);
+        const char *const dy = s.dy + token * s.dy_stride + head * p.dim * 2, *const in = s.in + token * s.in_stride + head * p.dim * 2;
+        char *const out = s.out + token * s.out_stride + head * p.dim * 2;
+        P d[2] = {}, x[2] = {};
 #pragma unroll
-            for (int h = 0; h < 2; ++h)
-                if (l.has[h]) load_chunk<V>(p.weight[t] + l.c[h] * 2, w[t][h]);
-    const int64_t items = p.tokens * p.slots, step = static_cast<int64_t>(gridDim.x) * groups;
-    for (int64_t item = static_cast<int64_t>(blockIdx.x) * groups + (threadIdx.x >> p.lanes_log2); item < items; item += step) {
-        const int64_t token = item / p.slots;
-        const int slot = static_cast<int>(item - token * p.slots);
+        for (int h = 0; h < 2; ++h)
+            if (l.has[h]) {
+                d[h] = __builtin_nontemporal_load(reinterpret_cast<const P *>(dy + l.c[h] * 2));
+                if constexpr (NORM) x[h] = __builtin_nontemporal_load(reinterpret_cast<const P *>(in + l.c[h] * 2));
+            }
         const int64_t position = position_of(p, token);
         if (position < 0) continue;
-        if (p.rotation) load_angles<V>(p, l, position, cs, sn);
-        for (int head = slot; head < p.heads; head += p.slots) {
-            const int t = head >= p.q_heads;
-            const char *const from = p.dy[t] + head_at(p, p.dy_stride, token, t, head);
-            float d[2][V] = {}, x[2][V] = {};
+        float cs[V], sn[V], g[2][V];
+        if (p.rotation) load_angles<V, NEXT>(p, l, position, cs, sn);
 #pragma unroll
-            for (int h = 0; h < 2; ++h)
-                if (l.has[h]) load_chunk<V>(from + l.c[h] * 2, d[h]);
-            if constexpr (NORM) {
-                const char *const was = p.in[t] + head_at(p, p.in_stride, token, t, head);
+        for (int h = 0; h < 2; ++h) unpack(d[h], g[h]);
+        if (p.rotation) turn<V, NEXT, true>(l, cs, sn, g);
+        if constexpr (NORM) {
+            float f[2][V], square = 0.0f, along = 0.0f;
 #pragma unroll
-                for (int h = 0; h < 2; ++h)
-                    if (l.has[h]) load_chunk<V>(was + l.c[h] * 2, x[h]);
+            for (int h = 0; h < 2; ++h) {
+                float wf[V];
+                unpack(x[h], f[h]);
+                unpack(w[h], wf);
+#pragma unroll
+                for (int i = 0; i < V; ++i) {
+                    square = fmaf(f[h][i], f[h][i], square);
+                    along = fmaf(g[h][i] * wf[i], f[h][i], along);
+                }
             }
-            if (p.rotation) turn<V, true>(p, l, cs, sn, d[0], d[1]);
-            if constexpr (NORM) {
-                float square = 0.0f, along = 0.0f;
+            const float r = inverse_root(group_sum(square, p.lanes_log2) * p.inv_dim + p.eps);
+            const float back = group_sum(along, p.lanes_log2) * p.inv_dim * r * r;
 #pragma unroll
-                for (int h = 0; h < 2; ++h)
+            for (int h = 0; h < 2; ++h) {
+                float wf[V];
+                unpack(w[h], wf);
 #pragma unroll
-                    for (int i = 0; i < V; ++i) {
-                        square = fmaf(x[h][i], x[h][i], square);
-                        if (l.has[h]) along = fmaf(d[h][i] * (t ? w[1][h][i] : w[0][h][i]), x[h][i], along);
-                    }
-                const float r = 1.0f / sqrtf(group_sum(square, p.lanes_log2) * p.inv_dim + p.eps);
-                const float back = group_sum(along, p.lanes_log2) * p.inv_dim * r * r;
-#pragma unroll
-                for (int h = 0; h < 2; ++h)
-#pragma unroll
-                    for (int i = 0; i < V; ++i) {
-                        const float n = d[h][i] * x[h][i] * r;
-                        dw[0][h][i] += t ? 0.0f : n;
-                        dw[1][h][i] += t ? n : 0.0f;
-                        d[h][i] = r * (d[h][i] * (t ? w[1][h][i] : w[0][h][i]) - x[h][i] * back);
-                    }
+                for (int i = 0; i < V; ++i) {
+                    dw[h][i] = fmaf(g[h][i] * r, f[h][i], dw[h][i]);
+                    g[h][i] = r * (g[h][i] * wf[i] - f[h][i] * back);
+                }
             }
-            char *const to = p.out[t] + head_at(p, p.out_stride, token, t, head);
-#pragma unroll
-            for (int h = 0; h < 2; ++h)
-                if (l.has[h]) store_chunk<V>(to + l.c[h] * 2, d[h]);
         }
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+            if (l.has[h]) {
+                P *const to = reinterpret_cast<P *>(out + l.c[h] * 2);
+                if constexpr (STREAMED) __builtin_nontemporal_store(pack(g[h]), to);
+                else *to = pack(g[h]);
+            }
     }
     if constexpr (NORM) {
-        float *const mine = sums + (threadIdx.x >> p.lanes_log2) * 2 * p.dim;
 #pragma unroll
-        for (int t = 0; t < 2; ++t)
+        for (int h = 0; h < 2; ++h)
+            if (l.has[h])
 #pragma unroll
-            for (int h = 0; h < 2; ++h)
-                if (l.has[h])
-#pragma unroll
-                    for (int i = 0; i < V; ++i) mine[t * p.dim + l.c[h] + i] = dw[t][h][i];
+                for (int i = 0; i < V; ++i) sums[group * p.dim + l.c[h] + i] = dw[h][i];
         __syncthreads();
-        for (int c = threadIdx.x; c < 2 * p.dim; c += 256) {
+        for (int c = threadIdx.x; c < p.dim; c += 256) {
             float sum = 0.0f;
-            for (int g = 0; g < groups; ++g) sum += sums[g * 2 * p.dim + c];
-            p.part[static_cast<int64_t>(blockIdx.x) * 2 * p.dim + c] = sum;
+            for (int g = 0; g < groups; ++g) sum += sums[g * p.dim + c];
+            p.part[static_cast<int64_t>(blockIdx.x) * p.dim + c] = sum;
         }
     }
 }
 
-// The workgroups' sums of 16 columns: 16 of each column's at a time, then those in order.
-__global__ __launch_bounds__(256) void qk_norm_rope_join_kernel(const float *part, int parts, int dim, float *dq_weight, float *dk_weight)
+// The workgroups' sums of 16 columns, of the queries or the keys: 64 of each column's at a time, then those in order.
+__global__ __launch_bounds__(1024) void qk_norm_rope_join_kernel(const float *part, int q_parts, int k_parts, int dim, float *dq_weight,
+                                                                  float *dk_weight)
 {
-    __shared__ float sums[16][16];
+    __shared__ float sums[64][16];
     const int in = threadIdx.x & 15, row = threadIdx.x >> 4, c = blockIdx.x * 16 + in;
+    const float *const from = blockIdx.y ? part + static_cast<int64_t>(q_parts) * dim : part;
+    const int parts = blockIdx.y ? k_parts : q_parts;
     float sum = 0.0f;
-    if (c < 2 * dim)
-        for (int g = row; g < parts; g += 16) sum += part[static_cast<int64_t>(g) * 2 * dim + c];
+    if (c < dim)
+#pragma unroll 8
+        for (int g = row; g < parts; g += 64) sum += from[static_cast<int64_t>(g) * dim + c];
     sums[row][in] = sum;
     __syncthreads();
-    if (row != 0 || c >= 2 * dim) return;
-    for (int g = 1; g < 16; ++g) sum += sums[g][in];
-    (c < dim ? dq_weight[c] : dk_weight[c - dim]) = sum;
+    if (row != 0 || c >= dim) return;
+    for (int g = 1; g < 64; ++g) sum += sums[g][in];
+    (blockIdx.y ? dk_weight : dq_weight)[c] = sum;
 }
 
 // ---- host ----
@@ -404,8 +430,8 @@ static tw_status rope_stride(int64_t stride, int64_t width)
 }
 
 struct RopeLayout {
-    int v, lanes_log2, slots;
-    int64_t grid;
+    int v, lanes_log2;
+    int64_t grid[2];
 };
 static RopeLayout rope_layout(const tw_qk_norm_rope_args &a, bool backward)
 {
@@ -416,44 +442,53 @@ static RopeLayout rope_layout(const tw_qk_norm_rope_args &a, bool backward)
     const int lanes = pairs + (chunks - 2 * pairs + 1) / 2;
     l.lanes_log2 = 0;
     while ((1 << l.lanes_log2) < lanes) ++l.lanes_log2;
-    const int heads = a.q_heads + a.kv_heads, groups = 256 >> l.lanes_log2;
-    // a head to a group until there are enough groups for the device, then up to eight
-    int each = 1;
-    while (each < 8 && a.tokens * heads / (each * 2) >= int64_t(groups) * 1024) each *= 2;
-    l.slots = (heads + each - 1) / each;
-    l.grid = (a.tokens * l.slots + groups - 1) / groups;
-    if (backward) l.grid = std::min<int64_t>(l.grid, 1024);
+    const int64_t groups = 256 >> l.lanes_log2;
+    l.grid[0] = (a.tokens * a.q_heads + groups - 1) / groups;
+    l.grid[1] = (a.tokens * a.kv_heads + groups - 1) / groups;
+    if (backward) {
+        // as many workgroups as 256 compute units hold, four each, shared out by the heads (16384 tokens, 32 / 8 heads: 98 us, with
+        // three each 103, five 111, eight 97; 2000 tokens 20.0, 20.2, 22.3, 22.8)
+        const int64_t most = 1024, k = std::max<int64_t>(1, most * a.kv_heads / (a.q_heads + a.kv_heads));
+        l.grid[0] = std::min(l.grid[0], std::max<int64_t>(1, most - k));
+        l.grid[1] = std::min(l.grid[1], k);
+    }
     return l;
 }
 
 static RopeParams rope_params(const tw_qk_norm_rope_args &a, const RopeLayout &l)
 {
     RopeParams p = {};
-    p.in[0] = static_cast<const char *>(a.q);
-    p.in[1] = static_cast<const char *>(a.k);
-    p.out[0] = static_cast<char *>(a.q_out);
-    p.out[1] = static_cast<char *>(a.k_out);
-    p.in_stride[0] = a.q_stride * 2;
-    p.in_stride[1] = a.k_stride * 2;
-    p.out_stride[0] = a.q_out_stride * 2;
-    p.out_stride[1] = a.k_out_stride * 2;
-    p.weight[0] = static_cast<const char *>(a.q_weight);
-    p.weight[1] = static_cast<const char *>(a.k_weight);
+    const char *const in[2] = {static_cast<const char *>(a.q), static_cast<const char *>(a.k)};
+    const int64_t in_stride[2] = {a.q_stride, a.k_stride}, out_stride[2] = {a.q_out_stride, a.k_out_stride};
+    void *const out[2] = {a.q_out, a.k_out};
+    const void *const weight[2] = {a.q_weight, a.k_weight};
+    for (int i = 0; i < 2; ++i) {
+        RopeSide &s = p.side[i];
+        s.in = in[i];
+        s.out = static_cast<char *>(out[i]);
+        s.in_stride = in_stride[i] * 2;
+        s.out_stride = out_stride[i] * 2;
+        s.weight = static_cast<const char *>(weight[i]);
+        s.heads = i ? a.kv_heads : a.q_heads;
+        s.first = i ? static_cast<int>(l.grid[0]) : 0;
+        s.grid = static_cast<int>(l.grid[i]);
+    }
     p.positions = a.positions;
     p.rotation = a.rotation;
-    p.tokens = a.tokens;
+    p.tokens = static_cast<int>(a.tokens);
     p.n_positions = a.n_positions;
     p.position_bytes = a.position_bytes;
-    p.q_heads = a.q_heads;
-    p.heads = a.q_heads + a.kv_heads;
     p.dim = a.head_dim;
     p.rot = a.rotation ? a.rot_dim : 0;
-    p.interleaved = a.interleaved != 0;
     p.lanes_log2 = l.lanes_log2;
-    p.slots = l.slots;
     p.eps = a.eps;
     p.inv_dim = 1.0f / static_cast<float>(a.head_dim);
     return p;
+}
+
+static bool rope_streamed(const tw_qk_norm_rope_args &a)
+{
+    return a.tokens * (a.q_heads + a.kv_heads) * a.head_dim * 2 > kLastLevelCacheBytes / 2;
 }
 
 // What both directions ask of the arguments; `read` are the gradients' inputs besides.
@@ -524,6 +559,31 @@ static tw_status rope_tensors(const tw_qk_norm_rope_args &a, bool backward)
     return TW_OK;
 }
 
+template <bool BACKWARD, int V, bool NEXT, bool NORM, bool STREAMED>
+static constexpr auto rope_kernel()
+{
+    if constexpr (BACKWARD) return qk_norm_rope_backward_kernel<V, NEXT, NORM, STREAMED>;
+    else return qk_norm_rope_kernel<V, NEXT, NORM, STREAMED>;
+}
+
+template <bool BACKWARD, int V, bool NEXT>
+static tw_status launch_rope_t(const tw_qk_norm_rope_args &a, const RopeLayout &l, const RopeParams &p, hipStream_t stream)
+{
+    static void (*const kernels[])(RopeParams) = {rope_kernel<BACKWARD, V, NEXT, false, false>(), rope_kernel<BACKWARD, V, NEXT, false, true>(),
+                                                  rope_kernel<BACKWARD, V, NEXT, true, false>(), rope_kernel<BACKWARD, V, NEXT, true, true>()};
+    const bool norm = a.q_weight != nullptr;
+    const unsigned lds = BACKWARD && norm ? (256u >> l.lanes_log2) * a.head_dim * 4 : 0;
+    TW_HIP(launch_kernel(kernels[norm * 2 + rope_streamed(a)], dim3(static_cast<uint32_t>(l.grid[0] + l.grid[1])), dim3(256), lds, stream, p));
+    return TW_OK;
+}
+
+template <bool BACKWARD>
+static tw_status launch_rope(const tw_qk_norm_rope_args &a, const RopeLayout &l, const RopeParams &p, hipStream_t stream)
+{
+    if (a.interleaved) return launch_rope_t<BACKWARD, 8, true>(a, l, p, stream);
+    return l.v == 8 ? launch_rope_t<BACKWARD, 8, false>(a, l, p, stream) : launch_rope_t<BACKWARD, 4, false>(a, l, p, stream);
+}
+
 // The workspace shares nothing with the call's tensors.
 static tw_status rope_workspace(const tw_qk_norm_rope_args &a, const void *workspace, uint64_t need)
 {
@@ -542,10 +602,10 @@ static tw_status rope_workspace(const tw_qk_norm_rope_args &a, const void *works
     return TW_OK;
 }
 
-static tw_status launch_join(const tw_qk_norm_rope_args &a, const float *part, int parts, hipStream_t stream)
+static tw_status launch_join(const tw_qk_norm_rope_args &a, const float *part, int q_parts, int k_parts, hipStream_t stream)
 {
-    TW_HIP(launch_kernel(qk_norm_rope_join_kernel, dim3(static_cast<uint32_t>((2 * a.head_dim + 15) / 16)), dim3(256), 0, stream, part, parts,
-                         a.head_dim, a.dq_weight, a.dk_weight));
+    TW_HIP(launch_kernel(qk_norm_rope_join_kernel, dim3(static_cast<uint32_t>((a.head_dim + 15) / 16), 2), dim3(1024), 0, stream, part, q_parts,
+                         k_parts, a.head_dim, a.dq_weight, a.dk_weight));
     return TW_OK;
 }
 
@@ -597,18 +657,16 @@ tw_status tw_qk_norm_rope(const tw_qk_norm_rope_args *args, void *stream)
     TW_TRY(rope_tensors(a, false));
     const RopeLayout l = rope_layout(a, false);
     const RopeParams p = rope_params(a, l);
-    if (l.grid > (1 << 23)) return TW_ERR_UNSUPPORTED;
-    auto *const kernel = a.q_weight ? (l.v == 8 ? qk_norm_rope_kernel<8, true> : qk_norm_rope_kernel<4, true>)
-                                    : (l.v == 8 ? qk_norm_rope_kernel<8, false> : qk_norm_rope_kernel<4, false>);
-    TW_HIP(launch_kernel(kernel, dim3(static_cast<uint32_t>(l.grid)), dim3(256), 0, static_cast<hipStream_t>(stream), p));
-    return TW_OK;
+    if (l.grid[0] + l.grid[1] > (1 << 23)) return TW_ERR_UNSUPPORTED;
+    return launch_rope<false>(a, l, p, static_cast<hipStream_t>(stream));
 }
 
 int64_t tw_qk_norm_rope_backward_workspace_bytes(const tw_qk_norm_rope_args *args)
 {
     if (!args || rope_sizes(*args) != TW_OK) return -1;
     if (args->tokens == 0 || !args->q_weight) return 0;
-    return rope_layout(*args, true).grid * 2 * args->head_dim * 4;
+    const RopeLayout l = rope_layout(*args, true);
+    return (l.grid[0] + l.grid[1]) * args->head_dim * 4;
 }
 
 tw_status tw_qk_norm_rope_backward(const tw_qk_norm_rope_args *args, void *workspace, int64_t workspace_bytes, void *stream)
@@ -623,7 +681,7 @@ tw_status tw_qk_norm_rope_backward(const tw_qk_norm_rope_args *args, void *works
         if (!a.dq_weight || !a.dk_weight) return TW_ERR_NULL;
         if (!aligned_to(a.dq_weight, 4) || !aligned_to(a.dk_weight, 4)) return TW_ERR_ALIGN;
         if (ranges_overlap(a.dq_weight, a.head_dim * 4u, a.dk_weight, a.head_dim * 4u)) return TW_ERR_ALIAS;
-        return launch_join(a, nullptr, 0, s);
+        return launch_join(a, nullptr, 0, 0, s);
     }
     TW_TRY(rope_tensors(a, true));
     const int64_t need = tw_qk_norm_rope_backward_workspace_bytes(args);
@@ -633,16 +691,13 @@ tw_status tw_qk_norm_rope_backward(const tw_qk_norm_rope_args *args, void *works
     TW_TRY(rope_workspace(a, workspace, static_cast<uint64_t>(need)));
     const RopeLayout l = rope_layout(a, true);
     RopeParams p = rope_params(a, l);
-    p.dy[0] = static_cast<const char *>(a.dq);
-    p.dy[1] = static_cast<const char *>(a.dk);
-    p.dy_stride[0] = a.dq_stride * 2;
-    p.dy_stride[1] = a.dk_stride * 2;
+    p.side[0].dy = static_cast<const char *>(a.dq);
+    p.side[1].dy = static_cast<const char *>(a.dk);
+    p.side[0].dy_stride = a.dq_stride * 2;
+    p.side[1].dy_stride = a.dk_stride * 2;
     p.part = static_cast<float *>(workspace);
-    auto *const kernel = norm ? (l.v == 8 ? qk_norm_rope_backward_kernel<8, true> : qk_norm_rope_backward_kernel<4, true>)
-                              : (l.v == 8 ? qk_norm_rope_backward_kernel<8, false> : qk_norm_rope_backward_kernel<4, false>);
-    const unsigned lds = norm ? (256u >> l.lanes_log2) * 2 * a.head_dim * 4 : 0;
-    TW_HIP(launch_kernel(kernel, dim3(static_cast<uint32_t>(l.grid)), dim3(256), lds, s, p));
-    return norm ? launch_join(a, p.part, static_cast<int>(l.grid), s) : TW_OK;
+    TW_TRY(launch_rope<true>(a, l, p, s));
+    return norm ? launch_join(a, p.part, static_cast<int>(l.grid[0]), static_cast<int>(l.grid[1]), s) : TW_OK;
 }
 
 }  // extern "C"
