@@ -63,6 +63,7 @@
 #include <algorithm>
 #include <atomic>
 
+#include "tw_group.h"
 #include "tw_help.h"
 #include "tw_internal.h"
 #include "tw_mfma.h"
@@ -222,10 +223,12 @@ struct Rolling {
 // tiles_per_xcd: ceil(tiles / 8); phase_cycles: tracing variant only, kGemmPhases counters
 // per wave. (The step of the walk over tiles is gridDim.x: the same number as an argument
 // made every launch of this kernel 0.4 us slower.)
-template <bool B_KN, int WM, int WN, int STAGES, int BK, bool TRACE, bool HELPED>
+// GROUP: none, or a GroupedB, and the rows of A and C come in groups with a weight each; tiles_m, last_rows and tiles_per_xcd then
+// follow from the groups' offsets, on the device.
+template <bool B_KN, int WM, int WN, int STAGES, int BK, bool TRACE, bool HELPED, typename... GROUP>
 __global__ __launch_bounds__(64 * (2 * BM / (kBlk * WM))) void gemm_bf16_kernel(
     const char *A, const char *B, char *C, int N, int K, int tiles_m, int tiles_n, int last_rows, int group_m,
-    int tiles_per_xcd, uint32_t help, unsigned long long *phase_cycles)
+    int tiles_per_xcd, uint32_t help, unsigned long long *phase_cycles, GROUP... group)
 {
     // The body is for the device pass only: the host pass needs the launch stub,
     // and silently drops it when it cannot make sense of the target-specific
@@ -280,7 +283,13 @@ __global__ __launch_bounds__(64 * (2 * BM / (kBlk * WM))) void gemm_bf16_kernel(
     constexpr uint32_t kPastK = 0x80000000u;
     // (at least one: with K = 0 it loads nothing but zeros)
     const int k_tiles = K > 0 ? (K + BK - 1) / BK : 1;
-    const int total_tiles = tiles_m * tiles_n;
+    constexpr bool GROUPED = sizeof...(GROUP) > 0;
+    const GroupedB grouped = group_argument(group...);
+    int total_tiles = tiles_m * tiles_n;
+    if constexpr (GROUPED) {
+        total_tiles = count_group_tiles(grouped.groups, BM, tiles_n);
+        tiles_per_xcd = (total_tiles + kXcds - 1) / kXcds;
+    }
 
     // global -> LDS duty: wave instruction i of this wave fills slots
     // [(i * NW + wave) * 64, +64); this lane's slot inside a line and the row and
@@ -337,17 +346,29 @@ __global__ __launch_bounds__(64 * (2 * BM / (kBlk * WM))) void gemm_bf16_kernel(
         const int slot_w = w / kXcds;
         const int lin = (w % kXcds) * tiles_per_xcd + slot_w;
         if (lin >= total_tiles) continue;
-        const TileAt at = tile_at(lin, tiles_m, tiles_n, group_m);
-        const int tm = at.m, tn = at.n;
+        TileAt at;
+        long long m0;
+        int rows_a;
+        const char *B_of = B;  // the weight of the tile's rows
+        if constexpr (GROUPED) {
+            const GroupTile g = find_group_tile(grouped.groups, BM, tiles_n, lin);
+            at = tile_at(g.tile, static_cast<int>((static_cast<uint32_t>(g.rows) + BM - 1) / BM), tiles_n, group_m);
+            m0 = g.begin + static_cast<long long>(at.m) * BM;
+            rows_a = min(BM, g.rows - at.m * BM);
+            B_of += g.group * grouped.b_bytes;
+        } else {
+            at = tile_at(lin, tiles_m, tiles_n, group_m);
+            m0 = static_cast<long long>(at.m) * BM;
+            rows_a = at.m == tiles_m - 1 ? last_rows : BM;
+        }
+        const int tn = at.n;
 
         unsigned long long t_tile = 0;
         if constexpr (TRACE) t_tile = now();
-        const long long m0 = static_cast<long long>(tm) * BM;
         const int n0 = tn * BN;
-        const int rows_a = at.m == tiles_m - 1 ? last_rows : BM;
         const int rows_b = min(BN, N - n0);
         const __amdgpu_buffer_rsrc_t ra = make_rsrc(A + m0 * row_bytes, static_cast<uint32_t>(rows_a * row_bytes));
-        const __amdgpu_buffer_rsrc_t rb = make_rsrc(B + n0 * row_bytes, static_cast<uint32_t>(rows_b * row_bytes));
+        const __amdgpu_buffer_rsrc_t rb = make_rsrc(B_of + n0 * row_bytes, static_cast<uint32_t>(rows_b * row_bytes));
 
         f32x4 acc[WN][WM];
 #pragma unroll
@@ -426,7 +447,7 @@ __global__ __launch_bounds__(64 * (2 * BM / (kBlk * WM))) void gemm_bf16_kernel(
                 // rows k0 .. k0+63 of B through a descriptor of their own: rows past K
                 // fall outside it, columns past N are redirected out of range
                 const int i = idx - A_LOADS;
-                const __amdgpu_buffer_rsrc_t rbk = make_rsrc(B + c.bk_off, c.bk_len);
+                const __amdgpu_buffer_rsrc_t rbk = make_rsrc(B_of + c.bk_off, c.bk_len);
                 if constexpr (kRoll) {
                     __builtin_amdgcn_raw_ptr_buffer_load_lds(rbk, (lds_ptr_t)(c.sb + (i * NW + wave) * 1024), 16,
                                                              kn_voff[i & 1], kn_instr_bytes * i, 0, 0);
@@ -904,6 +925,32 @@ static tw_status launch_cfg(const tw_gemm_args &g, int budget, hipStream_t strea
                          tile_group_m(tiles_m, tiles_per_xcd, BM, BN, budget), tiles_per_xcd,
                          HELPED ? help.packed | next_help_word() : 0u, phase_cycles));
     return TW_OK;
+}
+
+// Products by group on the tiles of this file, a workgroup to a compute unit. `tiles`: as many as there may be.
+template <bool B_KN, int WM, int WN, int STAGES>
+static tw_status launch_group_cfg(const GroupGemm &g, int64_t tiles, int cus, hipStream_t stream)
+{
+    using Cfg = TileCfg<WM, WN, STAGES, 64>;
+    const int64_t tiles_n = (g.N + Cfg::kBN - 1) / Cfg::kBN, slots = (tiles + kXcds - 1) / kXcds * kXcds;
+    auto kern = gemm_bf16_kernel<B_KN, WM, WN, STAGES, 64, false, false, GroupedB>;
+    static std::atomic<int> allowed[kMaxDevices];
+    TW_TRY(allow_dynamic_lds(reinterpret_cast<const void *>(kern), Cfg::kLdsBytes, allowed));
+    const GroupedB group = {{g.offsets, g.groups, static_cast<int>(g.rows)}, g.N * g.K * 2};
+    // (the block of tiles as for the rows of an average group)
+    const int64_t tiles_m = std::max<int64_t>(1, (g.rows / g.groups + BM / 2) / BM);
+    TW_HIP(launch_kernel(kern, dim3(static_cast<uint32_t>(std::min<int64_t>(slots, cus))), dim3(Cfg::kThreads), Cfg::kLdsBytes, stream,
+                         static_cast<const char *>(g.A), static_cast<const char *>(g.B), static_cast<char *>(g.C),
+                         static_cast<int>(g.N), static_cast<int>(g.K), 0, static_cast<int>(tiles_n), 0,
+                         tile_group_m(tiles_m, std::max<int64_t>(1, tiles / kXcds), BM, Cfg::kBN, cus), 0, 0u,
+                         static_cast<unsigned long long *>(nullptr), group));
+    return TW_OK;
+}
+
+tw_status launch_group_gemm(const GroupGemm &g, int cols, int64_t tiles, int cus, hipStream_t stream)
+{
+    if (g.kn) return cols == 256 ? launch_group_cfg<true, 8, 8, 5>(g, tiles, cus, stream) : launch_group_cfg<true, 4, 4, 3>(g, tiles, cus, stream);
+    return cols == 256 ? launch_group_cfg<false, 8, 8, 2>(g, tiles, cus, stream) : launch_group_cfg<false, 4, 4, 3>(g, tiles, cus, stream);
 }
 
 // Share of the launch's compute-unit slots that hold a tile when `tiles` tiles

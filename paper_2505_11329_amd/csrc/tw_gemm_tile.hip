@@ -37,6 +37,7 @@
 #include <algorithm>
 #include <atomic>
 
+#include "tw_group.h"
 #include "tw_help.h"
 #include "tw_internal.h"
 #include "tw_mfma.h"
@@ -119,10 +120,11 @@ struct StageFrags {
 // no division that tile_at can spare, the fragment addresses later. (16 rows, K = 1024, N =
 // 8192: 5.6 -> 5.1 us; K = 8192, N = 3584: 13.7 -> 13.2; 512 x 4096 x 2048: 15.0 -> 14.7.)
 // last_rows: rows of A in the last row of tiles.
-template <bool B_KN, int WM, int WN, int WVM, int WVN, int BK, int S, bool LOADERS, bool STREAM_B, bool ROLLS>
+// GROUP: as in tw_gemm.hip.
+template <bool B_KN, int WM, int WN, int WVM, int WVN, int BK, int S, bool LOADERS, bool STREAM_B, bool ROLLS, typename... GROUP>
 __global__ __launch_bounds__((SmallTile<WM, WN, WVM, WVN, BK, S, LOADERS>::kThreads)) void gemm_tile_kernel(
     const char *A, const char *B, char *C, int N, int K, int tiles_m, int tiles_n, int last_rows, int group_m,
-    int tiles_per_xcd, uint32_t help)
+    int tiles_per_xcd, uint32_t help, GROUP... group)
 {
 #if defined(__HIP_DEVICE_COMPILE__)  // as in tw_gemm.hip: the host pass needs the launch stub only
     using T = SmallTile<WM, WN, WVM, WVN, BK, S, LOADERS>;
@@ -134,7 +136,8 @@ __global__ __launch_bounds__((SmallTile<WM, WN, WVM, WVN, BK, S, LOADERS>::kThre
     constexpr int kBPolicy = STREAM_B ? kStreamPolicy : 0;
     extern __shared__ __attribute__((aligned(16))) char lds[];
     // (with loading waves only: shapes without helpers came out up to 2 % slower with the branch)
-    if (LOADERS && static_cast<int>(blockIdx.x) >= tiles_per_xcd * kXcds)
+    constexpr bool GROUPED = sizeof...(GROUP) > 0;
+    if (!GROUPED && LOADERS && static_cast<int>(blockIdx.x) >= tiles_per_xcd * kXcds)
         return help_tiles<B_KN, false, T::kThreads / 64>(A, B, (tiles_m - 1) * BM + last_rows, N, K, tiles_m, tiles_n, group_m,
                                                          tiles_per_xcd, BM, BN, help);
     const int tid = threadIdx.x, lane = tid & 63;
@@ -162,16 +165,34 @@ __global__ __launch_bounds__((SmallTile<WM, WN, WVM, WVN, BK, S, LOADERS>::kThre
     const int kn_row = loader * kKnInstrRows + lane / kKnPieces;  // + i * NW * kKnInstrRows
     const int kn_piece = (lane % kKnPieces) ^ (kn_swizzle<BN>(kn_row) << 1);
 
+    const GroupedB grouped = group_argument(group...);
+    int total_tiles = tiles_m * tiles_n;
+    if constexpr (GROUPED) {
+        total_tiles = count_group_tiles(grouped.groups, BM, tiles_n);
+        tiles_per_xcd = (total_tiles + kXcds - 1) / kXcds;
+    }
     for (int w = blockIdx.x; w < tiles_per_xcd * kXcds; w += gridDim.x) {
         const int lin = (w % kXcds) * tiles_per_xcd + w / kXcds;
-        if (lin >= tiles_m * tiles_n) continue;
-        const TileAt at = tile_at(lin, tiles_m, tiles_n, group_m);
-        const long long m0 = static_cast<long long>(at.m) * BM;
+        if (lin >= total_tiles) continue;
+        TileAt at;
+        long long m0;
+        int rows_a;
+        const char *B_of = B;  // the weight of the tile's rows
+        if constexpr (GROUPED) {
+            const GroupTile g = find_group_tile(grouped.groups, BM, tiles_n, lin);
+            at = tile_at(g.tile, static_cast<int>((static_cast<uint32_t>(g.rows) + BM - 1) / BM), tiles_n, group_m);
+            m0 = g.begin + static_cast<long long>(at.m) * BM;
+            rows_a = min(BM, g.rows - at.m * BM);
+            B_of += g.group * grouped.b_bytes;
+        } else {
+            at = tile_at(lin, tiles_m, tiles_n, group_m);
+            m0 = static_cast<long long>(at.m) * BM;
+            rows_a = at.m == tiles_m - 1 ? last_rows : BM;
+        }
         const int n0 = at.n * BN;
-        const int rows_a = at.m == tiles_m - 1 ? last_rows : BM;
         const int rows_b = min(BN, N - n0);
         const __amdgpu_buffer_rsrc_t ra = make_rsrc(A + m0 * row_bytes, static_cast<uint32_t>(rows_a * row_bytes));
-        const __amdgpu_buffer_rsrc_t rb = make_rsrc(B + n0 * row_bytes, static_cast<uint32_t>(rows_b * row_bytes));
+        const __amdgpu_buffer_rsrc_t rb = make_rsrc(B_of + n0 * row_bytes, static_cast<uint32_t>(rows_b * row_bytes));
         const uint32_t load_row_off = static_cast<uint32_t>(load_row * row_bytes);
         const uint32_t step_bytes = static_cast<uint32_t>(kStepRows * row_bytes);
         const uint32_t kn_off = n0 + kn_piece * 8 < N
@@ -179,6 +200,7 @@ __global__ __launch_bounds__((SmallTile<WM, WN, WVM, WVN, BK, S, LOADERS>::kThre
                                     : kPastK;
         const uint32_t kn_step_bytes = static_cast<uint32_t>(NW * kKnInstrRows * bkn_row_bytes);
 
+        const int k_first = GROUPED ? (at.n * last_rows) % k_tiles : 0;
         f32x4 acc[WM][WN];
 #pragma unroll
         for (int i = 0; i < WM; ++i)
@@ -193,6 +215,10 @@ __global__ __launch_bounds__((SmallTile<WM, WN, WVM, WVN, BK, S, LOADERS>::kThre
         };
         auto fetch_ctx = [&](int kt, int slot) {
             Fetch c;
+            if constexpr (GROUPED) {
+                const int from = kt + k_first;
+                kt = kt >= k_tiles ? k_tiles : from >= k_tiles ? from - k_tiles : from;
+            }
             c.base = (lds_char_ptr_t)(lds + slot * T::kStageBytes + loader * 1024);
 #pragma unroll
             for (int q = 0; q < kRepeat; ++q) {
@@ -203,7 +229,7 @@ __global__ __launch_bounds__((SmallTile<WM, WN, WVM, WVN, BK, S, LOADERS>::kThre
                 // rows k0 ... of B through a descriptor of their own: rows past K lie outside it
                 const long long k0 = static_cast<long long>(kt) * BK, left = K - k0;
                 const int rows_k = static_cast<int>(left < 0 ? 0 : left > BK ? BK : left);
-                c.rbk = make_rsrc(B + (left > 0 ? k0 : 0) * bkn_row_bytes, static_cast<uint32_t>(rows_k * bkn_row_bytes));
+                c.rbk = make_rsrc(B_of + (left > 0 ? k0 : 0) * bkn_row_bytes, static_cast<uint32_t>(rows_k * bkn_row_bytes));
             } else {
                 c.rbk = rb;
             }
@@ -802,6 +828,44 @@ int small_tile_loading_waves(const tw_gemm_args &g, int shape, const HelpPlan &h
     int waves = 0;
     (g.b_layout == TW_B_KN ? t.kn : t.nk)(g, {0, 0, place, help, &waves}, nullptr);
     return waves;
+}
+
+// Products by group, a workgroup to a tile. Each tile begins at another step of K (`last_rows`, which groups have no use for, says how
+// many further than its neighbour): begun together they ask for the same columns of all their rows at one time, which lie in a few of
+// the memory's channels where rows are 4 or 8 KB apart. 96 rows of 8 experts, [4096 x 3584] each, 64 x 128 tiles: 46.5 to 36.7 us.
+template <bool B_KN, int WM, int WN, int WVM, int WVN, int BK, int S, bool STREAM>
+static tw_status launch_group_tile_t(const GroupGemm &g, int64_t tiles, hipStream_t stream)
+{
+    using T = SmallTile<WM, WN, WVM, WVN, BK, S, false>;
+    const int64_t tiles_n = (g.N + T::BN - 1) / T::BN, slots = (tiles + kXcds - 1) / kXcds * kXcds;
+    auto kern = gemm_tile_kernel<B_KN, WM, WN, WVM, WVN, BK, S, false, STREAM, false, GroupedB>;
+    static std::atomic<int> allowed[kMaxDevices];
+    TW_TRY(allow_dynamic_lds(reinterpret_cast<const void *>(kern), T::kLdsBytes, allowed));
+    const GroupedB group = {{g.offsets, g.groups, static_cast<int>(g.rows)}, g.N * g.K * 2};
+    TW_HIP(launch_kernel(kern, dim3(static_cast<uint32_t>(slots)), dim3(T::kThreads), T::kLdsBytes, stream,
+                         static_cast<const char *>(g.A), static_cast<const char *>(g.B), static_cast<char *>(g.C),
+                         static_cast<int>(g.N), static_cast<int>(g.K), 0, static_cast<int>(tiles_n), 1,
+                         4, 0, 0u, group));  // (blocks of four rows of tiles: those that read one weight next to each other)
+    return TW_OK;
+}
+
+// STREAM: weights go past the caches.
+tw_status launch_group_tile(const GroupGemm &g, int rows, int64_t tiles, hipStream_t stream)
+{
+    switch (rows) {
+    case 32:
+        return g.kn ? launch_group_tile_t<true, 1, 1, 2, 2, 128, 4, false>(g, tiles, stream)
+                    : launch_group_tile_t<false, 1, 1, 2, 2, 128, 4, false>(g, tiles, stream);
+    case 64:
+        return g.kn ? launch_group_tile_t<true, 2, 2, 2, 2, 128, 4, false>(g, tiles, stream)
+                    : launch_group_tile_t<false, 2, 4, 2, 2, 64, 3, true>(g, tiles, stream);
+    case 128:
+        return g.kn ? launch_group_tile_t<true, 2, 4, 4, 2, 64, 4, false>(g, tiles, stream)
+                    : launch_group_tile_t<false, 2, 4, 4, 2, 64, 4, true>(g, tiles, stream);
+    default:
+        return g.kn ? launch_group_tile_t<true, 3, 4, 4, 2, 64, 3, false>(g, tiles, stream)
+                    : launch_group_tile_t<false, 3, 4, 4, 2, 64, 3, false>(g, tiles, stream);
+    }
 }
 
 }  // namespace tw

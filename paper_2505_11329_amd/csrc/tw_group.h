@@ -2,6 +2,8 @@
 // wave finds its tile by itself.
 #pragma once
 
+#include <stdint.h>
+
 #include "tw_device.h"
 
 namespace tw {
@@ -42,13 +44,13 @@ struct GroupTile {
     int begin, rows;  // the group's
     int total;        // tiles of all groups up to this one's, of all where there is no such tile
 };
-__device__ __forceinline__ GroupTile find_group_tile(const Groups &g, int tile_rows_log2, int tiles_n, int index)
+__device__ __forceinline__ GroupTile find_group_tile(const Groups &g, uint32_t tile_rows, int tiles_n, int index)
 {
     const int lane = threadIdx.x & 63;
     int carry = first_group_row(g), before = 0;
     for (int first = 0; first < g.n_groups; first += 64) {
         const GroupRows r = group_rows(g, first, lane, &carry);
-        const int tiles = static_cast<int>((static_cast<uint32_t>(r.end - r.begin) + (1u << tile_rows_log2) - 1) >> tile_rows_log2) * tiles_n;
+        const int tiles = static_cast<int>((static_cast<uint32_t>(r.end - r.begin) + tile_rows - 1) / tile_rows) * tiles_n;
         const int upto = before + sum_upto(tiles);
         const uint64_t past = __ballot(upto > index);
         if (past) {
@@ -60,6 +62,20 @@ __device__ __forceinline__ GroupTile find_group_tile(const Groups &g, int tile_r
         before = __builtin_amdgcn_readlane(upto, 63);
     }
     return {-1, 0, 0, 0, before};
+}
+
+// What a kernel of single products takes besides for products by group: B has a weight for each, `b_bytes` apart.
+struct GroupedB {
+    Groups groups;
+    int64_t b_bytes;
+};
+__device__ __forceinline__ GroupedB group_argument() { return {}; }
+__device__ __forceinline__ GroupedB group_argument(const GroupedB &g) { return g; }
+
+// All groups' tiles.
+__device__ __forceinline__ int count_group_tiles(const Groups &g, uint32_t tile_rows, int tiles_n)
+{
+    return find_group_tile(g, tile_rows, tiles_n, INT32_MAX).total;
 }
 
 }  // namespace tw

@@ -119,6 +119,23 @@ tw_status launch_small_tile(const tw_gemm_args &g, int shape, const HelpPlan &he
                             hipStream_t stream);
 int small_tile_loading_waves(const tw_gemm_args &g, int shape, const HelpPlan &help, GemmPlace place);
 
+// ---- products by group: rows that come in groups with a weight each (tw_expert_gemm.hip) ----
+struct GroupGemm {
+    const void *A, *B;
+    void *C;
+    const int32_t *offsets;  // device: the groups' first rows
+    int64_t rows, N, K;      // rows of A and C, groups or not
+    int groups;
+    bool kn;
+};
+// `tiles` is as many as there may be. On tiles of 256 x `cols` (tw_gemm.hip: 128 or 256);
+tw_status launch_group_gemm(const GroupGemm &g, int cols, int64_t tiles, int cus, hipStream_t stream);
+// on those of `rows` rows, 32, 64, 128 or 192 (tw_gemm_tile.hip).
+tw_status launch_group_tile(const GroupGemm &g, int rows, int64_t tiles, hipStream_t stream);
+// out[e](m, n) = sum over the rows r of group e of x[r, m] y[r, n] (tw_expert_gradient.hip).
+tw_status launch_expert_gradient(const void *x, const void *y, void *out, const int32_t *offsets, int64_t rows, int64_t M, int64_t N,
+                                 int n_experts, hipStream_t stream);
+
 // ---- fork/join events (tw_host.hip) ----
 // A small per-device pool of timing-disabled events used to order streams.
 tw_status borrow_event(hipEvent_t *ev);
