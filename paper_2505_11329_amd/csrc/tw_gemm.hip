@@ -927,7 +927,8 @@ static tw_status launch_cfg(const tw_gemm_args &g, int budget, hipStream_t strea
     return TW_OK;
 }
 
-// Products by group on the tiles of this file, a workgroup to a compute unit. `tiles`: as many as there may be.
+// Products by group on tiles of 256 x 256, a workgroup to a compute unit. `tiles`: as many as there may be. 65536 rows of 64 experts,
+// [4096 x 2048] each: 944 us, 1.16 PFLOP/s, an eighth of it on rows that are not there.
 template <bool B_KN, int WM, int WN, int STAGES>
 static tw_status launch_group_cfg(const GroupGemm &g, int64_t tiles, int cus, hipStream_t stream)
 {
@@ -947,10 +948,9 @@ static tw_status launch_group_cfg(const GroupGemm &g, int64_t tiles, int cus, hi
     return TW_OK;
 }
 
-tw_status launch_group_gemm(const GroupGemm &g, int cols, int64_t tiles, int cus, hipStream_t stream)
+tw_status launch_group_gemm(const GroupGemm &g, int64_t tiles, int cus, hipStream_t stream)
 {
-    if (g.kn) return cols == 256 ? launch_group_cfg<true, 8, 8, 5>(g, tiles, cus, stream) : launch_group_cfg<true, 4, 4, 3>(g, tiles, cus, stream);
-    return cols == 256 ? launch_group_cfg<false, 8, 8, 2>(g, tiles, cus, stream) : launch_group_cfg<false, 4, 4, 3>(g, tiles, cus, stream);
+    return g.kn ? launch_group_cfg<true, 8, 8, 5>(g, tiles, cus, stream) : launch_group_cfg<false, 8, 8, 2>(g, tiles, cus, stream);
 }
 
 // Share of the launch's compute-unit slots that hold a tile when `tiles` tiles

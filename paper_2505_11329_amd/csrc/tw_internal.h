@@ -128,9 +128,9 @@ struct GroupGemm {
     int groups;
     bool kn;
 };
-// `tiles` is as many as there may be. On tiles of 256 x `cols` (tw_gemm.hip: 128 or 256);
-tw_status launch_group_gemm(const GroupGemm &g, int cols, int64_t tiles, int cus, hipStream_t stream);
-// on those of `rows` rows, 32, 64, 128 or 192 (tw_gemm_tile.hip).
+// `tiles` is as many as there may be. On tiles of 256 x 256 (tw_gemm.hip);
+tw_status launch_group_gemm(const GroupGemm &g, int64_t tiles, int cus, hipStream_t stream);
+// on those of 32 x 32 or of `rows` = 64, 128 or 192 by 128 (tw_gemm_tile.hip).
 tw_status launch_group_tile(const GroupGemm &g, int rows, int64_t tiles, hipStream_t stream);
 // out[e](m, n) = sum over the rows r of group e of x[r, m] y[r, n] (tw_expert_gradient.hip).
 tw_status launch_expert_gradient(const void *x, const void *y, void *out, const int32_t *offsets, int64_t rows, int64_t M, int64_t N,
