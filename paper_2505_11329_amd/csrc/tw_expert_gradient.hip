@@ -18,8 +18,8 @@ namespace tw {
 // read, and the loads of the 64 after the next take their slots.
 static constexpr int kEdge = 256, kStep = 64, kRowBytes = kEdge * 2, kSlotBytes = kStep * kRowBytes, kWaves = 4;
 static constexpr int kBlocks = 8;      // of 16 rows, or columns, to a wave
-static constexpr int kYSlots = 2 * kSlotBytes, kLdsBytes = 5 * kSlotBytes;
-static constexpr uint32_t kPast = 0x80000000u;  // out of range with any scalar offset on top
+[[maybe_unused]] static constexpr int kYSlots = 2 * kSlotBytes, kLdsBytes = 5 * kSlotBytes;
+[[maybe_unused]] static constexpr uint32_t kPast = 0x80000000u;  // out of range with any scalar offset on top
 
 struct GradientParams {
     const char *x, *y;
@@ -251,6 +251,130 @@ __global__ __launch_bounds__(64 * kWaves) void expert_gradient_kernel(GradientPa
 #endif
 }
 
+// Few rows to an expert, or few tiles: the results are most of what moves, and a large tile's start and end most of its time. Tiles of 128 x 128,
+// four waves of 64 x 64, four workgroups to a compute unit, so that one's loads run beside the others' products and stores; 32 rows at a
+// time, two slots, and the results through the LDS by whole rows. 1172 rows of 16 experts, [2048 x 1024] each: 26.0 to 16.7 us; 400 of 8,
+// [4096 x 3584]: 82 to 55 (three workgroups 61, with three slots as well).
+static constexpr int kThinEdge = 128, kThinStep = 32, kThinRowBytes = kThinEdge * 2, kThinSlot = 2 * kThinStep * kThinRowBytes;
+static constexpr int kThinPitch = kThinRowBytes + 32, kThinLds = kThinEdge * kThinPitch, kThinAtOnce = 4;
+static_assert(2 * kThinSlot <= kThinLds, "the slots lie in the results' room");
+
+__global__ __launch_bounds__(64 * kWaves, kThinAtOnce) void expert_gradient_thin_kernel(GradientParams p)
+{
+#if defined(__HIP_DEVICE_COMPILE__)
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int wave_m = wave >> 1, wave_n = wave & 1, l15 = lane & 15, lgrp = lane >> 4;
+    const int x_pitch = p.M * 2, y_pitch = p.N * 2;
+    // Instruction i of this wave fills rows load_row + 16 i. Row r keeps piece c at c ^ ((r & 3) << 1) ^ (r & 8).
+    const int load_row = wave * 4 + lane / 16, load_piece = (lane % 16) ^ ((load_row & 3) << 1) ^ (load_row & 8);
+    const int j = l15 >> 2, frag_row = lgrp * 8 + j;
+    auto frag_at = [&](int first_col) {
+        const int col = first_col + 4 * (l15 & 3);
+        return static_cast<uint32_t>(frag_row * kThinRowBytes + (((col >> 3) ^ (j << 1) ^ ((lgrp & 1) << 3)) << 4) + (col & 7) * 2);
+    };
+    const uint32_t x_at = frag_at(wave_m * 64), y_at = kThinStep * kThinRowBytes + frag_at(wave_n * 64);
+
+    for (int w = blockIdx.x; w < p.slots; w += gridDim.x) {
+        const int turn = w / kXcds / p.run, lin = (turn * kXcds + w % kXcds) * p.run + w / kXcds - turn * p.run;
+        if (lin >= p.tiles) continue;
+        const int of_expert = p.tiles_m * p.tiles_n, e = lin / of_expert;
+        const TileAt at = tile_at(lin - e * of_expert, p.tiles_m, p.tiles_n, p.group_m);
+        int carry = first_group_row(p.groups);
+        GroupRows rows = {};
+        for (int first = 0; first <= e; first += 64) rows = group_rows(p.groups, first, lane, &carry);
+        const int begin = __builtin_amdgcn_readlane(rows.begin, e & 63), depth = __builtin_amdgcn_readlane(rows.end, e & 63) - begin;
+        const int m0 = at.m * kThinEdge, n0 = at.n * kThinEdge;
+        const int steps = static_cast<int>((static_cast<uint32_t>(depth) + kThinStep - 1) / kThinStep);
+        const char *const x = p.x + static_cast<int64_t>(begin) * x_pitch, *const y = p.y + static_cast<int64_t>(begin) * y_pitch;
+        const int c = load_piece * 8;
+        const uint32_t x_off = m0 + c < p.M ? static_cast<uint32_t>(load_row * x_pitch + (m0 + c) * 2) : kPast;
+        const uint32_t y_off = n0 + c < p.N ? static_cast<uint32_t>(load_row * y_pitch + (n0 + c) * 2) : kPast;
+        auto fetch = [&](int step, int slot) {
+            const uint32_t row = static_cast<uint32_t>(step) * kThinStep, n = min(static_cast<uint32_t>(depth) - row, static_cast<uint32_t>(kThinStep));
+            const __amdgpu_buffer_rsrc_t rx = make_rsrc(x + static_cast<int64_t>(row) * x_pitch, n * static_cast<uint32_t>(x_pitch));
+            const __amdgpu_buffer_rsrc_t ry = make_rsrc(y + static_cast<int64_t>(row) * y_pitch, n * static_cast<uint32_t>(y_pitch));
+            const lds_char_ptr_t to = (lds_char_ptr_t)(lds + slot * kThinSlot + wave * 1024);
+            static_for<2>([&](auto i_tag) {
+                constexpr int i = decltype(i_tag)::value;
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(rx, (lds_ptr_t)(to + i * kWaves * 1024), 16, x_off, 16 * i * x_pitch, 0, 0);
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(ry, (lds_ptr_t)(to + (i + 2) * kWaves * 1024), 16, y_off, 16 * i * y_pitch, 0, 0);
+            });
+        };
+
+        f32x4 acc[4][4];
+#pragma unroll
+        for (int n = 0; n < 4; ++n)
+#pragma unroll
+            for (int m = 0; m < 4; ++m) acc[n][m] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        // all waves are done with the previous tile's results in the LDS
+        __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0)
+        __builtin_amdgcn_s_barrier();
+        if (steps > 0) fetch(0, 0);
+        for (int s = 0; s < steps; ++s) {
+            if (s + 1 < steps) {
+                fetch(s + 1, (s + 1) & 1);
+                __builtin_amdgcn_s_waitcnt(0x0F74);  // vmcnt(4): this step's
+            } else {
+                __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0)
+            }
+            __builtin_amdgcn_s_barrier();
+            const uint32_t slot = static_cast<uint32_t>((s & 1) * kThinSlot);
+            u32x2 xlo[4], xhi[4], ylo[4], yhi[4];
+            static_for<4>([&](auto b_tag) {
+                constexpr int b = decltype(b_tag)::value;
+                const uint32_t ax = (slot + x_at) ^ (b << 5), ay = (slot + y_at) ^ (b << 5);
+                xlo[b] = lds_read_tr8<0>(ax);
+                xhi[b] = lds_read_tr8<4 * kThinRowBytes>(ax);
+                ylo[b] = lds_read_tr8<0>(ay);
+                yhi[b] = lds_read_tr8<4 * kThinRowBytes>(ay);
+            });
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+#pragma unroll
+            for (int b = 0; b < 4; ++b) asm volatile("" : "+v"(xlo[b]), "+v"(xhi[b]), "+v"(ylo[b]), "+v"(yhi[b]));
+            __builtin_amdgcn_s_barrier();  // every wave has this slot's fragments
+#pragma unroll
+            for (int n = 0; n < 4; ++n)
+#pragma unroll
+                for (int m = 0; m < 4; ++m)
+                    acc[n][m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(GradientFrags::join(ylo[n], yhi[n]), GradientFrags::join(xlo[m], xhi[m]),
+                                                                        acc[n][m], 0, 0, 0);
+        }
+
+        // (every wave has its last fragments: the barrier above, or nothing was loaded)
+        const uint32_t put = static_cast<uint32_t>((wave_m * 64 + l15) * kThinPitch + wave_n * 128 + lgrp * 8);
+#pragma unroll
+        for (int m = 0; m < 4; ++m)
+#pragma unroll
+            for (int n = 0; n < 4; ++n) {
+                const u32x2 v = {pack_bf16x2(acc[n][m][0], acc[n][m][1]), pack_bf16x2(acc[n][m][2], acc[n][m][3])};
+                *reinterpret_cast<__attribute__((address_space(3))) u32x2 *>(static_cast<uintptr_t>(put + m * 16 * kThinPitch + n * 32)) = v;
+            }
+        __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0)
+        __builtin_amdgcn_s_barrier();
+        char *const out = p.out + (static_cast<int64_t>(e) * p.M + m0) * y_pitch;
+        const __amdgpu_buffer_rsrc_t to = make_rsrc(out, static_cast<uint32_t>(min(kThinEdge, p.M - m0) * y_pitch));
+        const int row = wave * 32 + lane / 16, col = n0 + (lane % 16) * 8;
+        const uint32_t to_off = col < p.N ? static_cast<uint32_t>(row * y_pitch + col * 2) : kPast;
+        const uint32_t get = static_cast<uint32_t>(row * kThinPitch + (lane % 16) * 16);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const u32x4 v = *reinterpret_cast<__attribute__((address_space(3))) u32x4 *>(static_cast<uintptr_t>(get + i * 4 * kThinPitch));
+            __builtin_amdgcn_raw_buffer_store_b128(v, to, to_off + static_cast<uint32_t>(4 * i * y_pitch), 0, kStorePolicy);  // (no scalar offset: see st())
+        }
+    }
+#endif
+}
+
+// us, tiles of 256 x 256 and of 128 x 128. By the rows of an expert: 8 experts' [4096 x 3584], 300 rows each 127 and 116, 500 rows 163 and 160; [4096 x
+// 2048], 1000 rows 162 and 169; 128 experts' [2048 x 1024], 250 rows 327 and 267, 500 rows 440 and 426; 64 experts' [2816 x 1408], 375 rows 357 and 295.
+// Where half of the compute units would have no large tile: 8 experts' [1024 x 1024], 500 rows 27 and 17, 4000 rows 155 and 119.
+static bool thin_tiles(int64_t rows, int64_t M, int64_t N, int n_experts, int cus)
+{
+    const int64_t large = ((M + kEdge - 1) / kEdge) * ((N + kEdge - 1) / kEdge) * n_experts;
+    return rows < 400 * int64_t(n_experts) || 2 * large <= cus;
+}
+
 tw_status launch_expert_gradient(const void *x, const void *y, void *out, const int32_t *offsets, int64_t rows, int64_t M, int64_t N,
                                  int n_experts, hipStream_t stream)
 {
@@ -263,18 +387,27 @@ tw_status launch_expert_gradient(const void *x, const void *y, void *out, const 
     p.groups = {offsets, n_experts, static_cast<int>(rows)};
     p.M = static_cast<int>(M);
     p.N = static_cast<int>(N);
-    p.tiles_m = static_cast<int>((M + kEdge - 1) / kEdge);
-    p.tiles_n = static_cast<int>((N + kEdge - 1) / kEdge);
+    const bool thin = thin_tiles(rows, M, N, n_experts, cus);
+    const int edge = thin ? kThinEdge : kEdge, at_once = thin ? kThinAtOnce : 1;
+    p.tiles_m = static_cast<int>((M + edge - 1) / edge);
+    p.tiles_n = static_cast<int>((N + edge - 1) / edge);
     const int64_t tiles = int64_t(p.tiles_m) * p.tiles_n * n_experts;
     if (tiles > (1 << 30)) return TW_ERR_UNSUPPORTED;
     p.tiles = static_cast<int>(tiles);
-    p.run = static_cast<int>(std::min<int64_t>((tiles + kXcds - 1) / kXcds, std::max(1, cus / kXcds)));
+    p.run = static_cast<int>(std::min<int64_t>((tiles + kXcds - 1) / kXcds, std::max(1, cus * at_once / kXcds)));
     const int64_t runs = (tiles + p.run - 1) / p.run;
     p.slots = static_cast<int>((runs + kXcds - 1) / kXcds * kXcds * p.run);
-    p.group_m = tile_group_m(p.tiles_m, p.run, kEdge, kEdge, cus);
+    p.group_m = tile_group_m(p.tiles_m, p.run, edge, edge, cus);
+    // Workgroups that take tile after tile where these are few, else one for each: 2048 small tiles 13.4-20.4 us and 15.1-20.4, 7168 42-63 and 43-60, 16384 102-168 and 94-163.
+    const bool stay = !thin || p.slots <= 4 * cus * at_once;
+    const dim3 grid(static_cast<uint32_t>(std::min(p.slots, stay ? cus * at_once : 1 << 20)));
+    if (thin) {
+        TW_HIP(launch_kernel(expert_gradient_thin_kernel, grid, dim3(64 * kWaves), kThinLds, stream, p));
+        return TW_OK;
+    }
     static std::atomic<int> allowed[kMaxDevices];
     TW_TRY(allow_dynamic_lds(reinterpret_cast<const void *>(expert_gradient_kernel), kLdsBytes, allowed));
-    TW_HIP(launch_kernel(expert_gradient_kernel, dim3(static_cast<uint32_t>(std::min(p.slots, cus))), dim3(64 * kWaves), kLdsBytes, stream, p));
+    TW_HIP(launch_kernel(expert_gradient_kernel, grid, dim3(64 * kWaves), kLdsBytes, stream, p));
     return TW_OK;
 }
 
