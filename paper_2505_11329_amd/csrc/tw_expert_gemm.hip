@@ -28,35 +28,42 @@ static tw_status expert_tensors(const void *a, uint64_t a_bytes, const void *b, 
     return TW_OK;
 }
 
-// The tile shapes: their size, how many workgroups of them a compute unit holds, and for weights stored [N x K] and [K x N] what a 64-deep
-// K step of a tile takes with every compute unit busy, what a tile takes besides (us), and how much of a tile an expert has more than its
-// rows fill, of which the host knows only the average. Fitted to 8127 products of 1 to 65536 rows, 8 to 128 experts, N and K of 512 to 8192, with
-// every shape timed: the choice is 3.0 % off the best of them on average, 2.2 % for [K x N]. Without 32 x 32 it would be 19 % and 13 %, without 64 x 128
-// 2.5 and 4.1 %, without 256 x 256 2.7 and 1.8 %, without the other two 0.5 to 1 % each.
+// The tile shapes: their size, and for weights stored [N x K] and [K x N] what a 64-deep K step of an almost empty tile takes with every
+// compute unit busy, how much of that more a full one, what a tile takes besides (us), the share of the time that goes by whole turns where tiles are few, the
+// rate at which the weights come in (TB/s) and what passes until they do (us). Fitted to 3200 products of 1 to 32768 rows, 8 to 160 experts, N and K of 256 to
+// 8192, with every shape timed: the choice is 2.5 % off the best of them on average, 2.7 % for [K x N]. (Without one of the shapes 3 to 7 %; 64 x 128 besides:
+// 0.4 % less.)
 struct GroupShape {
-    int rows, cols, at_once;
+    int rows, cols;
     struct {
-        double step, tile, more;
+        double step, fuller, tile, uneven, rate, start;
     } us[2];
 };
 static const GroupShape kGroupShapes[] = {
-    {32, 32, 2, {{0.166, 2.0, 0.89}, {0.302, 2.7, 1.0}}},   {64, 128, 2, {{0.843, 4.6, 0.32}, {0.716, 2.1, 0.69}}},
-    {128, 128, 1, {{0.554, 4.3, 0.55}, {0.540, 5.9, 0.32}}}, {192, 128, 1, {{0.810, 5.2, 0.38}, {0.794, 3.7, 0.38}}},
-    {256, 256, 1, {{1.372, 7.9, 0.54}, {1.566, 5.5, 0.55}}},
+    {32, 32, {{0.0981, 0.26, 1.76, 0.14, 6.1, 2.2}, {0.16, 0.10, 0.97, 0.32, 5.3, 3.0}}},
+    {16, 64, {{0.137, 0.35, 1.30, 0.19, 7.0, 3.2}, {0.257, 0.00, 0.86, 1.00, 7.0, 3.6}}},
+    {32, 128, {{0.409, 0.02, 0.95, 0.85, 7.0, 4.9}, {0.395, 0.06, 1.36, 0.53, 7.0, 3.2}}},
+    {128, 128, {{0.419, 0.36, 4.67, 0.35, 7.0, 5.4}, {0.466, 0.25, 4.68, 0.24, 7.0, 4.8}}},
+    {192, 128, {{0.545, 0.40, 4.05, 0.38, 5.5, 4.2}, {0.547, 0.29, 4.91, 0.60, 6.0, 4.9}}},
+    {256, 256, {{1.02, 0.26, 9.24, 0.86, 5.2, 8.1}, {1.27, 0.29, 6.07, 0.68, 5.3, 8.2}}},
 };
 
-// The shape of the least estimated time.
+// The shape of the least estimated time. The host knows only how many rows there are: they meet as many experts as choices at random do, and the
+// tiles that an expert has are those of rows spread like waiting times, 1 / (1 - exp(-tile / mean)).
 static const GroupShape &choose_shape(const GroupGemm &g, int cus)
 {
-    const double experts = static_cast<double>(std::min<int64_t>(g.groups, g.rows)), each = static_cast<double>(g.rows) / experts;
+    const double rows = static_cast<double>(g.rows), experts = -std::expm1(-rows / g.groups) * g.groups, each = rows / experts;
+    const double weights = experts * static_cast<double>(g.N) * static_cast<double>(g.K) * 2e-6;  // MB
     const GroupShape *best = nullptr;
     double least = 0.0;
     for (const GroupShape &s : kGroupShapes) {
         const auto &us = s.us[g.kn];
-        const double tiles = experts * std::max(1.0, each / s.rows + us.more) * static_cast<double>((g.N + s.cols - 1) / s.cols);
-        double turns = std::max(1.0, tiles / (double(cus) * s.at_once));
-        if (turns < 4.0) turns = 0.5 * (turns + std::ceil(turns));  // (few turns end in one that is not full)
-        const double time = turns * (static_cast<double>((g.K + 63) / 64) * us.step + us.tile);
+        const double tiles = -experts / std::expm1(-s.rows / each) * static_cast<double>((g.N + s.cols - 1) / s.cols);
+        double turns = tiles / cus;
+        if (turns < 8.0) turns = (1.0 - us.uneven) * std::max(1.0, turns) + us.uneven * std::ceil(turns);
+        const double step = us.step * (1.0 + us.fuller * std::min(1.0, each / s.rows));
+        const double tiles_us = turns * (static_cast<double>((g.K + 63) / 64) * step + us.tile), weights_us = weights / us.rate + us.start;
+        const double time = std::pow(std::pow(tiles_us, 4.0) + std::pow(weights_us, 4.0), 0.25);
         if (!best || time < least) {
             best = &s;
             least = time;
@@ -73,7 +80,7 @@ static tw_status launch_products(const GroupGemm &g, hipStream_t stream)
     // every expert has one tile more than its rows fill, at most
     const int64_t tiles = (g.rows / s.rows + std::min<int64_t>(g.groups, g.rows)) * ((g.N + s.cols - 1) / s.cols);
     if (tiles > (1 << 23)) return TW_ERR_UNSUPPORTED;
-    return s.rows == 256 ? launch_group_gemm(g, tiles, cus, stream) : launch_group_tile(g, s.rows, tiles, stream);
+    return s.rows == 256 ? launch_group_gemm(g, tiles, cus, stream) : launch_group_tile(g, s.rows, s.cols, tiles, stream);
 }
 
 }  // namespace tw
