@@ -31,7 +31,7 @@ static tw_status expert_tensors(const void *a, uint64_t a_bytes, const void *b, 
 // The tile shapes: their size, and for weights stored [N x K] and [K x N] what a 64-deep K step of an almost empty tile takes with every
 // compute unit busy, how much of that more a full one, what a tile takes besides (us), the share of the time that goes by whole turns where tiles are few, the
 // rate at which the weights come in (TB/s) and what passes until they do (us). Fitted to 3200 products of 1 to 32768 rows, 8 to 160 experts, N and K of 256 to
-// 8192, with every shape timed: the choice is 2.5 % off the best of them on average, 2.7 % for [K x N]. (Without one of the shapes 3 to 7 %; 64 x 128 besides:
+// 8192, with every shape timed: the choice is 2.3 % off the best of them on average, 2.6 % for [K x N]. (Without one of the shapes 3 to 7 %; 64 x 128 besides:
 // 0.4 % less.)
 struct GroupShape {
     int rows, cols;
@@ -40,16 +40,16 @@ struct GroupShape {
     } us[2];
 };
 static const GroupShape kGroupShapes[] = {
-    {32, 32, {{0.0981, 0.26, 1.76, 0.14, 6.1, 2.2}, {0.16, 0.10, 0.97, 0.32, 5.3, 3.0}}},
-    {16, 64, {{0.137, 0.35, 1.30, 0.19, 7.0, 3.2}, {0.257, 0.00, 0.86, 1.00, 7.0, 3.6}}},
-    {32, 128, {{0.409, 0.02, 0.95, 0.85, 7.0, 4.9}, {0.395, 0.06, 1.36, 0.53, 7.0, 3.2}}},
-    {128, 128, {{0.419, 0.36, 4.67, 0.35, 7.0, 5.4}, {0.466, 0.25, 4.68, 0.24, 7.0, 4.8}}},
-    {192, 128, {{0.545, 0.40, 4.05, 0.38, 5.5, 4.2}, {0.547, 0.29, 4.91, 0.60, 6.0, 4.9}}},
-    {256, 256, {{1.02, 0.26, 9.24, 0.86, 5.2, 8.1}, {1.27, 0.29, 6.07, 0.68, 5.3, 8.2}}},
+    {32, 32, {{0.122, 0.04, 1.33, 0.13, 7.07, 3.42}, {0.162, 0.05, 1.09, 0.82, 6.73, 3.74}}},
+    {16, 64, {{0.186, 0.00, 1.08, 0.29, 9.00, 4.44}, {0.252, 0.00, 0.94, 1.00, 8.62, 4.39}}},
+    {32, 128, {{0.397, 0.00, 1.16, 0.74, 7.78, 5.29}, {0.451, 0.00, 0.82, 0.67, 9.00, 4.61}}},
+    {128, 128, {{0.392, 0.47, 4.69, 0.32, 7.59, 5.06}, {0.476, 0.25, 4.57, 0.28, 7.79, 5.54}}},
+    {192, 128, {{0.549, 0.39, 4.08, 0.39, 5.78, 3.31}, {0.564, 0.28, 4.92, 0.57, 6.39, 5.45}}},
+    {256, 256, {{1.020, 0.28, 9.07, 0.84, 5.43, 10.00}, {1.360, 0.24, 5.80, 0.64, 5.69, 8.86}}},
 };
 
-// The shape of the least estimated time. The host knows only how many rows there are: they meet as many experts as choices at random do, and the
-// tiles that an expert has are those of rows spread like waiting times, 1 / (1 - exp(-tile / mean)).
+// The shape of the least estimated time: of its tiles' and of the weights' the longer, nearly. The host knows only how many rows there are: they
+// meet as many experts as choices at random do, and an expert has the tiles of a number of rows that is spread like waiting times, 1 / (1 - exp(-tile / mean)).
 static const GroupShape &choose_shape(const GroupGemm &g, int cus)
 {
     const double rows = static_cast<double>(g.rows), experts = -std::expm1(-rows / g.groups) * g.groups, each = rows / experts;
