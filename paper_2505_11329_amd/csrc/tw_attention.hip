@@ -16,6 +16,7 @@
 
 #include "tw_internal.h"
 #include "tw_mfma.h"
+#include "tw_scan.h"
 
 namespace tw {
 

@@ -4,7 +4,7 @@
 
 #include <stdint.h>
 
-#include "tw_device.h"
+#include "tw_scan.h"
 
 namespace tw {
 

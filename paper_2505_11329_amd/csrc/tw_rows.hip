@@ -655,10 +655,20 @@ tw_status tw_qk_norm_rope(const tw_qk_norm_rope_args *args, void *stream)
     TW_TRY(rope_sizes(a));
     if (a.tokens == 0) return TW_OK;
     TW_TRY(rope_tensors(a, false));
-    const RopeLayout l = rope_layout(a, false);
-    const RopeParams p = rope_params(a, l);
-    if (l.grid[0] + l.grid[1] > (1 << 23)) return TW_ERR_UNSUPPORTED;
-    return launch_rope<false>(a, l, p, static_cast<hipStream_t>(stream));
+    // a launch has at most 2^23 workgroups
+    const int64_t most = (int64_t(1) << 22) * (256 >> rope_layout(a, false).lanes_log2) / std::max(a.q_heads, a.kv_heads);
+    for (int64_t first = 0; first < a.tokens; first += most) {
+        tw_qk_norm_rope_args part = a;
+        part.tokens = std::min(most, a.tokens - first);
+        part.q = static_cast<const char *>(a.q) + first * a.q_stride * 2;
+        part.k = static_cast<const char *>(a.k) + first * a.k_stride * 2;
+        part.q_out = static_cast<char *>(a.q_out) + first * a.q_out_stride * 2;
+        part.k_out = static_cast<char *>(a.k_out) + first * a.k_out_stride * 2;
+        if (a.positions) part.positions = static_cast<const char *>(a.positions) + first * a.position_bytes;
+        const RopeLayout l = rope_layout(part, false);
+        TW_TRY(launch_rope<false>(part, l, rope_params(part, l), static_cast<hipStream_t>(stream)));
+    }
+    return TW_OK;
 }
 
 int64_t tw_qk_norm_rope_backward_workspace_bytes(const tw_qk_norm_rope_args *args)

@@ -111,7 +111,7 @@ def test_norm_rope_refuses():
     assert rope(**wide, q_out=addr(0) + 1008) == (E_ALIAS,) * 2                     # its end in the keys' columns
     assert rope(**wide, q_out=addr(0) + 1280) == (E_ALIAS,) * 2                     # its end in the next row's queries
     need = tw.qk_norm_rope_backward_workspace_bytes(10, 8, 2, 64, 64)
-    assert need > 0 and need % (2 * 64 * 4) == 0
+    assert need > 0 and need % (64 * 4) == 0        # rows of 64 sums, for the queries and for the keys
     assert rope(workspace=None)[1] == E_NULL and rope(size=need - 1)[1] == E_SHAPE and rope(workspace=addr(12) + 8)[1] == E_ALIGN
     for i in (0, 1, 2, 3, 4, 5, 6, 7, 8, 9, 10, 11):
         assert rope(workspace=addr(i), size=need)[1] == E_ALIAS, i

@@ -219,3 +219,22 @@ def test_captured_and_replayed_with_other_inputs(tw, sizes, lengths, padded):
         for name, t in d.items():
             n = {"dy": kept, "dh": kept, "dboth": kept, "drows": kept, "dq": live, "dk": live}.get(name, t.shape[0])
             assert torch.equal(t[:n], want_d[name][:n]), (i, name)
+
+
+def test_more_heads_than_one_launch_takes(tw):
+    """2^31 heads of 8 and some: the first tokens, those around where a launch ends, and the last."""
+    T, H, D = (1 << 21) + 5, 1024, 8
+    g = torch.Generator().manual_seed(9)
+    q, k = torch.zeros(T, H, D, dtype=torch.bfloat16, device="cuda"), torch.zeros(T, 1, D, dtype=torch.bfloat16, device="cuda")
+    rows = torch.tensor([0, 1, 7, (1 << 20) - 1, 1 << 20, (1 << 20) + 1, (1 << 21) - 1, 1 << 21, T - 2, T - 1]).cuda()
+    q[rows], k[rows] = (torch.randn(len(rows), n, D, generator=g).bfloat16().cuda() for n in (H, 1))
+    rotation, weight = L.table(64, D).cuda(), (1 + 0.1 * torch.randn(D, generator=g)).bfloat16().cuda()
+    at = (torch.arange(T, device="cuda", dtype=torch.int32) * 5) % 64
+    want = [L.norm_rope(x[rows], weight, at[rows], rotation, EPS, False) for x in (q, k)]
+    tw.qk_norm_rope(q, k, at, rotation, weight, weight, EPS, q_out=q, k_out=k)
+    R.assert_close(q[rows], *want[0], "q")
+    R.assert_close(k[rows], *want[1], "k")
+    keep = torch.ones(T, dtype=torch.bool, device="cuda")
+    keep[rows] = False
+    for x in (q, k):        # zeros, of either sign
+        assert not bool(x.view(T, -1).amax(1)[keep].any()) and not bool(x.view(T, -1).amin(1)[keep].any())
