@@ -167,8 +167,10 @@ __global__ __launch_bounds__((SmallTile<WM, WN, WVM, WVN, BK, S, LOADERS>::kThre
 
     const GroupedB grouped = group_argument(group...);
     int total_tiles = tiles_m * tiles_n;
+    KeptGroups kept;
     if constexpr (GROUPED) {
-        total_tiles = count_group_tiles(grouped.groups, BM, tiles_n);
+        kept = keep_groups(grouped.groups, BM, tiles_n);
+        total_tiles = kept.total;
         tiles_per_xcd = (total_tiles + kXcds - 1) / kXcds;
     }
     for (int w = blockIdx.x; w < tiles_per_xcd * kXcds; w += gridDim.x) {
@@ -180,7 +182,7 @@ __global__ __launch_bounds__((SmallTile<WM, WN, WVM, WVN, BK, S, LOADERS>::kThre
         const char *B_of = B;  // the weight of the tile's rows
         bool once = true;      // which no other tile of its group reads
         if constexpr (GROUPED) {
-            const GroupTile g = find_group_tile(grouped.groups, BM, tiles_n, lin);
+            const GroupTile g = find_group_tile(kept, BM, tiles_n, lin);
             const int tiles_of = static_cast<int>((static_cast<uint32_t>(g.rows) + BM - 1) / BM);
             once = tiles_of == 1;
             at = tile_at(g.tile, tiles_of, tiles_n, group_m);
