@@ -30,9 +30,9 @@ static tw_status expert_tensors(const void *a, uint64_t a_bytes, const void *b, 
 
 // The tile shapes: their size, and for weights stored [N x K] and [K x N] what a 64-deep K step of an almost empty tile takes with every
 // compute unit busy, how much of that more a full one, what a tile takes besides (us), the share of the time that goes by whole turns where tiles are few, the
-// rate at which the weights come in (TB/s) and what passes until they do (us). Fitted to 3200 products of 1 to 32768 rows, 8 to 160 experts, N and K of 256 to
-// 8192, with every shape timed: the choice is 2.3 % off the best of them on average, 2.6 % for [K x N]. (Without one of the shapes 3 to 7 %; 64 x 128 besides:
-// 0.4 % less.)
+// rate at which the weights come in (TB/s) and what passes until they do (us). Fitted to 3000 products of 1 to 32768 rows, 8 to 160 experts, N and K of 256 to
+// 8192, with every shape timed: the choice is 2.4 % off the best of them on average, 2.7 % for [K x N]. (The best without 16 x 32 is 4.3 and 3.4 % slower on average, without 16 x 64 5.0
+// and 3.5, 32 x 128 1.5 and 3.4, 128 x 128 1.0 and 0.9, 192 x 128 0.5 and 0.7, 256 x 256 0.8 and 0.4; 64 x 128, 64 x 64 and 32 x 32 besides gain less than 0.5 % each.)
 struct GroupShape {
     int rows, cols;
     struct {
@@ -40,23 +40,32 @@ struct GroupShape {
     } us[2];
 };
 static const GroupShape kGroupShapes[] = {
-    {32, 32, {{0.122, 0.04, 1.33, 0.13, 7.07, 3.42}, {0.162, 0.05, 1.09, 0.82, 6.73, 3.74}}},
-    {16, 64, {{0.186, 0.00, 1.08, 0.29, 9.00, 4.44}, {0.252, 0.00, 0.94, 1.00, 8.62, 4.39}}},
-    {32, 128, {{0.397, 0.00, 1.16, 0.74, 7.78, 5.29}, {0.451, 0.00, 0.82, 0.67, 9.00, 4.61}}},
-    {128, 128, {{0.392, 0.47, 4.69, 0.32, 7.59, 5.06}, {0.476, 0.25, 4.57, 0.28, 7.79, 5.54}}},
-    {192, 128, {{0.549, 0.39, 4.08, 0.39, 5.78, 3.31}, {0.564, 0.28, 4.92, 0.57, 6.39, 5.45}}},
-    {256, 256, {{1.020, 0.28, 9.07, 0.84, 5.43, 10.00}, {1.360, 0.24, 5.80, 0.64, 5.69, 8.86}}},
+    {16, 32, {{0.079, 0.16, 2.87, 0.65, 6.56, 2.52}, {0.126, 0.25, 2.34, 0.76, 5.14, 2.67}}},
+    {16, 64, {{0.186, 0.00, 1.06, 0.48, 9.00, 4.17}, {0.247, 0.00, 0.93, 0.94, 7.49, 4.23}}},
+    {32, 128, {{0.410, 0.00, 1.09, 0.45, 7.70, 4.81}, {0.441, 0.00, 0.67, 0.52, 9.00, 5.01}}},
+    {128, 128, {{0.422, 0.31, 4.35, 0.50, 7.47, 3.37}, {0.488, 0.18, 4.15, 0.27, 7.77, 4.60}}},
+    {192, 128, {{0.527, 0.47, 4.30, 0.20, 6.17, 5.73}, {0.564, 0.21, 4.83, 0.52, 6.02, 2.43}}},
+    {256, 256, {{1.080, 0.25, 6.87, 0.92, 4.83, 8.67}, {1.190, 0.32, 6.92, 0.81, 5.05, 13.70}}},
 };
+
+// As many tiles as there may be: every expert has one more than its rows fill, at most.
+static int64_t most_tiles(const GroupGemm &g, const GroupShape &s)
+{
+    return (g.rows / s.rows + std::min<int64_t>(g.groups, g.rows)) * ((g.N + s.cols - 1) / s.cols);
+}
+// Of a workgroup each but for the largest, whose workgroups stay.
+static bool launches(const GroupGemm &g, const GroupShape &s) { return most_tiles(g, s) <= (s.rows == 256 ? 1 << 30 : 1 << 22); }
 
 // The shape of the least estimated time: of its tiles' and of the weights' the longer, nearly. The host knows only how many rows there are: they
 // meet as many experts as choices at random do, and an expert has the tiles of a number of rows that is spread like waiting times, 1 / (1 - exp(-tile / mean)).
-static const GroupShape &choose_shape(const GroupGemm &g, int cus)
+static const GroupShape *choose_shape(const GroupGemm &g, int cus)
 {
     const double rows = static_cast<double>(g.rows), experts = -std::expm1(-rows / g.groups) * g.groups, each = rows / experts;
     const double weights = experts * static_cast<double>(g.N) * static_cast<double>(g.K) * 2e-6;  // MB
     const GroupShape *best = nullptr;
     double least = 0.0;
     for (const GroupShape &s : kGroupShapes) {
+        if (!launches(g, s)) continue;
         const auto &us = s.us[g.kn];
         const double tiles = -experts / std::expm1(-s.rows / each) * static_cast<double>((g.N + s.cols - 1) / s.cols);
         double turns = tiles / cus;
@@ -69,18 +78,17 @@ static const GroupShape &choose_shape(const GroupGemm &g, int cus)
             least = time;
         }
     }
-    return *best;
+    return best;
 }
 
 static tw_status launch_products(const GroupGemm &g, hipStream_t stream)
 {
     int cus = 0;
     TW_TRY(current_cu_count(&cus));
-    const GroupShape &s = choose_shape(g, cus);
-    // every expert has one tile more than its rows fill, at most
-    const int64_t tiles = (g.rows / s.rows + std::min<int64_t>(g.groups, g.rows)) * ((g.N + s.cols - 1) / s.cols);
-    if (tiles > (1 << 23)) return TW_ERR_UNSUPPORTED;
-    return s.rows == 256 ? launch_group_gemm(g, tiles, cus, stream) : launch_group_tile(g, s.rows, s.cols, tiles, stream);
+    const GroupShape *const s = choose_shape(g, cus);
+    if (!s) return TW_ERR_UNSUPPORTED;
+    const int64_t tiles = most_tiles(g, *s);
+    return s->rows == 256 ? launch_group_gemm(g, tiles, cus, stream) : launch_group_tile(g, s->rows, s->cols, tiles, stream);
 }
 
 }  // namespace tw

@@ -859,15 +859,15 @@ static tw_status launch_group_tile_t(const GroupGemm &g, int64_t tiles, hipStrea
 }
 
 // Weights that one tile of their expert reads go past the caches, others, which two tiles read at about the same time, do not: 3246 rows
-// of 64 experts, [2048 x 2816] each, 128 x 128 tiles: 159 us with all of them kept, 145 with none, 142 so. (32 x 32 tiles are taken for
+// of 64 experts, [2048 x 2816] each, 128 x 128 tiles: 159 us with all of them kept, 145 with none, 142 so. (16 x 32 tiles are taken for
 // little work, whose weights may well be in the cache.)
 tw_status launch_group_tile(const GroupGemm &g, int rows, int cols, int64_t tiles, hipStream_t stream)
 {
     const auto launch = [&](auto nk, auto kn) { return g.kn ? kn(g, tiles, stream) : nk(g, tiles, stream); };
-    if (rows == 16) return launch(launch_group_tile_t<false, 1, 1, 1, 4, 128, 4, true>, launch_group_tile_t<true, 1, 1, 1, 4, 128, 4, true>);
+    if (cols == 32) return launch(launch_group_tile_t<false, 1, 1, 1, 2, 256, 4, false>, launch_group_tile_t<true, 1, 1, 1, 2, 256, 4, false>);
+    if (cols == 64) return launch(launch_group_tile_t<false, 1, 1, 1, 4, 128, 4, true>, launch_group_tile_t<true, 1, 1, 1, 4, 128, 4, true>);
     if (rows == 128) return launch(launch_group_tile_t<false, 2, 4, 4, 2, 64, 4, true>, launch_group_tile_t<true, 2, 4, 4, 2, 64, 4, true>);
     if (rows == 192) return launch(launch_group_tile_t<false, 3, 4, 4, 2, 64, 3, false>, launch_group_tile_t<true, 3, 4, 4, 2, 64, 3, false>);
-    if (cols == 32) return launch(launch_group_tile_t<false, 1, 1, 2, 2, 128, 4, false>, launch_group_tile_t<true, 1, 1, 2, 2, 128, 4, false>);
     return launch(launch_group_tile_t<false, 1, 4, 2, 2, 64, 4, true>, launch_group_tile_t<true, 1, 4, 2, 2, 64, 4, true>);
 }
 

@@ -21,8 +21,8 @@ def spread_offsets(g, rows, E, ahead, behind):
     return torch.tensor([ahead] + cuts + [rows - behind], dtype=torch.int32).cuda()
 
 
-# rows, experts, N, K: tiles of 32 x 32, 16 x 64, 32 x 128, 128 x 128, 192 x 128 and 256 x 256 for one layout of the weights or both
-PRODUCTS = [(14, 2, 24, 376), (18, 9, 2344, 360), (41, 9, 976, 392), (18, 9, 2144, 368), (96, 8, 3592, 840), (5323, 5, 112, 328),
+# rows, experts, N, K: tiles of 16 x 32, 16 x 64, 32 x 128, 128 x 128, 192 x 128 and 256 x 256 for one layout of the weights or both
+PRODUCTS = [(14, 2, 24, 376), (4238, 5, 8, 352), (2336, 3, 40, 376), (4327, 5, 80, 328), (191, 9, 2928, 432), (2514, 9, 3112, 336), (18, 9, 2344, 360), (41, 9, 976, 392), (18, 9, 2144, 368), (96, 8, 3592, 840), (5323, 5, 112, 328),
             (5644, 5, 296, 328), (448, 9, 2992, 328), (768, 9, 2880, 344), (3163, 9, 2952, 336), (5301, 9, 1424, 336), (2600, 3, 1288, 1096)]
 
 
@@ -67,3 +67,17 @@ def test_weight_gradients_in_both_tiles(tw, lengths, N, K, kn):
         assert torch.equal(tw.expert_gemm_backward(A, dC, offsets, int(kn), dB=torch.full_like(want, math.nan)), want)
     normal_A, normal_dC = (torch.randn(rows, W, generator=g).bfloat16().cuda() for W in (K, N))
     R.assert_close(tw.expert_gemm_backward(normal_A, normal_dC, offsets, int(kn)), *L.weight_gradient(normal_A, normal_dC, offsets, E, kn), "dB")
+
+
+def test_more_rows_than_small_tiles_are_launched_for(tw):
+    """2^26 and some rows of few columns, for which a workgroup to a tile would be too many."""
+    g = torch.Generator().manual_seed(12)
+    rows = (1 << 26) + 77
+    A = whole(g, 4096, 8).repeat((rows + 4095) // 4096, 1)[:rows]
+    B, offsets = whole(g, 3, 8, 8), torch.tensor([5, 20_000_001, 20_000_001, rows - 3], dtype=torch.int32).cuda()
+    for kn in (False, True):
+        C = tw.expert_gemm(A, B, offsets, int(kn), C=torch.full((rows, 8), 7.0, dtype=torch.bfloat16, device="cuda"))
+        want = torch.full_like(C, 7.0)
+        for e, lo, hi in L.rows_of(offsets, rows):
+            want[lo:hi] = (A[lo:hi].float() @ (B[e].float() if kn else B[e].float().t())).bfloat16()
+        assert torch.equal(C, want), kn
