@@ -724,7 +724,8 @@ tw_status tw_expert_gemm_backward(const void *A, const void *dC, void *dB, const
  *   F         a multiple of 8, 8 ... TW_MAX_H;  rows < 2^31
  *   limit     device int32, 4-byte aligned, or NULL: rows from *limit on are left as they were (for rows sorted by expert:
  *             offsets + n_experts, so that rows without an expert cost nothing)
- * All of it is computed in fp32 and rounded once. Outputs must not overlap inputs but as stated.
+ * All of it is computed in fp32 and rounded once, also where exp(g) is less than fp32 holds and the factors beside it bring the result
+ * back; of finite numbers dout u alone may overflow ahead of its result. Outputs must not overlap inputs but as stated.
  */
 tw_status tw_gated_silu(const void *x, int64_t rows, int64_t F, const int32_t *limit, void *out, void *stream);
 

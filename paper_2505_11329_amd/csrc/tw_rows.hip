@@ -25,11 +25,18 @@ struct GateParams {
     uint32_t pieces;       // 16-byte pieces of F columns
 };
 
-// 1 / (1 + exp(-g)) without overflow: by exp(-|g|), which is at most 1.
-__device__ __forceinline__ float sigmoid(float g)
+// s = 1 / (1 + exp(-g)): r for g >= 0, a^3 r below, with a the cube root of exp(g). exp2 gives 0 where its result lies below 2^-126: for exp(g)
+// from g = -87.4 on, where products with large factors are not 0 before -190; for a from -262 on. With one a to each factor no product
+// overflows that the result does not (|g| a^2 < 1), and one that falls below 2^-126 meets no more than 1.1 behind it. (64810 rows of 1024,
+// gradient: 102.6 us, 101.6 with one exp(g) for all.)
+struct Gate {
+    float a, s;   // s a^2 is the gate's
+    float rest;   // 1 - s, without the difference
+};
+__device__ __forceinline__ Gate gate_of(float g)
 {
-    const float e = __builtin_amdgcn_exp2f(-fabsf(g) * kLog2e);
-    return (g >= 0.0f ? 1.0f : e) * __builtin_amdgcn_rcpf(1.0f + e);
+    const float a = __builtin_amdgcn_exp2f(-fabsf(g) * (kLog2e / 3.0f)), e = a * a * a, r = __builtin_amdgcn_rcpf(1.0f + e);
+    return g >= 0.0f ? Gate{1.0f, r, e * r} : Gate{a, a * r, r};
 }
 
 template <bool STREAMED>
@@ -53,16 +60,20 @@ __global__ __launch_bounds__(256) void gated_silu_kernel(GateParams p)
     unpack8(vu, u);
     if constexpr (!BACKWARD) {
 #pragma unroll
-        for (int k = 0; k < 8; ++k) u[k] *= g[k] * sigmoid(g[k]);
+        for (int k = 0; k < 8; ++k) {
+            const Gate t = gate_of(g[k]);
+            u[k] = (u[k] * t.a) * (g[k] * t.s) * t.a;
+        }
         put<STREAMED>(p.out, row * p.pieces + c, pack8(u));
     } else {
         float d[8];
         unpack8(__builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(p.dout) + row * p.pieces + c), d);
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
-            const float s = sigmoid(g[k]), gs = g[k] * s;
-            g[k] = d[k] * u[k] * fmaf(gs, 1.0f - s, s);
-            u[k] = d[k] * gs;
+            const Gate t = gate_of(g[k]);
+            const float gs = g[k] * t.s, slope = fmaf(g[k], t.rest, 1.0f) * t.s;
+            g[k] = (d[k] * u[k] * t.a) * slope * t.a;
+            u[k] = (d[k] * t.a) * gs * t.a;
         }
         put<STREAMED>(p.out, row * 2 * p.pieces + c, pack8(g));
         put<STREAMED>(p.out, row * 2 * p.pieces + p.pieces + c, pack8(u));
