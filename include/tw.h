@@ -808,7 +808,9 @@ tw_status tw_qk_norm_rope(const tw_qk_norm_rope_args *args, void *stream);
 /* dq_out and dk_out go to args->q_out and args->k_out. */
 tw_status tw_qk_norm_rope_backward(const tw_qk_norm_rope_args *args, void *workspace, int64_t workspace_bytes, void *stream);
 
-/* Bytes of workspace that the gradient needs for these sizes (of the pointers only whether there are weights counts); -1 for sizes it refuses. Host only. */
+/* Bytes of workspace that suffice for the gradient at these sizes, with a rotation of rot_dim columns and without one; -1 for sizes it
+ * refuses. Of the pointers only whether there are weights counts, but a rot_dim that no rotation can have is refused where there is a
+ * rotation and stands for none where there is not. Host only. */
 int64_t tw_qk_norm_rope_backward_workspace_bytes(const tw_qk_norm_rope_args *args);
 
 /* Compute units of the current device; -1 when no device can be queried. */

@@ -27,7 +27,7 @@ struct GateParams {
 
 // s = 1 / (1 + exp(-g)): r for g >= 0, a^3 r below, with a the cube root of exp(g). exp2 gives 0 where its result lies below 2^-126: for exp(g)
 // from g = -87.4 on, where products with large factors are not 0 before -190; for a from -262 on. With one a to each factor no product
-// overflows that the result does not (|g| a^2 < 1), and one that falls below 2^-126 meets no more than 1.1 behind it. (64810 rows of 1024,
+// overflows that the result does not (|g| a^2 < 1), and one that falls below 2^-126 meets no more than 1.1 behind it. (64080 rows of 1024,
 // gradient: 102.6 us, 101.6 with one exp(g) for all.)
 struct Gate {
     float a, s;   // s a^2 is the gate's
@@ -444,10 +444,9 @@ struct RopeLayout {
     int v, lanes_log2;
     int64_t grid[2];
 };
-static RopeLayout rope_layout(const tw_qk_norm_rope_args &a, bool backward)
+static RopeLayout rope_layout(const tw_qk_norm_rope_args &a, int rot, bool backward)
 {
     RopeLayout l;
-    const int rot = a.rotation ? a.rot_dim : 0;
     l.v = !a.interleaved && rot % 16 != 0 ? 4 : 8;
     const int chunks = a.head_dim / l.v, pairs = a.interleaved ? 0 : rot / 2 / l.v;
     const int lanes = pairs + (chunks - 2 * pairs + 1) / 2;
@@ -464,6 +463,14 @@ static RopeLayout rope_layout(const tw_qk_norm_rope_args &a, bool backward)
         l.grid[1] = std::min(l.grid[1], k);
     }
     return l;
+}
+
+static RopeLayout rope_layout(const tw_qk_norm_rope_args &a, bool backward) { return rope_layout(a, a.rotation ? a.rot_dim : 0, backward); }
+
+// The sums of the gradient's workgroups.
+static int64_t rope_part_bytes(const tw_qk_norm_rope_args &a, const RopeLayout &l)
+{
+    return a.q_weight ? (l.grid[0] + l.grid[1]) * a.head_dim * 4 : 0;
 }
 
 static RopeParams rope_params(const tw_qk_norm_rope_args &a, const RopeLayout &l)
@@ -685,9 +692,10 @@ tw_status tw_qk_norm_rope(const tw_qk_norm_rope_args *args, void *stream)
 int64_t tw_qk_norm_rope_backward_workspace_bytes(const tw_qk_norm_rope_args *args)
 {
     if (!args || rope_sizes(*args) != TW_OK) return -1;
-    if (args->tokens == 0 || !args->q_weight) return 0;
-    const RopeLayout l = rope_layout(*args, true);
-    return (l.grid[0] + l.grid[1]) * args->head_dim * 4;
+    if (args->tokens == 0) return 0;
+    // (a rotation never makes the launch smaller: its chunks are of 4 columns or of 8)
+    const bool rot = args->rot_dim >= 8 && args->rot_dim % 8 == 0 && args->rot_dim <= args->head_dim;
+    return rope_part_bytes(*args, rope_layout(*args, rot ? args->rot_dim : 0, true));
 }
 
 tw_status tw_qk_norm_rope_backward(const tw_qk_norm_rope_args *args, void *workspace, int64_t workspace_bytes, void *stream)
@@ -705,12 +713,12 @@ tw_status tw_qk_norm_rope_backward(const tw_qk_norm_rope_args *args, void *works
         return launch_join(a, nullptr, 0, 0, s);
     }
     TW_TRY(rope_tensors(a, true));
-    const int64_t need = tw_qk_norm_rope_backward_workspace_bytes(args);
+    const RopeLayout l = rope_layout(a, true);
+    const int64_t need = rope_part_bytes(a, l);
     if (need > 0 && !workspace) return TW_ERR_NULL;
     if (workspace_bytes < need) return TW_ERR_SHAPE;
     if (need > 0 && !aligned16(workspace)) return TW_ERR_ALIGN;
     TW_TRY(rope_workspace(a, workspace, static_cast<uint64_t>(need)));
-    const RopeLayout l = rope_layout(a, true);
     RopeParams p = rope_params(a, l);
     p.side[0].dy = static_cast<const char *>(a.dq);
     p.side[1].dy = static_cast<const char *>(a.dk);

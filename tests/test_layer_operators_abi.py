@@ -172,3 +172,29 @@ def test_the_binding_refuses_wrong_tensors_on_the_gpu():
         tw.qk_norm_rope_backward(q, k, p, r, q_weight=w, k_weight=w)
     with pytest.raises(tw.TwError):
         tw.qk_norm_rope(q, k, None, None)
+
+
+def test_norm_rope_workspace_before_the_tensors_are_there():
+    """Whether there is a rotation yet does not change the size: what the query says suffices for the call with one and without."""
+    f = tw.lib().tw_qk_norm_rope_backward_workspace_bytes
+    for tokens, q_heads, kv_heads, dim in ((1, 1, 1, 8), (10, 8, 2, 64), (40, 8, 2, 128), (300, 28, 4, 72), (20000, 32, 8, 128)):
+        for rot in range(8, dim + 1, 8):
+            for interleaved in (0, 1):
+                sizes = dict(tokens=tokens, q_heads=q_heads, kv_heads=kv_heads, head_dim=dim, rot_dim=rot, interleaved=interleaved,
+                             q_stride=q_heads * dim, k_stride=kv_heads * dim, q_out_stride=q_heads * dim, k_out_stride=kv_heads * dim,
+                             dq_stride=q_heads * dim, dk_stride=kv_heads * dim)
+                for i, name in enumerate(("q", "k", "q_out", "k_out", "dq", "dk")):
+                    sizes[name] = BASE + (i + 1) * 0x10_0000_0000
+                none = dict(rotation=None, positions=None)
+                need = f(ctypes.byref(rope_args(**{**sizes, **none})))
+                assert need > 0 and need == f(ctypes.byref(rope_args(**sizes))), sizes
+                bare = QkNormRopeArgs(tokens=tokens, q_heads=q_heads, kv_heads=kv_heads, head_dim=dim, rot_dim=rot, interleaved=interleaved,
+                                      q_weight=16, position_bytes=4)
+                assert f(ctypes.byref(bare)) == need, sizes
+                # enough (the address is refused after the size), and with the rotation not more than it takes
+                for given in ({}, none):
+                    assert rope(workspace=addr(12) + 8, size=need, **{**sizes, **given})[1] == E_ALIGN, (sizes, given)
+                assert rope(workspace=addr(12), size=need - 1, **sizes)[1] == E_SHAPE, sizes
+    # a rot_dim that is none where there is no rotation does not count
+    for rot in (0, -8, 20, 72, 1 << 30):
+        assert f(ctypes.byref(rope_args(rotation=None, positions=None, rot_dim=rot))) == tw.qk_norm_rope_backward_workspace_bytes(10, 8, 2, 64)
