@@ -193,8 +193,10 @@ def test_norm_rope_workspace_before_the_tensors_are_there():
                 assert f(ctypes.byref(bare)) == need, sizes
                 # enough (the address is refused after the size), and with the rotation not more than it takes
                 for given in ({}, none):
-                    assert rope(workspace=addr(12) + 8, size=need, **{**sizes, **given})[1] == E_ALIGN, (sizes, given)
-                assert rope(workspace=addr(12), size=need - 1, **sizes)[1] == E_SHAPE, sizes
+                    a = rope_args(**{**sizes, **given})
+                    assert tw.lib().tw_qk_norm_rope_backward(ctypes.byref(a), VP(addr(12) + 8), need, None) == E_ALIGN, (sizes, given)
+                a = rope_args(**sizes)
+                assert tw.lib().tw_qk_norm_rope_backward(ctypes.byref(a), VP(addr(12)), need - 1, None) == E_SHAPE, sizes
     # a rot_dim that is none where there is no rotation does not count
     for rot in (0, -8, 20, 72, 1 << 30):
         assert f(ctypes.byref(rope_args(rotation=None, positions=None, rot_dim=rot))) == tw.qk_norm_rope_backward_workspace_bytes(10, 8, 2, 64)
