@@ -259,6 +259,23 @@ typedef struct tw_attention_launch {
 
 tw_status tw_attention_plan(const tw_attention_args *args, tw_attention_launch *launch);
 
+/*
+ * The form of tw_expert_gemm's launch for these sizes on `cus` compute units, or, with backward, of tw_expert_gemm_backward's; all zero
+ * where nothing is launched. Errors as theirs for the sizes, TW_ERR_SHAPE for cus < 1, TW_ERR_NULL without a launch. Host arithmetic only.
+ *   tile_rows, tile_cols   of a tile (of an expert's rows and columns; backward: of its weights as they are stored)
+ *   tiles                  as many as there may be, whatever the offsets; backward: as many as there are
+ *   workgroups             fewer than tiles: they take one after the other
+ */
+typedef struct tw_expert_gemm_launch {
+    int tile_rows;
+    int tile_cols;
+    int64_t tiles;
+    int64_t workgroups;
+} tw_expert_gemm_launch;
+
+tw_status tw_expert_gemm_plan(int64_t rows, int64_t N, int64_t K, int n_experts, int b_layout, int backward, int cus,
+                              tw_expert_gemm_launch *launch);
+
 #ifdef __cplusplus
 }
 #endif

@@ -71,6 +71,11 @@ class QkNormRopeArgs(ctypes.Structure):
                 ("dk_stride", _i64)]
 
 
+class ExpertGemmLaunch(ctypes.Structure):
+    """struct tw_expert_gemm_launch"""
+    _fields_ = [("tile_rows", ctypes.c_int), ("tile_cols", ctypes.c_int), ("tiles", _i64), ("workgroups", _i64)]
+
+
 class AttentionLaunch(ctypes.Structure):
     """struct tw_attention_launch"""
     _fields_ = [("tile_rows", ctypes.c_int), ("key_waves", ctypes.c_int), ("chunks", ctypes.c_int), ("min_chunk", ctypes.c_int)]
@@ -199,6 +204,9 @@ def lib():
         for name in ("tw_expert_gemm", "tw_expert_gemm_backward"):
             getattr(L, name).argtypes = [_vp, _vp, _vp, _vp, _i64, _i64, _i64, ctypes.c_int, ctypes.c_int, _vp]
             getattr(L, name).restype = ctypes.c_int
+        L.tw_expert_gemm_plan.argtypes = [_i64, _i64, _i64, ctypes.c_int, ctypes.c_int, ctypes.c_int, ctypes.c_int,
+                                          ctypes.POINTER(ExpertGemmLaunch)]
+        L.tw_expert_gemm_plan.restype = ctypes.c_int
         L.tw_gated_silu.argtypes = [_vp, _i64, _i64, _vp, _vp, _vp]
         L.tw_gated_silu.restype = ctypes.c_int
         L.tw_gated_silu_backward.argtypes = [_vp, _vp, _i64, _i64, _vp, _vp, _vp]
@@ -579,6 +587,13 @@ def attention_plan(n_seqs, q_rows, k_rows, q_heads, kv_heads, head_dim):
     """tw_attention_plan: the form of the launch for tensors of these sizes, an AttentionLaunch."""
     a, launch = _attention_sizes(n_seqs, q_rows, k_rows, q_heads, kv_heads, head_dim), AttentionLaunch()
     _check(lib().tw_attention_plan(ctypes.byref(a), ctypes.byref(launch)), "tw_attention_plan")
+    return launch
+
+
+def expert_gemm_plan(rows, N, K, n_experts, b_layout=B_NK, backward=False, cus=256):
+    """tw_expert_gemm_plan: the form of expert_gemm's launch, or of expert_gemm_backward's, an ExpertGemmLaunch."""
+    launch = ExpertGemmLaunch()
+    _check(lib().tw_expert_gemm_plan(rows, N, K, n_experts, b_layout, int(backward), cus, ctypes.byref(launch)), "tw_expert_gemm_plan")
     return launch
 
 

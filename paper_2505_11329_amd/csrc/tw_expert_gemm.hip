@@ -3,6 +3,7 @@
 #include <cmath>
 
 #include "tw_internal.h"
+#include "tw_mfma.h"
 
 namespace tw {
 
@@ -81,14 +82,22 @@ static const GroupShape *choose_shape(const GroupGemm &g, int cus)
     return best;
 }
 
+static tw_status plan_products(const GroupGemm &g, int cus, GroupLaunch *l)
+{
+    const GroupShape *const s = choose_shape(g, cus);
+    if (!s) return TW_ERR_UNSUPPORTED;
+    const int64_t tiles = most_tiles(g, *s), slots = (tiles + kXcds - 1) / kXcds * kXcds;
+    *l = {s->rows, s->cols, tiles, s->rows == 256 ? std::min<int64_t>(slots, cus) : slots};
+    return TW_OK;
+}
+
 static tw_status launch_products(const GroupGemm &g, hipStream_t stream)
 {
     int cus = 0;
     TW_TRY(current_cu_count(&cus));
-    const GroupShape *const s = choose_shape(g, cus);
-    if (!s) return TW_ERR_UNSUPPORTED;
-    const int64_t tiles = most_tiles(g, *s);
-    return s->rows == 256 ? launch_group_gemm(g, tiles, cus, stream) : launch_group_tile(g, s->rows, s->cols, tiles, stream);
+    GroupLaunch l;
+    TW_TRY(plan_products(g, cus, &l));
+    return l.tile_rows == 256 ? launch_group_gemm(g, l, cus, stream) : launch_group_tile(g, l, stream);
 }
 
 }  // namespace tw
@@ -115,6 +124,20 @@ tw_status tw_expert_gemm_backward(const void *A, const void *dC, void *dB, const
     const bool nk = b_layout == TW_B_NK;
     return launch_expert_gradient(nk ? dC : A, nk ? A : dC, dB, offsets, rows, nk ? N : K, nk ? K : N, n_experts,
                                   static_cast<hipStream_t>(stream));
+}
+
+tw_status tw_expert_gemm_plan(int64_t rows, int64_t N, int64_t K, int n_experts, int b_layout, int backward, int cus,
+                              tw_expert_gemm_launch *launch)
+{
+    if (!launch) return TW_ERR_NULL;
+    TW_TRY(expert_sizes(rows, N, K, n_experts, b_layout));
+    if (cus < 1) return TW_ERR_SHAPE;
+    *launch = {};
+    if (N == 0 || (backward ? K : rows) == 0) return TW_OK;
+    const bool nk = b_layout == TW_B_NK;
+    if (!backward) return plan_products({nullptr, nullptr, nullptr, nullptr, rows, N, K, n_experts, !nk}, cus, launch);
+    *launch = plan_expert_gradient(rows, nk ? N : K, nk ? K : N, n_experts, cus);
+    return TW_OK;
 }
 
 }  // extern "C"

@@ -375,11 +375,35 @@ static bool thin_tiles(int64_t rows, int64_t M, int64_t N, int n_experts, int cu
     return rows < 400 * int64_t(n_experts) || 2 * large <= cus;
 }
 
+// Tiles of a run of neighbouring ones in an XCD, and the places of all runs, which are as many in each XCD.
+struct GradientRuns {
+    int64_t run, slots;
+};
+static GradientRuns gradient_runs(int64_t tiles, int at_once, int cus)
+{
+    const int64_t run = std::min<int64_t>((tiles + kXcds - 1) / kXcds, std::max(1, cus * at_once / kXcds));
+    return {run, ((tiles + run - 1) / run + kXcds - 1) / kXcds * kXcds * run};
+}
+
+GroupLaunch plan_expert_gradient(int64_t rows, int64_t M, int64_t N, int n_experts, int cus)
+{
+    const bool thin = thin_tiles(rows, M, N, n_experts, cus);
+    const int edge = thin ? kThinEdge : kEdge, at_once = thin ? kThinAtOnce : 1;
+    const int64_t tiles = (M + edge - 1) / edge * ((N + edge - 1) / edge) * n_experts, slots = gradient_runs(tiles, at_once, cus).slots;
+    // Workgroups that take tile after tile where these are few, else one for each: 2048 small tiles 13.4-20.4 us and 15.1-20.4, 7168 42-63 and 43-60, 16384 102-168 and 94-163.
+    const bool stay = !thin || slots <= int64_t(4) * cus * at_once;
+    return {edge, edge, tiles, std::min<int64_t>(slots, stay ? cus * at_once : 1 << 20)};
+}
+
 tw_status launch_expert_gradient(const void *x, const void *y, void *out, const int32_t *offsets, int64_t rows, int64_t M, int64_t N,
                                  int n_experts, hipStream_t stream)
 {
     int cus = 0;
     TW_TRY(current_cu_count(&cus));
+    const GroupLaunch l = plan_expert_gradient(rows, M, N, n_experts, cus);
+    if (l.tiles > (1 << 30)) return TW_ERR_UNSUPPORTED;
+    const bool thin = l.tile_rows == kThinEdge;
+    const GradientRuns runs = gradient_runs(l.tiles, thin ? kThinAtOnce : 1, cus);
     GradientParams p = {};
     p.x = static_cast<const char *>(x);
     p.y = static_cast<const char *>(y);
@@ -387,20 +411,13 @@ tw_status launch_expert_gradient(const void *x, const void *y, void *out, const 
     p.groups = {offsets, n_experts, static_cast<int>(rows)};
     p.M = static_cast<int>(M);
     p.N = static_cast<int>(N);
-    const bool thin = thin_tiles(rows, M, N, n_experts, cus);
-    const int edge = thin ? kThinEdge : kEdge, at_once = thin ? kThinAtOnce : 1;
-    p.tiles_m = static_cast<int>((M + edge - 1) / edge);
-    p.tiles_n = static_cast<int>((N + edge - 1) / edge);
-    const int64_t tiles = int64_t(p.tiles_m) * p.tiles_n * n_experts;
-    if (tiles > (1 << 30)) return TW_ERR_UNSUPPORTED;
-    p.tiles = static_cast<int>(tiles);
-    p.run = static_cast<int>(std::min<int64_t>((tiles + kXcds - 1) / kXcds, std::max(1, cus * at_once / kXcds)));
-    const int64_t runs = (tiles + p.run - 1) / p.run;
-    p.slots = static_cast<int>((runs + kXcds - 1) / kXcds * kXcds * p.run);
-    p.group_m = tile_group_m(p.tiles_m, p.run, edge, edge, cus);
-    // Workgroups that take tile after tile where these are few, else one for each: 2048 small tiles 13.4-20.4 us and 15.1-20.4, 7168 42-63 and 43-60, 16384 102-168 and 94-163.
-    const bool stay = !thin || p.slots <= 4 * cus * at_once;
-    const dim3 grid(static_cast<uint32_t>(std::min(p.slots, stay ? cus * at_once : 1 << 20)));
+    p.tiles_m = static_cast<int>((M + l.tile_rows - 1) / l.tile_rows);
+    p.tiles_n = static_cast<int>((N + l.tile_cols - 1) / l.tile_cols);
+    p.tiles = static_cast<int>(l.tiles);
+    p.run = static_cast<int>(runs.run);
+    p.slots = static_cast<int>(runs.slots);
+    p.group_m = tile_group_m(p.tiles_m, p.run, l.tile_rows, l.tile_cols, cus);
+    const dim3 grid(static_cast<uint32_t>(l.workgroups));
     if (thin) {
         TW_HIP(launch_kernel(expert_gradient_thin_kernel, grid, dim3(64 * kWaves), kThinLds, stream, p));
         return TW_OK;

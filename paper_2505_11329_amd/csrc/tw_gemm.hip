@@ -927,30 +927,30 @@ static tw_status launch_cfg(const tw_gemm_args &g, int budget, hipStream_t strea
     return TW_OK;
 }
 
-// Products by group on tiles of 256 x 256, a workgroup to a compute unit. `tiles`: as many as there may be. 65536 rows of 64 experts,
+// Products by group on tiles of 256 x 256, a workgroup to a compute unit. 65536 rows of 64 experts,
 // [4096 x 2048] each: 944 us, 1.16 PFLOP/s, an eighth of it on rows that are not there.
 template <bool B_KN, int WM, int WN, int STAGES>
-static tw_status launch_group_cfg(const GroupGemm &g, int64_t tiles, int cus, hipStream_t stream)
+static tw_status launch_group_cfg(const GroupGemm &g, const GroupLaunch &l, int cus, hipStream_t stream)
 {
     using Cfg = TileCfg<WM, WN, STAGES, 64>;
-    const int64_t tiles_n = (g.N + Cfg::kBN - 1) / Cfg::kBN, slots = (tiles + kXcds - 1) / kXcds * kXcds;
+    const int64_t tiles_n = (g.N + Cfg::kBN - 1) / Cfg::kBN;
     auto kern = gemm_bf16_kernel<B_KN, WM, WN, STAGES, 64, false, false, GroupedB>;
     static std::atomic<int> allowed[kMaxDevices];
     TW_TRY(allow_dynamic_lds(reinterpret_cast<const void *>(kern), Cfg::kLdsBytes, allowed));
     const GroupedB group = {{g.offsets, g.groups, static_cast<int>(g.rows)}, g.N * g.K * 2};
     // (the block of tiles as for the rows of an average group)
     const int64_t tiles_m = std::max<int64_t>(1, (g.rows / g.groups + BM / 2) / BM);
-    TW_HIP(launch_kernel(kern, dim3(static_cast<uint32_t>(std::min<int64_t>(slots, cus))), dim3(Cfg::kThreads), Cfg::kLdsBytes, stream,
+    TW_HIP(launch_kernel(kern, dim3(static_cast<uint32_t>(l.workgroups)), dim3(Cfg::kThreads), Cfg::kLdsBytes, stream,
                          static_cast<const char *>(g.A), static_cast<const char *>(g.B), static_cast<char *>(g.C),
                          static_cast<int>(g.N), static_cast<int>(g.K), 0, static_cast<int>(tiles_n), 0,
-                         tile_group_m(tiles_m, std::max<int64_t>(1, tiles / kXcds), BM, Cfg::kBN, cus), 0, 0u,
+                         tile_group_m(tiles_m, std::max<int64_t>(1, l.tiles / kXcds), BM, Cfg::kBN, cus), 0, 0u,
                          static_cast<unsigned long long *>(nullptr), group));
     return TW_OK;
 }
 
-tw_status launch_group_gemm(const GroupGemm &g, int64_t tiles, int cus, hipStream_t stream)
+tw_status launch_group_gemm(const GroupGemm &g, const GroupLaunch &l, int cus, hipStream_t stream)
 {
-    return g.kn ? launch_group_cfg<true, 8, 8, 5>(g, tiles, cus, stream) : launch_group_cfg<false, 8, 8, 2>(g, tiles, cus, stream);
+    return g.kn ? launch_group_cfg<true, 8, 8, 5>(g, l, cus, stream) : launch_group_cfg<false, 8, 8, 2>(g, l, cus, stream);
 }
 
 // Share of the launch's compute-unit slots that hold a tile when `tiles` tiles

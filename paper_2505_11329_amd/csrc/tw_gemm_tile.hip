@@ -843,15 +843,15 @@ int small_tile_loading_waves(const tw_gemm_args &g, int shape, const HelpPlan &h
 // many further than its neighbour): begun together they ask for the same columns of all their rows at one time, which lie in a few of
 // the memory's channels where rows are 4 or 8 KB apart. 96 rows of 8 experts, [4096 x 3584] each, 64 x 128 tiles: 46.5 to 36.7 us.
 template <bool B_KN, int WM, int WN, int WVM, int WVN, int BK, int S, bool STREAM>
-static tw_status launch_group_tile_t(const GroupGemm &g, int64_t tiles, hipStream_t stream)
+static tw_status launch_group_tile_t(const GroupGemm &g, const GroupLaunch &l, hipStream_t stream)
 {
     using T = SmallTile<WM, WN, WVM, WVN, BK, S, false>;
-    const int64_t tiles_n = (g.N + T::BN - 1) / T::BN, slots = (tiles + kXcds - 1) / kXcds * kXcds;
+    const int64_t tiles_n = (g.N + T::BN - 1) / T::BN;
     auto kern = gemm_tile_kernel<B_KN, WM, WN, WVM, WVN, BK, S, false, STREAM, false, GroupedB>;
     static std::atomic<int> allowed[kMaxDevices];
     TW_TRY(allow_dynamic_lds(reinterpret_cast<const void *>(kern), T::kLdsBytes, allowed));
     const GroupedB group = {{g.offsets, g.groups, static_cast<int>(g.rows)}, g.N * g.K * 2};
-    TW_HIP(launch_kernel(kern, dim3(static_cast<uint32_t>(slots)), dim3(T::kThreads), T::kLdsBytes, stream,
+    TW_HIP(launch_kernel(kern, dim3(static_cast<uint32_t>(l.workgroups)), dim3(T::kThreads), T::kLdsBytes, stream,
                          static_cast<const char *>(g.A), static_cast<const char *>(g.B), static_cast<char *>(g.C),
                          static_cast<int>(g.N), static_cast<int>(g.K), 0, static_cast<int>(tiles_n), 1,
                          4, 0, 0u, group));  // (blocks of four rows of tiles: those that read one weight next to each other)
@@ -861,13 +861,13 @@ static tw_status launch_group_tile_t(const GroupGemm &g, int64_t tiles, hipStrea
 // Weights that one tile of their expert reads go past the caches, others, which two tiles read at about the same time, do not: 3246 rows
 // of 64 experts, [2048 x 2816] each, 128 x 128 tiles: 159 us with all of them kept, 145 with none, 142 so. (16 x 32 tiles are taken for
 // little work, whose weights may well be in the cache.)
-tw_status launch_group_tile(const GroupGemm &g, int rows, int cols, int64_t tiles, hipStream_t stream)
+tw_status launch_group_tile(const GroupGemm &g, const GroupLaunch &l, hipStream_t stream)
 {
-    const auto launch = [&](auto nk, auto kn) { return g.kn ? kn(g, tiles, stream) : nk(g, tiles, stream); };
-    if (cols == 32) return launch(launch_group_tile_t<false, 1, 1, 1, 2, 256, 4, false>, launch_group_tile_t<true, 1, 1, 1, 2, 256, 4, false>);
-    if (cols == 64) return launch(launch_group_tile_t<false, 1, 1, 1, 4, 128, 4, true>, launch_group_tile_t<true, 1, 1, 1, 4, 128, 4, true>);
-    if (rows == 128) return launch(launch_group_tile_t<false, 2, 4, 4, 2, 64, 4, true>, launch_group_tile_t<true, 2, 4, 4, 2, 64, 4, true>);
-    if (rows == 192) return launch(launch_group_tile_t<false, 3, 4, 4, 2, 64, 3, false>, launch_group_tile_t<true, 3, 4, 4, 2, 64, 3, false>);
+    const auto launch = [&](auto nk, auto kn) { return g.kn ? kn(g, l, stream) : nk(g, l, stream); };
+    if (l.tile_cols == 32) return launch(launch_group_tile_t<false, 1, 1, 1, 2, 256, 4, false>, launch_group_tile_t<true, 1, 1, 1, 2, 256, 4, false>);
+    if (l.tile_cols == 64) return launch(launch_group_tile_t<false, 1, 1, 1, 4, 128, 4, true>, launch_group_tile_t<true, 1, 1, 1, 4, 128, 4, true>);
+    if (l.tile_rows == 128) return launch(launch_group_tile_t<false, 2, 4, 4, 2, 64, 4, true>, launch_group_tile_t<true, 2, 4, 4, 2, 64, 4, true>);
+    if (l.tile_rows == 192) return launch(launch_group_tile_t<false, 3, 4, 4, 2, 64, 3, false>, launch_group_tile_t<true, 3, 4, 4, 2, 64, 3, false>);
     return launch(launch_group_tile_t<false, 1, 4, 2, 2, 64, 4, true>, launch_group_tile_t<true, 1, 4, 2, 2, 64, 4, true>);
 }
 

@@ -128,13 +128,16 @@ struct GroupGemm {
     int groups;
     bool kn;
 };
-// `tiles` is as many as there may be. On tiles of 256 x 256 (tw_gemm.hip);
-tw_status launch_group_gemm(const GroupGemm &g, int64_t tiles, int cus, hipStream_t stream);
+// The form of a launch: its tiles, as many as there may be, and the workgroups that take them.
+using GroupLaunch = tw_expert_gemm_launch;
+// On tiles of 256 x 256 (tw_gemm.hip);
+tw_status launch_group_gemm(const GroupGemm &g, const GroupLaunch &l, int cus, hipStream_t stream);
 // on those of 16 x 32, 16 x 64, or 32, 128 or 192 x 128 (tw_gemm_tile.hip).
-tw_status launch_group_tile(const GroupGemm &g, int rows, int cols, int64_t tiles, hipStream_t stream);
+tw_status launch_group_tile(const GroupGemm &g, const GroupLaunch &l, hipStream_t stream);
 // out[e](m, n) = sum over the rows r of group e of x[r, m] y[r, n] (tw_expert_gradient.hip).
 tw_status launch_expert_gradient(const void *x, const void *y, void *out, const int32_t *offsets, int64_t rows, int64_t M, int64_t N,
                                  int n_experts, hipStream_t stream);
+GroupLaunch plan_expert_gradient(int64_t rows, int64_t M, int64_t N, int n_experts, int cus);
 
 // ---- fork/join events (tw_host.hip) ----
 // A small per-device pool of timing-disabled events used to order streams.

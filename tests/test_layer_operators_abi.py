@@ -200,3 +200,36 @@ def test_norm_rope_workspace_before_the_tensors_are_there():
     # a rot_dim that is none where there is no rotation does not count
     for rot in (0, -8, 20, 72, 1 << 30):
         assert f(ctypes.byref(rope_args(rotation=None, positions=None, rot_dim=rot))) == tw.qk_norm_rope_backward_workspace_bytes(10, 8, 2, 64)
+
+
+def test_expert_gemm_plan():
+    L, launch = tw.lib(), tw.ExpertGemmLaunch()
+
+    def plan(rows=10, N=64, K=128, E=4, layout=0, backward=0, cus=256, to=ctypes.byref(launch)):
+        return L.tw_expert_gemm_plan(rows, N, K, E, layout, backward, cus, to)
+
+    for backward in (0, 1):
+        assert plan(backward=backward, to=None) == E_NULL
+        for change in (dict(rows=-1), dict(N=-8), dict(K=-8), dict(E=0), dict(layout=2), dict(cus=0), dict(cus=-1)):
+            assert plan(backward=backward, **change) == E_SHAPE, change
+        for change in (dict(rows=1 << 31), dict(N=60), dict(K=4), dict(N=(1 << 17) + 8), dict(K=(1 << 17) + 8), dict(E=1025)):
+            assert plan(backward=backward, **change) == E_UNSUP, change
+        assert plan(backward=backward, N=0) == OK and launch.tiles == launch.workgroups == launch.tile_rows == launch.tile_cols == 0
+    assert plan(rows=0) == OK and launch.tiles == 0
+    assert plan(rows=0, backward=1) == OK and launch.tiles > 0      # gradients of 0 are written
+    assert plan(K=0) == OK and launch.tiles > 0                     # and sums of nothing
+    assert plan(K=0, backward=1) == OK and launch.tiles == 0
+    for layout in (0, 1):
+        # no more tiles than a launch takes, whatever the sizes; as many workgroups as compute units for tiles that fill one
+        for rows in (1, 7, 100, 5000, 100_000, (1 << 31) - 1):
+            for E in (1, 8, 1024):
+                for N, K in ((8, 8), (4096, 2048), (1 << 17, 64), (1 << 17, 1 << 17)):
+                    if rows * N >= 1 << 46:     # more than 2^30 tiles: results of 140 TB
+                        continue
+                    f = tw.expert_gemm_plan(rows, N, K, E, layout)
+                    assert 1 <= f.tiles <= 1 << 30 and f.tile_rows >= 16 and f.tile_cols >= 32, (rows, E, N, K)
+                    assert f.tiles >= (rows + f.tile_rows - 1) // f.tile_rows * ((N + f.tile_cols - 1) // f.tile_cols)
+                    assert f.workgroups == 256 if f.tile_rows == 256 and f.tiles > 256 else f.tiles <= f.workgroups < f.tiles + 8
+                    b = tw.expert_gemm_plan(rows, N, K, E, layout, True)
+                    edge = b.tile_rows
+                    assert edge == b.tile_cols and edge in (128, 256) and b.tiles == -(-N // edge) * -(-K // edge) * E and b.workgroups >= 1
