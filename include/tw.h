@@ -704,7 +704,9 @@ tw_status tw_expert_combine_backward(const void *dout, const void *y, int64_t ro
  *   N, K          multiples of 8, at most TW_MAX_EXPERT_WIDTH; K == 0: rows of C that have an expert are 0
  *   n_experts     1 ... TW_MAX_EXPERTS
  * What a row, or a weight's gradient, comes to depends on its own inputs and on the form of the launch, which follows from
- * the sizes of the call alone; no atomics order any sum. Inf and NaN propagate by IEEE rules within their row (their
+ * the sizes of the call alone (tw_expert_gemm_plan); no atomics order any sum. The order of a sum over K goes by the form and by
+ * the place of the column among all N: equal weights in two columns may give results that differ by the rounding of their sums,
+ * and so may tw_gemm_bf16 on one expert's rows. Inf and NaN propagate by IEEE rules within their row (their
  * expert's gradient) and reach no other. Outputs must not overlap inputs.
  */
 #define TW_MAX_EXPERT_WIDTH (1 << 17)

@@ -3,7 +3,8 @@
 // are read once and that is all the work) and batches of up to a thousand rows or
 // so. Same product, same bits: every output is the chain of its K / 32 partial dot
 // products (v_mfma_f32_16x16x32_bf16) in the order of increasing k, so K is never
-// split, and parallelism comes from the tile shape alone.
+// split, and parallelism comes from the tile shape alone. (Products by group begin that chain at another
+// step of K in each column of tiles, and go round: see launch_group_tile_t.)
 //
 // What bounds it: what a compute unit can pull into its LDS. Whatever the tile, a
 // compute unit takes in 64 to 72 GB/s of operands (90 to 100 requests, 11 to 13 KB,
@@ -120,7 +121,7 @@ struct StageFrags {
 // no division that tile_at can spare, the fragment addresses later. (16 rows, K = 1024, N =
 // 8192: 5.6 -> 5.1 us; K = 8192, N = 3584: 13.7 -> 13.2; 512 x 4096 x 2048: 15.0 -> 14.7.)
 // last_rows: rows of A in the last row of tiles.
-// GROUP: as in tw_gemm.hip.
+// GROUP: as in tw_gemm.hip; last_rows is then how many steps of K later each column of tiles begins than the one before it.
 template <bool B_KN, int WM, int WN, int WVM, int WVN, int BK, int S, bool LOADERS, bool STREAM_B, bool ROLLS, typename... GROUP>
 __global__ __launch_bounds__((SmallTile<WM, WN, WVM, WVN, BK, S, LOADERS>::kThreads)) void gemm_tile_kernel(
     const char *A, const char *B, char *C, int N, int K, int tiles_m, int tiles_n, int last_rows, int group_m,
@@ -841,7 +842,8 @@ int small_tile_loading_waves(const tw_gemm_args &g, int shape, const HelpPlan &h
 
 // Products by group, a workgroup to a tile. Each tile begins at another step of K (`last_rows`, which groups have no use for, says how
 // many further than its neighbour): begun together they ask for the same columns of all their rows at one time, which lie in a few of
-// the memory's channels where rows are 4 or 8 KB apart. 96 rows of 8 experts, [4096 x 3584] each, 64 x 128 tiles: 46.5 to 36.7 us.
+// the memory's channels where rows are 4 or 8 KB apart. 96 rows of 8 experts, [4096 x 3584] each, 32 x 128 tiles: 43.1 to 36.4 us; 3246 rows
+// of 64, [2048 x 2816] each, 128 x 128 tiles: 145 to 136.
 template <bool B_KN, int WM, int WN, int WVM, int WVN, int BK, int S, bool STREAM>
 static tw_status launch_group_tile_t(const GroupGemm &g, const GroupLaunch &l, hipStream_t stream)
 {

@@ -83,8 +83,9 @@ __global__ __launch_bounds__(256) void gated_silu_kernel(GateParams p)
 // ---- norms and rotation ----
 //
 // A head belongs to a group of up to 16 lanes, each of which has two chunks of V columns of it: of rotated halves the two whose
-// columns are pairs, so that nothing but the norm's sums goes from lane to lane. Bound by memory: 16384 tokens, 32 / 8 heads of 128
-// take 59 us, 5.6 TB/s of what is read and written, as a copy does, 8101 of 28 / 4 heads 27 us. (The angles come from the caches
+// columns are pairs, so that nothing but the norm's sums goes from lane to lane. 16384 tokens, 32 / 8 heads of 128 take 60 us, 5.6 TB/s of
+// what is read and written, 8101 of 28 / 4 heads 25.5, where the activation's gradient has 6.4: a wave has one round of loads under way,
+// between the position's and the angles', and its stores behind them. (The angles come from the caches
 // for each head: two, four and eight heads of a token to a group, with their loads under way together, are 3 to 15 % slower.)
 
 // Queries or keys.
@@ -277,7 +278,8 @@ __global__ __launch_bounds__(256) void qk_norm_rope_kernel(RopeParams p)
 }
 
 // The gradient. The sums over tokens of the weights' gradient stay in registers; the workgroup's groups are added in their order.
-// 16384 tokens, 32 / 8 heads of 128: 98 us, 5.1 TB/s (the next head's loads ahead of this one's work: 101).
+// 16384 tokens, 32 / 8 heads of 128: 98 us, 5.1 TB/s, 4.5 us of it the join: with norms 118 registers, four waves to a SIMD, each with one
+// head's loads under way (the next head's ahead of this one's work: 101).
 template <int V, bool NEXT, bool NORM, bool STREAMED>
 __global__ __launch_bounds__(256) void qk_norm_rope_backward_kernel(RopeParams p)
 {
