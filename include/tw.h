@@ -743,7 +743,8 @@ tw_status tw_gated_silu_backward(const void *dout, const void *x, int64_t rows, 
  *       y[a] = z[a] cos - z[b] sin,  y[b] = z[b] cos + z[a] sin,   cos, sin = rotation[p][i], rotation[p][rot_dim/2 + i]
  *       pair i is a, b = i, i + rot_dim/2, or, interleaved, a, b = 2i, 2i + 1;  i < rot_dim/2
  *
- * in fp32, rounded to bf16 once.
+ * in fp32, rounded to bf16 once (the sum of squares is in fp32 as well: a head of finite elements whose squares add up to 2^128 or more
+ * comes out 0, and its gradient 0 or NaN).
  *
  *   q, k            device bf16, token t, head h, at q + t * q_stride + h * head_dim (strides count elements); may be
  *                   columns of one buffer (the result of one projection)

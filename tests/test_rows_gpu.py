@@ -290,3 +290,17 @@ def test_no_tokens(tw):
                                    dq_out=dq, dk_out=dk)
     assert bool(dq.isnan().all()) and not bool(got[2].any()) and not bool(got[3].any())
     assert tw.gated_silu(torch.empty(0, 64, dtype=torch.bfloat16, device="cuda")).shape == (0, 32)
+
+
+def test_heads_whose_squares_overflow_are_0(tw):
+    """The sum of squares is in fp32: Inf from 2^128 on. Other heads of the token are as they are without it."""
+    g = torch.Generator().manual_seed(6)
+    q, k = normal(g, 5, 4, 64), normal(g, 5, 2, 64)
+    w, rotation, at = normal(g, 64), L.table(16, 64).cuda(), torch.arange(5).cuda()
+    clean = tw.qk_norm_rope(q, k, at, rotation, w, w)
+    q[1, 2, 7], k[3, 1] = -2.0 ** 64, 2.0 ** 62
+    out = tw.qk_norm_rope(q, k, at, rotation, w, w)
+    assert not bool(out[0][1, 2].any()) and not bool(out[1][3, 1].any())
+    for x, was, head in ((out[0], clean[0], (1, 2)), (out[1], clean[1], (3, 1))):
+        x[head] = was[head]
+        assert torch.equal(x, was)
